@@ -240,6 +240,65 @@ int blossom_copy_rows(int32_t batch, int32_t heads, int32_t seq_len, int32_t row
                       const int64_t *src_strides /* host */, void *dst,
                       const int64_t *dst_strides /* host */, blossom_stream_t stream);
 
+/*
+ * The rows around the attention in a training step (paper: Eq. 20-22, S = LN(H + Drop(O))): dropout from a
+ * counter-based generator, and the sub-layer ending
+ * out = LayerNorm(residual + dropout(x)) of a post-norm encoder, forward and backward.
+ *
+ * Which elements a dropout keeps is a function of (seed, step, site, row, column) alone and is never
+ * stored: the backward forms it again.  Philox 4x32 with ten rounds (Salmon et al., "Parallel random
+ * numbers: as easy as 1, 2, 3", 2011) under the 64-bit key `seed` of the counter
+ * (column / 8 + 65536 * site, row, low and high word of `step`) gives 8 numbers of 16 bits for the 8 columns of
+ * a group, word i the columns 8 g + 2 i (low half) and 8 g + 2 i + 1 (high half); an element is kept if
+ * its number is at least thr = floor(65536 * dropout + 1/2), and is then scaled by 65536 / (65536 - thr), so that
+ * the expectation is exact for the probability in use, thr / 65536.  A dropped element is 0 whatever was there.
+ *
+ * Tensors are rows of cols elements, row r at r * stride (elements; 0 = cols, else at least cols); any
+ * alignment of the element type (16-byte aligned rows of a multiple of 8 columns take the widest accesses).  Sums,
+ * mean, variance and gradients are formed in single precision from the unrounded residual + dropout(x) and
+ * rounded once to the tensor's type.  The same call gives the same bits.
+ */
+typedef struct {
+  int64_t rows;         /* 0 <= rows < 2^31; 0: nothing but dweight, dbias (zeros) is written           */
+  int32_t cols;         /* 1 .. 8192                                                                   */
+  int32_t dtype;        /* of x, residual, out, dout, dx, dresidual                                    */
+  int32_t weight_dtype; /* of weight, bias, dweight, dbias                                             */
+  int32_t site;         /* 0 .. 65535: tells the dropouts of one step apart (layer, sub-layer)         */
+  double dropout;       /* 0 <= dropout <= 1; 0: everything is kept, unscaled, and rng may be NULL     */
+  double eps;           /* >= 0, added to the variance                                                 */
+  int64_t x_stride, residual_stride;
+  int64_t out_stride;   /* of out (forward) or dout (backward)                                         */
+  int64_t dx_stride, dresidual_stride;
+} blossom_rows_params;
+
+/* out = dropout(x); its gradient is the same call on dout.  out may be x itself (with the same stride).
+ *   rng   in   int64 [2] = (seed, step), read on the device when the kernel runs: a captured graph takes the
+ *              step that is there when it is replayed */
+int blossom_dropout(const blossom_rows_params *params /* host */, const void *x, const int64_t *rng, void *out,
+                    blossom_stream_t stream);
+
+/* out = (z - mean) * rstd * weight + bias with z = residual + dropout(x), mean and variance (of the cols elements) per
+ * row, rstd = 1 / sqrt(variance + eps).
+ *   residual      in   may be NULL (z = dropout(x))
+ *   weight, bias  in   [cols], either may be NULL (ones, zeros)
+ *   stats         out  float [rows][2] = (mean, rstd), 8-byte aligned; NULL if no backward follows */
+int blossom_add_norm_fwd(const blossom_rows_params *params /* host */, const void *x, const void *residual,
+                         const void *weight, const void *bias, const int64_t *rng, void *out, float *stats,
+                         blossom_stream_t stream);
+
+/* Backward: a = dout * weight, n = (z - mean) * rstd, dz = rstd * (a - mean(a) - n * mean(a * n)); dresidual = dz,
+ * dx = dz where kept, scaled, else 0; dweight = sum over rows of dout * n, dbias = sum over rows of dout.
+ *   x, residual, weight, rng   in   as given to the forward (z and what is kept are formed again)
+ *   dx, dresidual              out  either may be NULL (not wanted); without dropout they are equal, so one suffices
+ *   dweight, dbias             out  [cols], either may be NULL (not wanted)
+ *   workspace                  blossom_add_norm_workspace_bytes, 256-byte aligned: partial sums of dweight and dbias,
+ *                              added up in a fixed order; carries nothing from call to call */
+int blossom_add_norm_bwd(const blossom_rows_params *params /* host */, const void *x, const void *residual,
+                         const void *weight, const int64_t *rng, const float *stats, const void *dout, void *dx,
+                         void *dresidual, void *dweight, void *dbias, void *workspace, size_t workspace_bytes,
+                         blossom_stream_t stream);
+size_t blossom_add_norm_workspace_bytes(const blossom_rows_params *params /* host */);
+
 /* Synchronises the stream and copies the workspace's device status to *host_out (host): 0 = no
  * device-side error, else a blossom_status.  The workspace holds one status word for the forward
  * (blossom_select_blocks and blossom_attn_fwd clear both words when they start: a new step) and

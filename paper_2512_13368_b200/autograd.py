@@ -59,19 +59,22 @@ def check_arguments(q, k, v, gate_logits, seq_lens, require_cuda=True, gate_mode
     return seq_lens
 
 
-_native = None
+_native = _mod = None
 
 
 def _module():
     """``csrc/front.cpp`` as a module; the library it links is loaded first (the same instance, and its own
     message if it is missing)."""
-    binding.load()
-    try:
-        from . import _front as m
-    except ImportError as e:
-        raise RuntimeError("_front.so is missing or stale: build it with "
-                           "`python -m paper_2512_13368_b200.build`") from e
-    return m
+    global _mod
+    if _mod is None:
+        binding.load()
+        try:
+            from . import _front as m
+        except ImportError as e:
+            raise RuntimeError("_front.so is missing or stale: build it with "
+                               "`python -m paper_2512_13368_b200.build`") from e
+        _mod = m
+    return _mod
 
 
 def _front():
@@ -128,3 +131,66 @@ def blossom_attention(q, k, v, gate_logits, block_size, top_k, window, seq_lens=
         check_arguments(q, k, v, gate_logits, seq_lens, gate_mode=int(bool(input_dependent_gate)))
         raise ValueError("blossom_attention: unusable arguments")
     return res if return_indices else res[0]
+
+
+# ---- the rows around the attention ---------------------------------------------------------------
+def check_rows(x, p, rng, others=(), weights=(), require_cuda=True):
+    """Why the native front end would not take the arguments of ``blossom_dropout`` and ``blossom_add_norm``: raises for
+    what is wrong with them.  ``others``: (name, tensor or None) that must look like x; ``weights``: (name, tensor or
+    None) of x's last size."""
+    if not isinstance(x, torch.Tensor) or (require_cuda and not x.is_cuda) or x.dim() < 1 or x.shape[-1] < 1:
+        raise ValueError("x must be a CUDA tensor with at least one column")
+    if x.dtype not in _DT:
+        raise TypeError("x must be float32 or bfloat16")
+    for name, t in others:
+        if t is None:
+            continue
+        if not isinstance(t, torch.Tensor) or t.shape != x.shape or t.device != x.device:
+            raise ValueError(f"{name} must be a tensor of x's shape on x's device")
+        if t.dtype != x.dtype:
+            raise TypeError(f"{name} must have x's dtype")
+    kinds = set()
+    for name, t in weights:
+        if t is None:
+            continue
+        if not isinstance(t, torch.Tensor) or tuple(t.shape) != (x.shape[-1],) or t.device != x.device:
+            raise ValueError(f"{name} must be a tensor of shape [{x.shape[-1]}] on x's device")
+        kinds.add(t.dtype)
+    if len(kinds) > 1 or any(k not in _DT for k in kinds):
+        raise TypeError(" and ".join(n for n, _ in weights) + " must share one dtype, float32 or bfloat16")
+    if p:
+        if not (isinstance(rng, torch.Tensor) and rng.dtype == torch.int64 and tuple(rng.shape) == (2,)
+                and rng.device == x.device):
+            raise ValueError("rng must be an int64 tensor (seed, step) of shape [2] on x's device")
+
+
+def blossom_dropout(x, p, rng, site=0):
+    """Dropout of x [..., C] (float32 or bfloat16, CUDA) with probability p in [0, 1] (in steps of 1 / 65536: the kept
+    elements are scaled by the inverse of the probability in use), from a counter-based generator: which elements are
+    kept is a function of ``rng``, ``site`` and the element's place, evaluated again in the backward and never stored.
+
+    rng: int64 CUDA tensor (seed, step).  The caller moves the step on between training steps (``rng[1] += 1``: after the
+    backward, which reads it again; autograd notices a change in between); it is read on the device, so a captured
+    graph draws anew on every replay.  site: 0 .. 65535, another one for every dropout of a step."""
+    p = float(p)
+    if p == 0.0:
+        check_rows(x, p, rng)
+        return x
+    res = _module().dropout(x, p, rng, site)
+    if res is None:
+        check_rows(x, p, rng)
+        raise ValueError("blossom_dropout: unusable arguments")
+    return res
+
+
+def blossom_add_norm(x, residual, weight, bias, p=0.0, rng=None, site=0, eps=1e-5):
+    """LayerNorm(residual + dropout(x)) over the last dimension of x [..., C], C up to 8192 (float32 or bfloat16, CUDA): the
+    end of a post-norm sub-layer (Eq. 20-22) in one pass.
+
+    residual: like x, or None.  weight, bias: [C] float32 or bfloat16, either may be None.  p, rng, site: as for
+    ``blossom_dropout`` (p = 0: no dropout, rng may be None).  Differentiable in x, residual, weight and bias."""
+    res = _module().add_norm(x, residual, weight, bias, p, rng, site, eps)
+    if res is None:
+        check_rows(x, p, rng, (("residual", residual),), (("weight", weight), ("bias", bias)))
+        raise ValueError("blossom_add_norm: unusable arguments")
+    return res

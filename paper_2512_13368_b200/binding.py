@@ -30,6 +30,7 @@ EXPORTS = (
     "blossom_profile_start", "blossom_profile_every", "blossom_profile_stop", "blossom_kernel_name",
     "blossom_debug_switch",
     "blossom_selftest_wait_timeout", "blossom_copy_rows", "blossom_launch_plan",
+    "blossom_dropout", "blossom_add_norm_fwd", "blossom_add_norm_bwd", "blossom_add_norm_workspace_bytes",
 )
 
 
@@ -46,6 +47,16 @@ class blossom_params(ctypes.Structure):
         ("phi_logits", ctypes.c_void_p), ("gate_mode", ctypes.c_int32),
         ("rope_theta", ctypes.c_float),
         ("reuse_tile_lists", ctypes.c_int32),
+    ]
+
+
+class blossom_rows_params(ctypes.Structure):
+    _fields_ = [
+        ("rows", ctypes.c_int64), ("cols", ctypes.c_int32), ("dtype", ctypes.c_int32),
+        ("weight_dtype", ctypes.c_int32), ("site", ctypes.c_int32),
+        ("dropout", ctypes.c_double), ("eps", ctypes.c_double),
+        ("x_stride", ctypes.c_int64), ("residual_stride", ctypes.c_int64), ("out_stride", ctypes.c_int64),
+        ("dx_stride", ctypes.c_int64), ("dresidual_stride", ctypes.c_int64),
     ]
 
 
@@ -100,6 +111,15 @@ def load():
     lib.blossom_launch_plan.argtypes = [pp, ctypes.c_int, ctypes.c_int]
     lib.blossom_debug_switch.restype = ctypes.c_int
     lib.blossom_debug_switch.argtypes = [ctypes.c_int, ctypes.c_int]
+    rp = ctypes.POINTER(blossom_rows_params)
+    lib.blossom_dropout.restype = ctypes.c_int
+    lib.blossom_dropout.argtypes = [rp] + [vp] * 4
+    lib.blossom_add_norm_fwd.restype = ctypes.c_int
+    lib.blossom_add_norm_fwd.argtypes = [rp] + [vp] * 8
+    lib.blossom_add_norm_bwd.restype = ctypes.c_int
+    lib.blossom_add_norm_bwd.argtypes = [rp] + [vp] * 11 + [sz, vp]
+    lib.blossom_add_norm_workspace_bytes.restype = sz
+    lib.blossom_add_norm_workspace_bytes.argtypes = [rp]
     _lib = lib
     return lib
 
@@ -207,6 +227,49 @@ def blossom_attn_bwd(params, q, k, v, gate_logits, seq_lens, block_idx, out_lt, 
                                  _stream(stream))
     if rc and check:
         raise BlossomError(rc, "blossom_attn_bwd")
+    return rc
+
+
+def _dtype(dtype):
+    return {"fp32": DTYPE_FP32, "bf16": DTYPE_BF16}.get(dtype, dtype)
+
+
+def make_rows_params(rows, cols, dtype, dropout=0.0, site=0, eps=1e-5, weight_dtype=None, x_stride=0, residual_stride=0,
+                     out_stride=0, dx_stride=0, dresidual_stride=0) -> blossom_rows_params:
+    """Fill a ``blossom_rows_params``; strides in elements from row to row, 0 = ``cols``; the weights' type is ``dtype``
+    unless given."""
+    return blossom_rows_params(int(rows), int(cols), _dtype(dtype), _dtype(dtype if weight_dtype is None else weight_dtype),
+                               int(site), float(dropout), float(eps), int(x_stride), int(residual_stride),
+                               int(out_stride), int(dx_stride), int(dresidual_stride))
+
+
+def blossom_dropout(params, x, rng, out, stream=None, check=True) -> int:
+    rc = load().blossom_dropout(ctypes.byref(params), _ptr(x), _ptr(rng), _ptr(out), _stream(stream))
+    if rc and check:
+        raise BlossomError(rc, "blossom_dropout")
+    return rc
+
+
+def blossom_add_norm_workspace_bytes(params) -> int:
+    return int(load().blossom_add_norm_workspace_bytes(ctypes.byref(params)))
+
+
+def blossom_add_norm_fwd(params, x, residual, weight, bias, rng, out, stats, stream=None, check=True) -> int:
+    rc = load().blossom_add_norm_fwd(ctypes.byref(params), _ptr(x), _ptr(residual), _ptr(weight), _ptr(bias), _ptr(rng),
+                                     _ptr(out), _ptr(stats), _stream(stream))
+    if rc and check:
+        raise BlossomError(rc, "blossom_add_norm_fwd")
+    return rc
+
+
+def blossom_add_norm_bwd(params, x, residual, weight, rng, stats, dout, dx, dresidual, dweight, dbias, workspace,
+                         workspace_bytes=None, stream=None, check=True) -> int:
+    rc = load().blossom_add_norm_bwd(ctypes.byref(params), _ptr(x), _ptr(residual), _ptr(weight), _ptr(rng), _ptr(stats),
+                                     _ptr(dout), _ptr(dx), _ptr(dresidual), _ptr(dweight), _ptr(dbias), _ptr(workspace),
+                                     _nbytes(workspace) if workspace_bytes is None else workspace_bytes,
+                                     _stream(stream))
+    if rc and check:
+        raise BlossomError(rc, "blossom_add_norm_bwd")
     return rc
 
 

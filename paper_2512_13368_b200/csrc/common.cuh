@@ -78,10 +78,11 @@ extern std::atomic<unsigned long long> g_launches;  // host-side launch counter
 enum KernelId {
   K_SUMMARY = 0, K_SCORE_SELECT, K_FWD_SIMT, K_BWD_DQ_SIMT, K_BWD_DKDV_SIMT, K_GATE_GRAD,
   K_FWD_TC, K_BWD_DQ_TC, K_BWD_DKDV_TC, K_SCORE_FAST, K_BWD_PREP, K_TC_META, K_ROPE, K_BWD_SHORT,
-  K_COPY_ROWS,
+  K_COPY_ROWS, K_DROPOUT, K_NORM_FWD, K_NORM_BWD, K_NORM_WEIGHTS,
   K_COUNT
 };
 void prof_mark(int id, int phase, cudaStream_t st);  // no-op unless a profile is running
+void prof_break();  // what follows on a stream is not charged from the last call's end
 
 // Wrap every kernel launch: counts it and, when a profile is running, brackets it with events.
 struct LaunchScope {

@@ -15,11 +15,13 @@
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/function.h>
+#include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/csrc/autograd/functions/utils.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/autograd/saved_variable.h>
 #include <torch/csrc/autograd/variable.h>
 
+#include <algorithm>
 #include <stdexcept>
 #include <string>
 
@@ -320,6 +322,268 @@ PyObject *attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
   }
 }
 
+// ---- rows around the attention: dropout, residual + layer norm ------------------------------------
+// A tensor as rows of its last dimension with one stride between them.
+struct RowView {
+  int64_t rows = 0, cols = 0, stride = 0;
+};
+bool row_view(const Tensor &t, RowView *v) {
+  const int64_t d = t.dim();
+  v->cols = t.size(d - 1);
+  v->rows = 1;
+  v->stride = v->cols;
+  if (t.stride(d - 1) != 1 && v->cols > 1) return false;
+  for (int64_t i = d - 2; i >= 0; --i) {
+    if (t.size(i) == 1) continue;
+    if (v->rows == 1) v->stride = t.stride(i);
+    else if (t.stride(i) != v->stride * v->rows) return false;
+    v->rows *= t.size(i);
+  }
+  return v->stride >= v->cols;
+}
+// t, or a copy of it that is plain rows
+Tensor as_rows(const Tensor &t, RowView *v) {
+  if (!t.defined()) return t;
+  Tensor r = t;
+  if (!row_view(r, v)) {
+    r = r.contiguous();
+    row_view(r, v);
+  }
+  make_plain(r);
+  return r;
+}
+const void *address(const Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; }
+blossom_stream_t stream_of(const Tensor &t) {
+  return (blossom_stream_t)c10::cuda::getCurrentCUDAStream(t.device().index()).stream();
+}
+
+// The gradients are not differentiable again: asked for a graph of them, whoever uses it is told so.
+void once_differentiable(variable_list &res, const char *what) {
+  if (!at::GradMode::is_enabled()) return;
+  for (Tensor &t : res)
+    if (t.defined()) {
+      t = t.detach();
+      auto node = std::shared_ptr<Node>(
+          new torch::autograd::Error(std::string(what) + " has no second derivative"), torch::autograd::deleteNode);
+      torch::autograd::set_history(t, node);
+    }
+}
+
+struct BlossomDropoutBackward : public Node {
+  SavedVariable rng_;
+  blossom_rows_params params_;
+
+  std::string name() const override { return "BlossomDropoutBackward"; }
+  void release_variables() override { rng_.reset_data(); }
+  variable_list apply(variable_list &&grads) override {
+    variable_list res(1);
+    if (!grads[0].defined()) return res;
+    {
+      at::NoGradGuard no_grad;
+      const Tensor rng = rng_.unpack();
+      c10::cuda::CUDAGuard guard(rng.device());
+      RowView v;
+      const Tensor dout = as_rows(grads[0], &v);
+      const Tensor dx = fresh(dout.sizes(), dout.scalar_type(), dout.device());
+      blossom_rows_params p = params_;
+      p.x_stride = v.stride;
+      p.out_stride = 0;
+      const int rc = blossom_dropout(&p, dout.data_ptr(), rng.data_ptr<int64_t>(), dx.data_ptr(), stream_of(dout));
+      if (rc) throw std::runtime_error(failure("blossom_dropout", rc));
+      res[0] = dx;
+    }
+    once_differentiable(res, "blossom_dropout");
+    return res;
+  }
+};
+
+struct BlossomAddNormBackward : public Node {
+  SavedVariable x_, res_, weight_, rng_, stats_;
+  blossom_rows_params params_;
+  bool has_bias_;
+
+  std::string name() const override { return "BlossomAddNormBackward"; }
+  void release_variables() override {
+    for (SavedVariable *v : {&x_, &res_, &weight_, &rng_, &stats_}) v->reset_data();
+  }
+  variable_list apply(variable_list &&grads) override {
+    variable_list out(4);  // x, residual, weight, bias
+    if (!grads[0].defined()) return out;
+    {
+      at::NoGradGuard no_grad;
+      const Tensor x = x_.unpack(), res = res_.unpack(), weight = weight_.unpack(), rng = rng_.unpack(),
+                   stats = stats_.unpack();
+      c10::cuda::CUDAGuard guard(x.device());
+      RowView v;
+      Tensor dout = as_rows(grads[0], &v);
+      blossom_rows_params p = params_;
+      p.out_stride = v.stride;
+      const auto type = x.scalar_type(), wtype = p.weight_dtype == BLOSSOM_DTYPE_FP32 ? at::kFloat : at::kBFloat16;
+      const at::Device dev = x.device();
+      const bool want_x = task_should_compute_output(0), want_res = res.defined() && task_should_compute_output(1);
+      // without dropout the two gradients are one
+      if (want_x || (want_res && p.dropout == 0.0)) out[0] = fresh(x.sizes(), type, dev);
+      if (want_res && p.dropout > 0.0) out[1] = fresh(x.sizes(), type, dev);
+      if (weight.defined() && task_should_compute_output(2)) out[2] = fresh({p.cols}, wtype, dev);
+      if (has_bias_ && task_should_compute_output(3)) out[3] = fresh({p.cols}, wtype, dev);
+      const size_t bytes = blossom_add_norm_workspace_bytes(&p);
+      const Tensor ws = fresh({(int64_t)bytes}, at::kByte, dev);
+      auto at = [](const Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; };
+      const int rc = blossom_add_norm_bwd(&p, x.data_ptr(), at(res), at(weight), static_cast<const int64_t *>(at(rng)),
+                                          stats.data_ptr<float>(), dout.data_ptr(), at(out[0]), at(out[1]), at(out[2]),
+                                          at(out[3]), ws.data_ptr(), bytes, stream_of(x));
+      if (rc) throw std::runtime_error(failure("blossom_add_norm_bwd", rc));
+      if (want_res && p.dropout == 0.0) {
+        out[1] = out[0];
+        if (!want_x) out[0] = Tensor();
+      }
+    }
+    once_differentiable(out, "blossom_add_norm");
+    return out;
+  }
+};
+
+bool row_type(const Tensor &t) { return t.scalar_type() == at::kFloat || t.scalar_type() == at::kBFloat16; }
+int32_t type_code(const Tensor &t) { return t.scalar_type() == at::kFloat ? BLOSSOM_DTYPE_FP32 : BLOSSOM_DTYPE_BF16; }
+// an argument that may be None
+bool optional(PyObject *o, Tensor *t) {
+  if (o == Py_None) return true;
+  if (!THPVariable_Check(o)) return false;
+  *t = THPVariable_Unpack(o);
+  return true;
+}
+bool rng_ok(const Tensor &rng, const Tensor &x) {
+  return rng.defined() && rng.scalar_type() == at::kLong && rng.dim() == 1 && rng.size(0) == 2 && rng.device() == x.device();
+}
+PyObject *no_tangents(const char *what) {
+  return PyErr_Format(PyExc_NotImplementedError, "%s has no forward-mode derivative", what);
+}
+bool has_tangent(const Tensor &t) { return t.defined() && t._fw_grad(/*level=*/0).defined(); }
+
+// dropout(x, p, rng, site) -> out; None: not what the library can be handed (autograd.check_rows says why)
+PyObject *dropout(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  if (n != 4) return PyErr_Format(PyExc_TypeError, "dropout() takes 4 arguments");
+  blossom_rows_params p = {};
+  p.dropout = PyFloat_AsDouble(a[1]);
+  if ((p.dropout == -1.0 && PyErr_Occurred()) || !read_int(a[3], &p.site)) return nullptr;
+  try {
+    Tensor rng;
+    if (!THPVariable_Check(a[0]) || !optional(a[2], &rng)) Py_RETURN_NONE;
+    const Tensor &x0 = THPVariable_Unpack(a[0]);
+    if (!x0.is_cuda() || !row_type(x0) || x0.dim() < 1 || x0.size(x0.dim() - 1) < 1 || !rng_ok(rng, x0)) Py_RETURN_NONE;
+    if (has_tangent(x0)) return no_tangents("blossom_dropout");
+    c10::cuda::CUDAGuard guard(x0.device());
+    Tensor x, state;
+    RowView v;
+    {
+      at::NoGradGuard no_grad;
+      x = as_rows(x0, &v);
+      state = rng.contiguous();
+    }
+    p.rows = v.rows;
+    p.cols = (int32_t)std::min<int64_t>(v.cols, INT32_MAX);
+    p.dtype = p.weight_dtype = type_code(x);
+    p.x_stride = v.stride;
+    Tensor out = fresh(x.sizes(), x.scalar_type(), x.device());
+    const void *xp = address(x);
+    const int64_t *rp = state.data_ptr<int64_t>();
+    void *op = out.data_ptr();
+    const blossom_stream_t st = stream_of(x);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS;
+    rc = blossom_dropout(&p, xp, rp, op, st);
+    Py_END_ALLOW_THREADS;
+    if (rc) return raise_blossom(rc, "blossom_dropout");
+    if (torch::autograd::compute_requires_grad(x0)) {
+      auto node = std::shared_ptr<BlossomDropoutBackward>(new BlossomDropoutBackward(), torch::autograd::deleteNode);
+      node->set_next_edges(torch::autograd::collect_next_edges(x0));
+      node->rng_ = SavedVariable(state, false);
+      node->params_ = p;
+      torch::autograd::set_history(out, node);
+    }
+    return THPVariable_Wrap(std::move(out));
+  } catch (const std::exception &e) {
+    if (!PyErr_Occurred()) PyErr_SetString(PyExc_RuntimeError, e.what());
+    return nullptr;
+  }
+}
+
+// add_norm(x, residual, weight, bias, p, rng, site, eps) -> out; None: as above
+PyObject *add_norm(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  if (n != 8) return PyErr_Format(PyExc_TypeError, "add_norm() takes 8 arguments");
+  blossom_rows_params p = {};
+  p.dropout = PyFloat_AsDouble(a[4]);
+  if ((p.dropout == -1.0 && PyErr_Occurred()) || !read_int(a[6], &p.site)) return nullptr;
+  p.eps = PyFloat_AsDouble(a[7]);
+  if (p.eps == -1.0 && PyErr_Occurred()) return nullptr;
+  try {
+    Tensor res0, weight0, bias0, rng;
+    if (!THPVariable_Check(a[0]) || !optional(a[1], &res0) || !optional(a[2], &weight0) || !optional(a[3], &bias0) ||
+        !optional(a[5], &rng))
+      Py_RETURN_NONE;
+    const Tensor &x0 = THPVariable_Unpack(a[0]);
+    if (!x0.is_cuda() || !row_type(x0) || x0.dim() < 1 || x0.size(x0.dim() - 1) < 1) Py_RETURN_NONE;
+    if (res0.defined() && (res0.sizes() != x0.sizes() || res0.scalar_type() != x0.scalar_type() || res0.device() != x0.device()))
+      Py_RETURN_NONE;
+    for (const Tensor *t : {&weight0, &bias0})
+      if (t->defined() && (t->dim() != 1 || t->size(0) != x0.size(x0.dim() - 1) || !row_type(*t) || t->device() != x0.device()))
+        Py_RETURN_NONE;
+    if (weight0.defined() && bias0.defined() && weight0.scalar_type() != bias0.scalar_type()) Py_RETURN_NONE;
+    if (p.dropout != 0.0 && !rng_ok(rng, x0)) Py_RETURN_NONE;
+    for (const Tensor *t : {&x0, (const Tensor *)&res0, (const Tensor *)&weight0, (const Tensor *)&bias0})
+      if (has_tangent(*t)) return no_tangents("blossom_add_norm");
+    c10::cuda::CUDAGuard guard(x0.device());
+    Tensor x, res, weight = weight0, bias = bias0, state;
+    RowView v, rv;
+    {
+      at::NoGradGuard no_grad;
+      x = as_rows(x0, &v);
+      res = as_rows(res0, &rv);
+      for (Tensor *t : {&weight, &bias})
+        if (t->defined()) {
+          *t = t->contiguous();
+          make_plain(*t);
+        }
+      if (p.dropout != 0.0) state = rng.contiguous();
+    }
+    p.rows = v.rows;
+    p.cols = (int32_t)std::min<int64_t>(v.cols, INT32_MAX);
+    p.dtype = type_code(x);
+    p.weight_dtype = weight.defined() ? type_code(weight) : bias.defined() ? type_code(bias) : p.dtype;
+    p.x_stride = v.stride;
+    p.residual_stride = rv.stride;
+    const bool grad = torch::autograd::compute_requires_grad(x0, res0, weight0, bias0);
+    Tensor out = fresh(x.sizes(), x.scalar_type(), x.device()), stats;
+    if (grad) stats = fresh({v.rows, 2}, at::kFloat, x.device());
+    const void *xp = address(x), *ep = address(res), *wp = address(weight), *bp = address(bias);
+    const int64_t *rp = state.defined() ? state.data_ptr<int64_t>() : nullptr;
+    void *op = out.data_ptr();
+    float *sp = grad ? stats.data_ptr<float>() : nullptr;
+    const blossom_stream_t st = stream_of(x);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS;
+    rc = blossom_add_norm_fwd(&p, xp, ep, wp, bp, rp, op, sp, st);
+    Py_END_ALLOW_THREADS;
+    if (rc) return raise_blossom(rc, "blossom_add_norm_fwd");
+    if (grad) {
+      auto node = std::shared_ptr<BlossomAddNormBackward>(new BlossomAddNormBackward(), torch::autograd::deleteNode);
+      node->set_next_edges(torch::autograd::collect_next_edges(x0, res0, weight0, bias0));
+      node->x_ = SavedVariable(x, false);
+      node->res_ = SavedVariable(res, false);
+      node->weight_ = SavedVariable(weight, false);
+      node->rng_ = SavedVariable(state, false);
+      node->stats_ = SavedVariable(stats, false);
+      node->params_ = p;
+      node->has_bias_ = bias.defined();
+      torch::autograd::set_history(out, node);
+    }
+    return THPVariable_Wrap(std::move(out));
+  } catch (const std::exception &e) {
+    if (!PyErr_Occurred()) PyErr_SetString(PyExc_RuntimeError, e.what());
+    return nullptr;
+  }
+}
+
 // dense(tensor) -> bool, like(tensor) -> tensor: the two rules above, for the host-side tests
 PyObject *py_dense(PyObject *, PyObject *t) {
   if (!THPVariable_Check(t)) return PyErr_Format(PyExc_TypeError, "dense() takes a tensor");
@@ -339,6 +603,8 @@ PyMethodDef methods[] = {
     {"dense", py_dense, METH_O, nullptr},
     {"like", py_like, METH_O, nullptr},
     {"attention", (PyCFunction)(void (*)(void))attention, METH_FASTCALL, nullptr},
+    {"dropout", (PyCFunction)(void (*)(void))dropout, METH_FASTCALL, nullptr},
+    {"add_norm", (PyCFunction)(void (*)(void))add_norm, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_front", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
