@@ -299,6 +299,60 @@ int blossom_add_norm_bwd(const blossom_rows_params *params /* host */, const voi
                          blossom_stream_t stream);
 size_t blossom_add_norm_workspace_bytes(const blossom_rows_params *params /* host */);
 
+/*
+ * Sampled softmax loss over an item table (paper: Eq. 26-28, "prediction", with a sampled catalogue), forward and
+ * backward: row t scores its target and n negative items, l_j = <hidden_t, table[c_j]>, and
+ * loss = mean over the rows that take part of log(sum_j exp l_j) - l_target.
+ *
+ * A row takes part if its target is an item (0 <= id < items) other than ignore_index; others (padding) have no loss and
+ * zero gradients, and are not read.  No row takes part: the loss and every gradient are 0.  Negatives outside
+ * [0, items) are no candidates, nor with mask_hits are negatives equal to the row's target; repeated negatives
+ * count each time.  The candidates' rows are read from the table where they are needed; nothing of the size
+ * [rows, n + 1, cols] is ever stored.  Logits, the sums and the gradients are formed in single precision (the loss
+ * itself in double precision) and rounded once; the order of every sum is fixed: the same call gives the same bits.
+ */
+typedef struct {
+  int64_t rows;             /* >= 0; rows * (negatives + 1) < 2^31                                        */
+  int32_t cols;             /* 1 .. 1024                                                                 */
+  int32_t items;            /* 1 <= items < 2^30                                                         */
+  int32_t negatives;        /* n >= 0 per row                                                            */
+  int32_t dtype;            /* of hidden, table, dhidden, dtable                                         */
+  int32_t index_bytes;      /* 4 or 8: targets and negatives are int32 or int64                          */
+  int32_t mask_hits;        /* 1: a negative equal to the row's target is no candidate                   */
+  int64_t ignore_index;     /* a target that takes no part, e.g. -100 or the padding item                */
+  int64_t hidden_stride, table_stride, dhidden_stride, dtable_stride; /* elements per row, 0 = cols          */
+  int64_t negatives_stride; /* elements per row, 0 = the same n negatives for every row                    */
+} blossom_loss_params;
+
+/* One size serves both calls, of which the forward uses the first BLOSSOM_LOSS_FORWARD_BYTES and asks for no more; 0 for
+ * invalid or unsupported params.  256-byte aligned; nothing is kept from call to call. */
+#define BLOSSOM_LOSS_FORWARD_BYTES 65536
+size_t blossom_sampled_loss_workspace_bytes(const blossom_loss_params *params /* host */);
+
+/*   targets      in   [rows]
+ *   negatives    in   [rows][n] or [n]; NULL if n = 0
+ *   loss         out  float [1]
+ *   lse          out  float [rows + 1]: log(sum_j exp l_j) of every row that takes part (0 for the others), and at the
+ *                     end the number of rows that do
+ *   grad_hidden  out  float [rows][cols] or NULL if the backward will not be asked for dhidden: the gradient of each
+ *                     row's own loss, sum_j p_j table[c_j] - table[c_target], formed while the candidates' rows
+ *                     are at hand; 16-byte aligned */
+int blossom_sampled_loss_fwd(const blossom_loss_params *params /* host */, const void *hidden, const void *table,
+                             const void *targets, const void *negatives, float *loss, float *lse, float *grad_hidden,
+                             void *workspace, size_t workspace_bytes, blossom_stream_t stream);
+
+/*   lse, grad_hidden  in   as the forward left them (grad_hidden only for dhidden)
+ *   grad_loss         in   float [1], device: the loss's upstream gradient g; NULL = 1
+ *   dhidden           out  or NULL (not wanted): g / count * grad_hidden
+ *   dtable            out  [items][cols] or NULL (not wanted): g / count * sum over the candidates (t, j) that are this item
+ *                          of (p_tj - [j is the target]) * hidden_t; every row is written, zeros for items that are
+ *                          nobody's candidate
+ *   workspace              needed for dtable only */
+int blossom_sampled_loss_bwd(const blossom_loss_params *params /* host */, const void *hidden, const void *table,
+                             const void *targets, const void *negatives, const float *lse, const float *grad_hidden,
+                             const float *grad_loss, void *dhidden, void *dtable, void *workspace,
+                             size_t workspace_bytes, blossom_stream_t stream);
+
 /* Synchronises the stream and copies the workspace's device status to *host_out (host): 0 = no
  * device-side error, else a blossom_status.  The workspace holds one status word for the forward
  * (blossom_select_blocks and blossom_attn_fwd clear both words when they start: a new step) and

@@ -194,3 +194,40 @@ def blossom_add_norm(x, residual, weight, bias, p=0.0, rng=None, site=0, eps=1e-
         check_rows(x, p, rng, (("residual", residual),), (("weight", weight), ("bias", bias)))
         raise ValueError("blossom_add_norm: unusable arguments")
     return res
+
+
+# ---- the loss ------------------------------------------------------------------------------------
+def check_loss(hidden, table, targets, negatives, require_cuda=True):
+    """Why the native front end would not take the arguments of ``blossom_sampled_loss``: raises for what is wrong."""
+    if not isinstance(hidden, torch.Tensor) or (require_cuda and not hidden.is_cuda) or hidden.dim() < 1 or hidden.shape[-1] < 1:
+        raise ValueError("hidden must be a CUDA tensor [..., C]")
+    if hidden.dtype not in _DT:
+        raise TypeError("hidden must be float32 or bfloat16")
+    if not isinstance(table, torch.Tensor) or table.dim() != 2 or table.shape[1] != hidden.shape[-1] or table.shape[0] < 1:
+        raise ValueError(f"table must be [items, {hidden.shape[-1]}]")
+    if table.dtype != hidden.dtype:
+        raise TypeError("table must have hidden's dtype")
+    if not isinstance(targets, torch.Tensor) or targets.shape != hidden.shape[:-1]:
+        raise ValueError(f"targets must be a tensor of shape {list(hidden.shape[:-1])}")
+    if not isinstance(negatives, torch.Tensor) or negatives.dim() < 1 or (
+            negatives.dim() > 1 and negatives.shape[:-1] != hidden.shape[:-1]):
+        raise ValueError(f"negatives must be a tensor of shape [n] or {list(hidden.shape[:-1])} + [n]")
+    if targets.dtype not in (torch.int32, torch.int64) or negatives.dtype != targets.dtype:
+        raise TypeError("targets and negatives must both be int64 or both int32")
+    if any(t.device != hidden.device for t in (table, targets, negatives)):
+        raise ValueError("hidden, table, targets and negatives must live on one device")
+
+
+def blossom_sampled_loss(hidden, table, targets, negatives, ignore_index=-100, mask_hits=False):
+    """Sampled softmax cross-entropy over an item table: the mean, over the positions that take part, of
+    ``logsumexp(logits) - logits[target]`` with the logits ``<hidden, table[c]>`` of the target and the negatives.
+
+    hidden [..., C] and table [items, C]: float32 or bfloat16 (CUDA), C up to 1024; targets [...]: int32 or int64, a position
+    whose target is ``ignore_index`` or no item takes no part; negatives [..., n], or [n] for all positions alike: ids
+    that are no items are no candidates, and with ``mask_hits`` those equal to the position's target are none.
+    Returns a float32 scalar (0 if no position takes part), differentiable in hidden and table."""
+    res = _module().sampled_loss(hidden, table, targets, negatives, ignore_index, mask_hits)
+    if res is None:
+        check_loss(hidden, table, targets, negatives)
+        raise ValueError("blossom_sampled_loss: unusable arguments")
+    return res

@@ -31,7 +31,9 @@ EXPORTS = (
     "blossom_debug_switch",
     "blossom_selftest_wait_timeout", "blossom_copy_rows", "blossom_launch_plan",
     "blossom_dropout", "blossom_add_norm_fwd", "blossom_add_norm_bwd", "blossom_add_norm_workspace_bytes",
+    "blossom_sampled_loss_fwd", "blossom_sampled_loss_bwd", "blossom_sampled_loss_workspace_bytes",
 )
+LOSS_FORWARD_BYTES = 65536  # what blossom_sampled_loss_fwd uses of its workspace
 
 
 class blossom_params(ctypes.Structure):
@@ -57,6 +59,16 @@ class blossom_rows_params(ctypes.Structure):
         ("dropout", ctypes.c_double), ("eps", ctypes.c_double),
         ("x_stride", ctypes.c_int64), ("residual_stride", ctypes.c_int64), ("out_stride", ctypes.c_int64),
         ("dx_stride", ctypes.c_int64), ("dresidual_stride", ctypes.c_int64),
+    ]
+
+
+class blossom_loss_params(ctypes.Structure):
+    _fields_ = [
+        ("rows", ctypes.c_int64), ("cols", ctypes.c_int32), ("items", ctypes.c_int32),
+        ("negatives", ctypes.c_int32), ("dtype", ctypes.c_int32), ("index_bytes", ctypes.c_int32),
+        ("mask_hits", ctypes.c_int32), ("ignore_index", ctypes.c_int64),
+        ("hidden_stride", ctypes.c_int64), ("table_stride", ctypes.c_int64), ("dhidden_stride", ctypes.c_int64),
+        ("dtable_stride", ctypes.c_int64), ("negatives_stride", ctypes.c_int64),
     ]
 
 
@@ -120,6 +132,13 @@ def load():
     lib.blossom_add_norm_bwd.argtypes = [rp] + [vp] * 11 + [sz, vp]
     lib.blossom_add_norm_workspace_bytes.restype = sz
     lib.blossom_add_norm_workspace_bytes.argtypes = [rp]
+    lp = ctypes.POINTER(blossom_loss_params)
+    lib.blossom_sampled_loss_workspace_bytes.restype = sz
+    lib.blossom_sampled_loss_workspace_bytes.argtypes = [lp]
+    lib.blossom_sampled_loss_fwd.restype = ctypes.c_int
+    lib.blossom_sampled_loss_fwd.argtypes = [lp] + [vp] * 8 + [sz, vp]
+    lib.blossom_sampled_loss_bwd.restype = ctypes.c_int
+    lib.blossom_sampled_loss_bwd.argtypes = [lp] + [vp] * 10 + [sz, vp]
     _lib = lib
     return lib
 
@@ -270,6 +289,43 @@ def blossom_add_norm_bwd(params, x, residual, weight, rng, stats, dout, dx, dres
                                      _stream(stream))
     if rc and check:
         raise BlossomError(rc, "blossom_add_norm_bwd")
+    return rc
+
+
+def make_loss_params(rows, cols, items, negatives, dtype, index_bytes=8, mask_hits=0, ignore_index=-100, hidden_stride=0,
+                     table_stride=0, dhidden_stride=0, dtable_stride=0, negatives_stride=None) -> blossom_loss_params:
+    """Fill a ``blossom_loss_params``; strides in elements, 0 = ``cols``; ``negatives_stride``: None = a row of
+    ``negatives`` ids per position, 0 = the same ids for all."""
+    return blossom_loss_params(int(rows), int(cols), int(items), int(negatives), _dtype(dtype), int(index_bytes),
+                               int(mask_hits), int(ignore_index), int(hidden_stride), int(table_stride),
+                               int(dhidden_stride), int(dtable_stride),
+                               int(negatives if negatives_stride is None else negatives_stride))
+
+
+def blossom_sampled_loss_workspace_bytes(params) -> int:
+    return int(load().blossom_sampled_loss_workspace_bytes(ctypes.byref(params)))
+
+
+def blossom_sampled_loss_fwd(params, hidden, table, targets, negatives, loss, lse, grad_hidden, workspace,
+                             workspace_bytes=None, stream=None, check=True) -> int:
+    rc = load().blossom_sampled_loss_fwd(ctypes.byref(params), _ptr(hidden), _ptr(table), _ptr(targets), _ptr(negatives),
+                                         _ptr(loss), _ptr(lse), _ptr(grad_hidden), _ptr(workspace),
+                                         _nbytes(workspace) if workspace_bytes is None else workspace_bytes,
+                                         _stream(stream))
+    if rc and check:
+        raise BlossomError(rc, "blossom_sampled_loss_fwd")
+    return rc
+
+
+def blossom_sampled_loss_bwd(params, hidden, table, targets, negatives, lse, grad_hidden, grad_loss, dhidden, dtable,
+                             workspace, workspace_bytes=None, stream=None, check=True) -> int:
+    rc = load().blossom_sampled_loss_bwd(ctypes.byref(params), _ptr(hidden), _ptr(table), _ptr(targets), _ptr(negatives),
+                                         _ptr(lse), _ptr(grad_hidden), _ptr(grad_loss), _ptr(dhidden), _ptr(dtable),
+                                         _ptr(workspace),
+                                         _nbytes(workspace) if workspace_bytes is None else workspace_bytes,
+                                         _stream(stream))
+    if rc and check:
+        raise BlossomError(rc, "blossom_sampled_loss_bwd")
     return rc
 
 

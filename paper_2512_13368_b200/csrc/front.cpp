@@ -584,6 +584,137 @@ PyObject *add_norm(PyObject *, PyObject *const *a, Py_ssize_t n) {
   }
 }
 
+// ---- sampled softmax loss ------------------------------------------------------------------------
+struct BlossomSampledLossBackward : public Node {
+  SavedVariable hidden_, table_, targets_, negatives_, lse_, grad_;
+  blossom_loss_params params_;
+
+  std::string name() const override { return "BlossomSampledLossBackward"; }
+  void release_variables() override {
+    for (SavedVariable *v : {&hidden_, &table_, &targets_, &negatives_, &lse_, &grad_}) v->reset_data();
+  }
+  variable_list apply(variable_list &&grads) override {
+    variable_list out(2);  // hidden, table
+    if (!grads[0].defined()) return out;
+    {
+      at::NoGradGuard no_grad;
+      const Tensor hidden = hidden_.unpack(), table = table_.unpack(), targets = targets_.unpack(),
+                   negatives = negatives_.unpack(), lse = lse_.unpack(), grad = grad_.unpack();
+      c10::cuda::CUDAGuard guard(hidden.device());
+      Tensor g = grads[0];
+      make_plain(g);
+      const at::Device dev = hidden.device();
+      if (grad.defined() && task_should_compute_output(0)) out[0] = fresh(hidden.sizes(), hidden.scalar_type(), dev);
+      Tensor ws;
+      if (task_should_compute_output(1)) {
+        out[1] = fresh(table.sizes(), table.scalar_type(), dev);
+        ws = fresh({(int64_t)blossom_sampled_loss_workspace_bytes(&params_)}, at::kByte, dev);
+      }
+      auto at = [](const Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; };
+      if (out[0].defined() || out[1].defined()) {
+        const int rc = blossom_sampled_loss_bwd(
+            &params_, hidden.data_ptr(), table.data_ptr(), targets.data_ptr(), at(negatives), lse.data_ptr<float>(),
+            static_cast<const float *>(at(grad)), g.data_ptr<float>(), at(out[0]), at(out[1]), at(ws),
+            ws.defined() ? (size_t)ws.nbytes() : 0, stream_of(hidden));
+        if (rc) throw std::runtime_error(failure("blossom_sampled_loss_bwd", rc));
+      }
+    }
+    once_differentiable(out, "blossom_sampled_loss");
+    return out;
+  }
+};
+
+// sampled_loss(hidden, table, targets, negatives, ignore_index, mask_hits) -> loss; None: not what the library can be
+// handed (autograd.check_loss says why)
+PyObject *sampled_loss(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  if (n != 6) return PyErr_Format(PyExc_TypeError, "sampled_loss() takes 6 arguments");
+  blossom_loss_params p = {};
+  p.ignore_index = PyLong_AsLongLong(a[4]);
+  if ((p.ignore_index == -1 && PyErr_Occurred()) || !read_int(a[5], &p.mask_hits)) return nullptr;
+  try {
+    for (int i = 0; i < 4; ++i)
+      if (!THPVariable_Check(a[i])) Py_RETURN_NONE;
+    const Tensor &hidden0 = THPVariable_Unpack(a[0]), &table0 = THPVariable_Unpack(a[1]),
+                 &targets0 = THPVariable_Unpack(a[2]), &negatives0 = THPVariable_Unpack(a[3]);
+    const int64_t d = hidden0.dim();
+    if (!hidden0.is_cuda() || !row_type(hidden0) || d < 1 || hidden0.size(d - 1) < 1 || table0.dim() != 2 ||
+        table0.size(1) != hidden0.size(d - 1) || table0.size(0) < 1 || table0.scalar_type() != hidden0.scalar_type())
+      Py_RETURN_NONE;
+    for (const Tensor *t : {&table0, &targets0, &negatives0})
+      if (t->device() != hidden0.device()) Py_RETURN_NONE;
+    const at::ScalarType ids = targets0.scalar_type();
+    if ((ids != at::kLong && ids != at::kInt) || negatives0.scalar_type() != ids) Py_RETURN_NONE;
+    const at::IntArrayRef lead = hidden0.sizes().slice(0, d - 1);
+    if (targets0.sizes() != lead || negatives0.dim() < 1) Py_RETURN_NONE;
+    const bool shared = negatives0.dim() == 1;
+    if (!shared && (negatives0.dim() != d || negatives0.sizes().slice(0, d - 1) != lead)) Py_RETURN_NONE;
+    for (const Tensor *t : {&hidden0, &table0})
+      if (has_tangent(*t)) return no_tangents("blossom_sampled_loss");
+    c10::cuda::CUDAGuard guard(hidden0.device());
+    Tensor hidden, table, targets, negatives = negatives0;
+    RowView hv, tv, nv;
+    {
+      at::NoGradGuard no_grad;
+      hidden = as_rows(hidden0, &hv);
+      table = as_rows(table0, &tv);
+      targets = targets0.contiguous();
+      bool one = true;  // the same ids for every position: a vector, or one that is expanded
+      for (int64_t i = 0; i + 1 < negatives.dim(); ++i) one = one && (negatives.stride(i) == 0 || negatives.size(i) == 1);
+      if (one && negatives.numel()) {
+        while (negatives.dim() > 1) negatives = negatives.select(0, 0);
+        negatives = negatives.contiguous();
+        nv.stride = 0;
+      } else {
+        negatives = as_rows(negatives, &nv);
+      }
+      for (Tensor *t : {&targets, &negatives}) make_plain(*t);
+    }
+    const int64_t n_neg = negatives0.size(negatives0.dim() - 1);
+    if (n_neg >= INT32_MAX || table.size(0) > INT32_MAX || hv.cols > INT32_MAX)
+      return raise_blossom(BLOSSOM_ERR_UNSUPPORTED, "blossom_sampled_loss_fwd");
+    p.rows = hv.rows;
+    p.cols = (int32_t)hv.cols;
+    p.items = (int32_t)table.size(0);
+    p.negatives = (int32_t)n_neg;
+    p.dtype = type_code(hidden);
+    p.index_bytes = ids == at::kLong ? 8 : 4;
+    p.hidden_stride = hv.stride;
+    p.table_stride = tv.stride;
+    p.negatives_stride = n_neg ? nv.stride : 0;
+    const at::Device dev = hidden.device();
+    const bool grad = torch::autograd::compute_requires_grad(hidden0, table0);
+    const bool grad_hidden = grad && hidden0.requires_grad();
+    Tensor loss = fresh({}, at::kFloat, dev), lse = fresh({hv.rows + 1}, at::kFloat, dev), gh;
+    if (grad_hidden) gh = fresh({hv.rows, hv.cols}, at::kFloat, dev);
+    const Tensor ws = fresh({BLOSSOM_LOSS_FORWARD_BYTES}, at::kByte, dev);
+    const void *hp = address(hidden), *tp = address(table), *gp = address(targets), *np = n_neg ? address(negatives) : nullptr;
+    float *lp = loss.data_ptr<float>(), *sp = lse.data_ptr<float>(), *dp = gh.defined() ? gh.data_ptr<float>() : nullptr;
+    void *wp = ws.data_ptr();
+    const blossom_stream_t st = stream_of(hidden);
+    int rc;
+    Py_BEGIN_ALLOW_THREADS;
+    rc = blossom_sampled_loss_fwd(&p, hp, tp, gp, np, lp, sp, dp, wp, BLOSSOM_LOSS_FORWARD_BYTES, st);
+    Py_END_ALLOW_THREADS;
+    if (rc) return raise_blossom(rc, "blossom_sampled_loss_fwd");
+    if (grad) {
+      auto node = std::shared_ptr<BlossomSampledLossBackward>(new BlossomSampledLossBackward(), torch::autograd::deleteNode);
+      node->set_next_edges(torch::autograd::collect_next_edges(hidden0, table0));
+      node->hidden_ = SavedVariable(hidden, false);
+      node->table_ = SavedVariable(table, false);
+      node->targets_ = SavedVariable(targets, false);
+      node->negatives_ = SavedVariable(n_neg ? negatives : Tensor(), false);
+      node->lse_ = SavedVariable(lse, false);
+      node->grad_ = SavedVariable(gh, false);
+      node->params_ = p;
+      torch::autograd::set_history(loss, node);
+    }
+    return THPVariable_Wrap(std::move(loss));
+  } catch (const std::exception &e) {
+    if (!PyErr_Occurred()) PyErr_SetString(PyExc_RuntimeError, e.what());
+    return nullptr;
+  }
+}
+
 // dense(tensor) -> bool, like(tensor) -> tensor: the two rules above, for the host-side tests
 PyObject *py_dense(PyObject *, PyObject *t) {
   if (!THPVariable_Check(t)) return PyErr_Format(PyExc_TypeError, "dense() takes a tensor");
@@ -605,6 +736,7 @@ PyMethodDef methods[] = {
     {"attention", (PyCFunction)(void (*)(void))attention, METH_FASTCALL, nullptr},
     {"dropout", (PyCFunction)(void (*)(void))dropout, METH_FASTCALL, nullptr},
     {"add_norm", (PyCFunction)(void (*)(void))add_norm, METH_FASTCALL, nullptr},
+    {"sampled_loss", (PyCFunction)(void (*)(void))sampled_loss, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_front", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -1,0 +1,303 @@
+// Sampled softmax loss, the part over positions: logits of a position's candidates, their log-sum-exp, the loss, and with
+// it the gradient of the position's hidden row, sum_j p_j table[c_j] - table[c_target]; nothing is stored per candidate.
+//
+// A warp takes a position.  Groups of LPC lanes hold one candidate's row each, several candidates in flight; a group keeps a
+// running maximum, sum and weighted sum of rows, and the groups are joined at the end.  Every candidate's row is read
+// once.  Bound: the candidates' rows come from L2 at best (128 bytes each for 64 columns of bf16), 2.1 GB for 131072
+// positions of 128 candidates, against 0.17 GB that HBM has to move.
+#include "loss.cuh"
+
+namespace blossom {
+namespace loss {
+namespace {
+
+constexpr int kThreads = 256;
+
+template <typename T, int W, typename P, bool GRAD>
+__global__ void __launch_bounds__(kThreads) loss_rows_kernel(Args a, const T *__restrict__ hidden, const T *__restrict__ table,
+                                                             float *__restrict__ lse, float *__restrict__ dh,
+                                                             double2 *__restrict__ sums) {
+  constexpr int LPC = P::LPC, V = P::V, CPW = 32 / LPC, U = V == 1 ? 4 : 1;
+  __shared__ double2 warp_sums[kThreads / 32];
+  grid_chain_enter();
+  const int lane = (int)threadIdx.x % 32, warp = (int)threadIdx.x / 32, col = lane % LPC, sub = lane / LPC;
+  double2 mine = make_double2(0.0, 0.0);
+  for (int64_t r = (int64_t)blockIdx.x * (kThreads / 32) + warp; r < a.rows; r += (int64_t)gridDim.x * (kThreads / 32)) {
+    const int row = (int)r, target = row_target(a, row);
+    float acc[V][8];
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) acc[v][i] = 0.f;
+    float row_lse = 0.f;
+    if (target >= 0) {
+      float h[V][8];
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const int g = col + v * LPC;
+        load_group<T, W>(hidden + row * a.sh + 8 * g, a.cols - 8 * g, h[v]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[v][i] *= kLog2e;  // logits in units of log 2
+      }
+      float top = -INFINITY, total = 0.f, own = 0.f;
+      for (int c0 = 0; c0 <= a.n; c0 += 32) {
+        const int id = c0 + lane <= a.n ? candidate(a, row, target, c0 + lane) : -1;
+        const int steps = (min(32, a.n + 1 - c0) + CPW - 1) / CPW;
+        for (int k = 0; k < steps; k += U) {
+          float w[U][V][8], l[U];
+          int at[U];
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            at[u] = __shfl_sync(0xffffffffu, id, (k + u) * CPW + sub);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+              const int g = col + v * LPC;
+              load_group<T, W>(table + at[u] * a.st + 8 * g, at[u] >= 0 ? a.cols - 8 * g : 0, w[u][v]);
+            }
+          }
+          float high = top;
+          bool any = false;
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            any |= at[u] >= 0;
+            l[u] = 0.f;
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+              for (int i = 0; i < 8; ++i) l[u] += h[v][i] * w[u][v][i];
+#pragma unroll
+            for (int o = 1; o < LPC; o <<= 1) l[u] += __shfl_xor_sync(0xffffffffu, l[u], o);
+            if (at[u] < 0) l[u] = -INFINITY;
+            high = fmaxf(high, l[u]);
+          }
+          if (c0 == 0 && k == 0) own = __shfl_sync(0xffffffffu, l[0], 0);
+          if (any) {  // (logits that are no numbers go in as well and make the row's sum one)
+            const float shrink = exp2f(top - high);
+            total *= shrink;
+            if (GRAD) {
+#pragma unroll
+              for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) acc[v][i] *= shrink;
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+              const float p = exp2f(l[u] - high);
+              total += p;
+              if (GRAD) {
+#pragma unroll
+                for (int v = 0; v < V; ++v)
+#pragma unroll
+                  for (int i = 0; i < 8; ++i) acc[v][i] += p * w[u][v][i];
+              }
+            }
+            top = high;
+          }
+        }
+      }
+      // the groups of lanes, joined (one that has met no candidate has top = -inf and weighs nothing)
+      float high = top;
+#pragma unroll
+      for (int o = LPC; o < 32; o <<= 1) high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, o));
+      const float weight = exp2f(top - high);
+      total *= weight;
+#pragma unroll
+      for (int o = LPC; o < 32; o <<= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+      const float lse2 = high + log2f(total);
+      row_lse = lse2 * kLn2;
+      mine.x += (double)((lse2 - own) * kLn2);
+      mine.y += 1.0;
+      if (GRAD) {
+        const float inv = weight / total;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          const int g = col + v * LPC;
+          float w[8];
+          load_group<T, W>(table + target * a.st + 8 * g, a.cols - 8 * g, w);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            acc[v][i] *= inv;
+#pragma unroll
+            for (int o = LPC; o < 32; o <<= 1) acc[v][i] += __shfl_xor_sync(0xffffffffu, acc[v][i], o);
+            acc[v][i] -= w[i];
+          }
+        }
+      }
+    }
+    if (lane == 0) lse[row] = row_lse;
+    if (GRAD && sub == 0) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const int g = col + v * LPC;
+        store_group<float, (W < 4 ? W : 4)>(dh + (int64_t)row * a.cols + 8 * g, a.cols - 8 * g, acc[v]);
+      }
+    }
+  }
+  if (lane == 0) warp_sums[warp] = mine;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < kThreads / 32; ++i) mine.x += warp_sums[i].x, mine.y += warp_sums[i].y;
+    sums[blockIdx.x] = mine;
+  }
+}
+
+// The mean, from the CTAs' sums in a fixed order.
+__global__ void __launch_bounds__(kThreads) loss_mean_kernel(int ctas, const double2 *__restrict__ sums, float *__restrict__ loss,
+                                                             float *__restrict__ count) {
+  __shared__ double2 warp_sums[kThreads / 32];
+  grid_chain_enter();
+  double2 s = make_double2(0.0, 0.0);
+  for (int i = (int)threadIdx.x; i < ctas; i += kThreads) s.x += sums[i].x, s.y += sums[i].y;
+#pragma unroll
+  for (int o = 16; o; o >>= 1) {
+    s.x += __shfl_xor_sync(0xffffffffu, s.x, o);
+    s.y += __shfl_xor_sync(0xffffffffu, s.y, o);
+  }
+  if (threadIdx.x % 32 == 0) warp_sums[threadIdx.x / 32] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < kThreads / 32; ++i) s.x += warp_sums[i].x, s.y += warp_sums[i].y;
+    *loss = s.y > 0.0 ? (float)(s.x / s.y) : 0.f;
+    *count = (float)s.y;
+  }
+}
+
+// dhidden = g / count * grad_hidden, rounded once
+template <typename T, int W>
+__global__ void __launch_bounds__(kThreads) loss_scale_kernel(Args a, const float *__restrict__ dh, const float *__restrict__ lse,
+                                                              const float *__restrict__ grad_loss, T *__restrict__ out) {
+  grid_chain_enter();
+  const float scale = grad_scale(a, lse, grad_loss);
+  const int64_t total = (int64_t)a.rows * a.groups, step = (int64_t)gridDim.x * kThreads;
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += step) {
+    const int row = (int)(i / a.groups), g = (int)(i - (int64_t)row * a.groups), valid = a.cols - 8 * g;
+    float v[8];
+    load_group<float, (W < 4 ? W : 4)>(dh + (int64_t)row * a.cols + 8 * g, valid, v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] *= scale;
+    store_group<T, W>(out + row * a.sdh + 8 * g, valid, v);
+  }
+}
+
+int check(const blossom_loss_params *p, Args *a) {
+  if (!p || p->rows < 0 || p->cols < 1 || p->items < 1 || p->negatives < 0) return BLOSSOM_ERR_INVALID_ARG;
+  if (p->dtype != BLOSSOM_DTYPE_FP32 && p->dtype != BLOSSOM_DTYPE_BF16) return BLOSSOM_ERR_INVALID_ARG;
+  if ((p->index_bytes != 4 && p->index_bytes != 8) || p->mask_hits < 0 || p->mask_hits > 1) return BLOSSOM_ERR_INVALID_ARG;
+  int64_t st[4] = {p->hidden_stride, p->table_stride, p->dhidden_stride, p->dtable_stride};
+  for (int64_t &s : st) {
+    if (s == 0) s = p->cols;
+    if (s < p->cols) return BLOSSOM_ERR_INVALID_ARG;
+  }
+  if (p->negatives_stride < 0) return BLOSSOM_ERR_INVALID_ARG;
+  const int64_t most = 0x7fffffffLL;
+  if (p->cols > kMaxCols || p->items >= 1 << 30 || p->rows > most || p->negatives == most ||
+      (p->rows > 0 && p->rows > most / ((int64_t)p->negatives + 1)))
+    return BLOSSOM_ERR_UNSUPPORTED;
+  a->rows = (int)p->rows, a->cols = p->cols, a->groups = (p->cols + 7) / 8, a->items = p->items, a->n = p->negatives;
+  a->ignore = p->ignore_index, a->sh = st[0], a->st = st[1], a->sn = p->negatives_stride, a->sdh = st[2], a->sdt = st[3];
+  a->idx8 = p->index_bytes == 8, a->hits = p->mask_hits;
+  a->targets = a->negatives = nullptr;
+  return BLOSSOM_OK;
+}
+// the inputs of either call
+int check_inputs(Args *a, int dtype, int index_bytes, const void *hidden, const void *table, const void *targets,
+                 const void *negatives) {
+  if (!table || (a->rows && (!hidden || !targets || (a->n && !negatives)))) return BLOSSOM_ERR_INVALID_ARG;
+  const size_t esz = dtype == BLOSSOM_DTYPE_FP32 ? 4 : 2;
+  if ((reinterpret_cast<uintptr_t>(hidden) | reinterpret_cast<uintptr_t>(table)) % esz) return BLOSSOM_ERR_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(targets) | reinterpret_cast<uintptr_t>(negatives)) % (size_t)index_bytes)
+    return BLOSSOM_ERR_INVALID_ARG;
+  a->targets = targets;
+  a->negatives = negatives;
+  return BLOSSOM_OK;
+}
+
+}  // namespace
+}  // namespace loss
+}  // namespace blossom
+
+extern "C" size_t blossom_sampled_loss_workspace_bytes(const blossom_loss_params *params) {
+  using namespace blossom;
+  loss::Args a;
+  return loss::check(params, &a) ? 0 : loss::carve(a, nullptr).bytes;
+}
+
+extern "C" int blossom_sampled_loss_fwd(const blossom_loss_params *params, const void *hidden, const void *table,
+                                        const void *targets, const void *negatives, float *loss_out, float *lse,
+                                        float *grad_hidden, void *workspace, size_t workspace_bytes, blossom_stream_t stream) {
+  using namespace blossom;
+  prof_break();
+  loss::Args a;
+  if (int rc = loss::check(params, &a)) return rc;
+  if (int rc = loss::check_inputs(&a, params->dtype, params->index_bytes, hidden, table, targets, negatives)) return rc;
+  if (!loss_out || !lse || (reinterpret_cast<uintptr_t>(loss_out) | reinterpret_cast<uintptr_t>(lse)) % 4 ||
+      reinterpret_cast<uintptr_t>(grad_hidden) % 16)
+    return BLOSSOM_ERR_INVALID_ARG;
+  if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256 || workspace_bytes < loss::kForwardBytes)
+    return BLOSSOM_ERR_WORKSPACE;
+  const cudaStream_t st = (cudaStream_t)stream;
+  const size_t esz = params->dtype == BLOSSOM_DTYPE_FP32 ? 4 : 2;
+  double2 *sums = static_cast<double2 *>(workspace);
+  const int64_t want = ((int64_t)a.rows + 7) / 8;
+  const int ctas = (int)(want < loss::kMaxRowCtas ? want : loss::kMaxRowCtas);
+  if (ctas) {
+    rows::Alignment al;
+    al.rows_at(hidden, a.sh, esz);
+    al.rows_at(table, a.st, esz);
+    loss::with_plan(a.groups, [&](auto plan) {
+      using P = decltype(plan);
+      rows::with_type(params->dtype, al.elements(a.cols, esz), [&](auto t, auto w) {
+        using T = decltype(t);
+        constexpr int W = decltype(w)::value;
+        LaunchScope ls(K_LOSS_ROWS, st);
+        launch_chained(grad_hidden ? loss::loss_rows_kernel<T, W, P, true> : loss::loss_rows_kernel<T, W, P, false>,
+                       dim3((unsigned)ctas), dim3(loss::kThreads), 0, st, a, static_cast<const T *>(hidden),
+                       static_cast<const T *>(table), lse, grad_hidden, sums);
+      });
+    });
+  }
+  LaunchScope ls(K_LOSS_MEAN, st);
+  launch_chained(loss::loss_mean_kernel, dim3(1), dim3(loss::kThreads), 0, st, ctas, (const double2 *)sums, loss_out,
+                 lse + a.rows);
+  return cudaGetLastError() == cudaSuccess ? BLOSSOM_OK : BLOSSOM_ERR_CUDA;
+}
+
+extern "C" int blossom_sampled_loss_bwd(const blossom_loss_params *params, const void *hidden, const void *table,
+                                        const void *targets, const void *negatives, const float *lse,
+                                        const float *grad_hidden, const float *grad_loss, void *dhidden, void *dtable,
+                                        void *workspace, size_t workspace_bytes, blossom_stream_t stream) {
+  using namespace blossom;
+  prof_break();
+  loss::Args a;
+  if (int rc = loss::check(params, &a)) return rc;
+  if (int rc = loss::check_inputs(&a, params->dtype, params->index_bytes, hidden, table, targets, negatives)) return rc;
+  const size_t esz = params->dtype == BLOSSOM_DTYPE_FP32 ? 4 : 2;
+  if (!lse || (reinterpret_cast<uintptr_t>(lse) | reinterpret_cast<uintptr_t>(grad_loss)) % 4 || !(dhidden || dtable) ||
+      (reinterpret_cast<uintptr_t>(dhidden) | reinterpret_cast<uintptr_t>(dtable)) % esz ||
+      (dhidden && a.rows && !grad_hidden) || reinterpret_cast<uintptr_t>(grad_hidden) % 16)
+    return BLOSSOM_ERR_INVALID_ARG;
+  const loss::Scratch s = loss::carve(a, workspace);
+  if (dtable && (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256 || workspace_bytes < s.bytes))
+    return BLOSSOM_ERR_WORKSPACE;
+  const cudaStream_t st = (cudaStream_t)stream;
+  if (dhidden && a.rows) {
+    rows::Alignment al;
+    al.rows_at(dhidden, a.sdh, esz);
+    const int64_t ctas = ((int64_t)a.rows * a.groups + loss::kThreads - 1) / loss::kThreads, most = loss::kSMs * 8;
+    rows::with_type(params->dtype, al.elements(a.cols, esz), [&](auto t, auto w) {
+      using T = decltype(t);
+      LaunchScope ls(K_LOSS_SCALE, st);
+      launch_chained(loss::loss_scale_kernel<T, decltype(w)::value>, dim3((unsigned)(ctas < most ? ctas : most)),
+                     dim3(loss::kThreads), 0, st, a, grad_hidden, lse, grad_loss, static_cast<T *>(dhidden));
+    });
+  }
+  if (dtable) {
+    rows::Alignment al;
+    al.rows_at(hidden, a.sh, esz);
+    al.rows_at(table, a.st, esz);
+    al.rows_at(dtable, a.sdt, esz);
+    if (int rc = loss::launch_items(a, params->dtype, hidden, table, lse, grad_loss, dtable, al.elements(a.cols, esz), s, st))
+      return rc;
+  }
+  return cudaGetLastError() == cudaSuccess ? BLOSSOM_OK : BLOSSOM_ERR_CUDA;
+}
