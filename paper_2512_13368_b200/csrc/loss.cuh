@@ -50,11 +50,86 @@ inline void with_plan(int groups, F &&f) {
 }
 inline int lanes_of(int groups) { return groups <= 4 ? 4 : groups <= 8 ? 8 : groups <= 16 ? 16 : 32; }
 
+// ---- bf16 rows of up to 32 NC columns on the matrix units ---------------------------------------------
+// A warp scores 16 rows against one vector.  Lane 4 g + q loads 16 bytes at columns 32 c + 8 q of the rows g and g + 8: as the
+// order in which a product's columns are added up is free, those are the first operand of two m16n8k16 products a
+// chunk c as they come, without a detour through shared memory; the vector, laid out alike, is the second operand in all
+// 8 of its columns, so that every lane of a quad ends up with the products of its own two rows.
+template <int NC>
+struct Rows16 {
+  uint4 w[2][NC];
+};
+__device__ __forceinline__ uint4 load16(const __nv_bfloat16 *p, bool there) {
+  return there ? *reinterpret_cast<const uint4 *>(p) : make_uint4(0, 0, 0, 0);
+}
+__device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                         uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// <row g, v> and <row g + 8, v>
+template <int NC>
+__device__ __forceinline__ float2 dots16(const Rows16<NC> &r, const uint4 (&v)[NC]) {
+  float d[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    mma16816(d, r.w[0][c].x, r.w[1][c].x, r.w[0][c].y, r.w[1][c].y, v[c].x, v[c].y);
+    mma16816(d, r.w[0][c].z, r.w[1][c].z, r.w[0][c].w, r.w[1][c].w, v[c].z, v[c].w);
+  }
+  return make_float2(d[0], d[2]);
+}
+// acc += p.x * row g + p.y * row g + 8, in single precision (the weights keep their 24 bits)
+template <int NC>
+__device__ __forceinline__ void weigh16(const Rows16<NC> &r, float2 p, float2 (&acc)[NC][4]) {
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const float2 pp = k ? make_float2(p.y, p.y) : make_float2(p.x, p.x);
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      const uint32_t x[4] = {r.w[k][c].x, r.w[k][c].y, r.w[k][c].z, r.w[k][c].w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        acc[c][i] = fma2(pp, make_float2(__uint_as_float(x[i] << 16), __uint_as_float(x[i] & 0xffff0000u)), acc[c][i]);
+    }
+  }
+}
+// The sum over the 8 quads, scattered: lane 4 g + q is left with column 32 c + 8 q + g of every chunk c.
+template <int NC>
+__device__ __forceinline__ void scatter16(const float2 (&acc)[NC][4], float (&out)[NC]) {
+  const int g = ((int)threadIdx.x % 32) / 4;
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    float v[8], a[4], b[2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[2 * i] = acc[c][i].x, v[2 * i + 1] = acc[c][i].y;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      a[i] = (g & 4 ? v[i + 4] : v[i]) + __shfl_xor_sync(0xffffffffu, g & 4 ? v[i] : v[i + 4], 16);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      b[i] = (g & 2 ? a[i + 2] : a[i]) + __shfl_xor_sync(0xffffffffu, g & 2 ? a[i] : a[i + 2], 8);
+    out[c] = (g & 1 ? b[1] : b[0]) + __shfl_xor_sync(0xffffffffu, g & 1 ? b[0] : b[1], 4);
+  }
+}
+// Chunks of 32 columns where the matrix units take the rows (bf16, 16-byte aligned rows of up to 128 columns), else 0.
+inline int mma_chunks(int dtype, int width, int cols) {
+  return dtype == BLOSSOM_DTYPE_BF16 && width == 8 && cols <= 128 ? (cols <= 32 ? 1 : cols <= 64 ? 2 : 4) : 0;
+}
+template <typename F>
+inline void with_chunks(int nc, F &&f) {
+  using std::integral_constant;
+  if (nc == 1) f(integral_constant<int, 1>());
+  else if (nc == 2) f(integral_constant<int, 2>());
+  else f(integral_constant<int, 4>());
+}
+
 // Device scratch; the forward uses `sums` alone.
 struct Scratch {
   double2 *sums;                 // [kMaxRowCtas] loss and number of rows of a CTA
   uint32_t *keys[2], *vals[2];   // [entries] item and position (top bit: it is the target) of every candidate, being sorted
   uint32_t *hist, *totals;       // [digits][tiles], [digits]
+  uint32_t *range;               // [2][items] where an item's entries start and end in the sorted list (0, 0: it has none)
   float *part;                   // [chunks][2][cols] sums of items that reach over the end of a chunk
   size_t bytes;
 };
@@ -65,12 +140,12 @@ static_assert(kMaxRowCtas * sizeof(double2) <= kForwardBytes, "a sum per CTA");
 struct SortPlan {
   int passes, bits;
   int64_t entries, tiles;
-  int chunk;  // sorted entries that a group of lanes adds up
+  int chunk;  // sorted entries that a warp or a group of lanes adds up
   int64_t chunks;
 };
 constexpr int kSortThreads = 512, kSortPerThread = 16, kTile = kSortThreads * kSortPerThread, kMaxDigits = 512;
 
-SortPlan sort_plan(const Args &a);
+SortPlan sort_plan(const Args &a, int lanes);  // lanes: of a group that walks a chunk
 Scratch carve(const Args &a, void *base);
 // dtable from the candidates, sorted by item
 int launch_items(const Args &a, int dtype, const void *hidden, const void *table, const float *lse, const float *grad_loss,

@@ -15,36 +15,57 @@ namespace {
 // ---- the sort ------------------------------------------------------------------------------------
 // Entry e of the unsorted list is candidate e % (n + 1) of position e / (n + 1); what is no candidate gets the item
 // number `items` and ends up behind all others.
-__device__ __forceinline__ void make_entry(const Args &a, uint32_t e, uint32_t *key, uint32_t *val) {
-  const uint32_t t = e / (uint32_t)(a.n + 1), j = e - t * (uint32_t)(a.n + 1);
+struct Split {  // e / (n + 1) for e < 2^31: a product and a shift
+  uint32_t mul, shift;
+  __device__ __forceinline__ uint32_t operator()(uint32_t e) const { return (uint32_t)((uint64_t)e * mul >> shift); }
+};
+inline Split split_by(uint32_t d) {
+  int l = 0;
+  while (((uint64_t)1 << l) < d) ++l;
+  return Split{(uint32_t)((((uint64_t)1 << (31 + l)) + d - 1) / d), (uint32_t)(31 + l)};
+}
+__device__ __forceinline__ uint32_t entry_key(const Args &a, const Split &by, uint32_t e) {
+  const uint32_t t = by(e), j = e - t * (uint32_t)(a.n + 1);
   const int target = row_target(a, (int)t);
   const int c = target >= 0 ? candidate(a, (int)t, target, (int)j) : -1;
-  *key = c >= 0 ? (uint32_t)c : (uint32_t)a.items;
-  *val = t | (j == 0 ? 0x80000000u : 0u);
+  return c >= 0 ? (uint32_t)c : (uint32_t)a.items;
+}
+__device__ __forceinline__ uint32_t entry_val(const Args &a, const Split &by, uint32_t e) {
+  const uint32_t t = by(e);
+  return t | (e == t * (uint32_t)(a.n + 1) ? 0x80000000u : 0u);
 }
 
-// Counts of a tile's digits, to hist[digit][tile].
+// Counts of a tile's digits, to hist[digit][tile].  The first pass makes the keys.
 template <bool FIRST>
-__global__ void __launch_bounds__(kSortThreads) sort_count_kernel(Args a, const uint32_t *__restrict__ keys, uint32_t entries,
-                                                                  int shift, int bits, uint32_t *__restrict__ hist) {
+__global__ void __launch_bounds__(kSortThreads) sort_count_kernel(Args a, Split by, uint32_t *__restrict__ keys, uint32_t entries,
+                                                                  int shift, int bits, uint32_t *__restrict__ hist,
+                                                                  uint32_t *__restrict__ range) {
   __shared__ uint32_t count[kMaxDigits];
   grid_chain_enter();
   const int digits = 1 << bits;
+  const uint32_t mask = (uint32_t)digits - 1, none = (uint32_t)a.items;
   if ((int)threadIdx.x < digits) count[threadIdx.x] = 0;
+  if (FIRST)
+    for (int64_t i = (int64_t)blockIdx.x * kSortThreads + threadIdx.x; i < 2 * (int64_t)a.items; i += (int64_t)gridDim.x * kSortThreads)
+      range[i] = 0;
   __syncthreads();
-  const uint32_t lane = threadIdx.x % 32, e0 = blockIdx.x * (uint32_t)kTile + threadIdx.x / 32 * (32 * kSortPerThread) + lane;
-#pragma unroll 4
+  const uint32_t e0 = blockIdx.x * (uint32_t)kTile + threadIdx.x;
+  uint32_t key[kSortPerThread];
+#pragma unroll
   for (int r = 0; r < kSortPerThread; ++r) {
-    const uint32_t e = e0 + 32 * r;
-    uint32_t key = 0, val, d = 0xffffffffu;
-    if (e < entries) {
-      if (FIRST) make_entry(a, e, &key, &val);
-      else key = keys[e];
-      d = key >> shift & (uint32_t)(digits - 1);
-    }
-    // (one addition for the lanes that share a digit: a batch of padding is one digit throughout)
-    const uint32_t peers = __match_any_sync(0xffffffffu, d);
-    if (e < entries && (peers & ((1u << lane) - 1)) == 0) atomicAdd(&count[d], (uint32_t)__popc(peers));
+    const uint32_t e = e0 + kSortThreads * r;
+    key[r] = 0;
+    if (e < entries) key[r] = FIRST ? entry_key(a, by, e) : keys[e];
+  }
+#pragma unroll
+  for (int r = 0; r < kSortPerThread; ++r) {
+    const uint32_t e = e0 + kSortThreads * r;
+    const bool there = e < entries, padding = there && key[r] == none;
+    if (FIRST && there) keys[e] = key[r];
+    // (padding comes in long runs of one key: one addition a warp; items are mostly different ones)
+    const uint32_t pads = __ballot_sync(0xffffffffu, padding);
+    if (padding && threadIdx.x % 32 == __ffs(pads) - 1) atomicAdd(&count[none >> shift & mask], (uint32_t)__popc(pads));
+    if (there && !padding) atomicAdd(&count[key[r] >> shift & mask], 1u);
   }
   __syncthreads();
   if ((int)threadIdx.x < digits) hist[(size_t)threadIdx.x * gridDim.x + blockIdx.x] = count[threadIdx.x];
@@ -88,14 +109,27 @@ __global__ void __launch_bounds__(kSortThreads) sort_scan_kernel(uint32_t *__res
   if (threadIdx.x == 0) totals[blockIdx.x] = carry;
 }
 
+// Lanes that hold the same digit as this one, among those that hold any: one ballot a bit.
+__device__ __forceinline__ uint32_t same_digit(uint32_t d, int bits, bool there) {
+  uint32_t peers = __ballot_sync(0xffffffffu, there);
+  for (int b = 0; b < bits; ++b) {
+    const bool bit = d >> b & 1;
+    const uint32_t v = __ballot_sync(0xffffffffu, bit);
+    peers &= bit ? v : ~v;
+  }
+  return peers;
+}
+
 // A tile's entries to their places, in order: ranks within a warp by matching digits, then warps, then digits; the tile is put
-// in order in shared memory first, so that it leaves in runs.  hist null: there is one tile, whose own counts are all.
+// in order in shared memory first, so that it leaves in runs.  FIRST: the values are made here, and where there is
+// one tile (hist null, its own counts are all) the keys too.
 template <bool FIRST>
-__global__ void __launch_bounds__(kSortThreads) sort_move_kernel(Args a, const uint32_t *__restrict__ keys,
-                                                                 const uint32_t *__restrict__ vals, uint32_t entries, int shift,
-                                                                 int bits, const uint32_t *__restrict__ hist,
-                                                                 const uint32_t *__restrict__ totals,
-                                                                 uint32_t *__restrict__ keys_out, uint32_t *__restrict__ vals_out) {
+__global__ void __launch_bounds__(kSortThreads, 2) sort_move_kernel(Args a, Split by, const uint32_t *__restrict__ keys,
+                                                                    const uint32_t *__restrict__ vals, uint32_t entries,
+                                                                    int shift, int bits, const uint32_t *__restrict__ hist,
+                                                                    const uint32_t *__restrict__ totals,
+                                                                    uint32_t *__restrict__ keys_out,
+                                                                    uint32_t *__restrict__ vals_out, uint32_t *__restrict__ range) {
   constexpr int NW = kSortThreads / 32;
   extern __shared__ uint32_t sm[];
   uint32_t *sk = sm, *sv = sm + kTile, *offset = sm + 2 * kTile, *count = offset + kMaxDigits;  // count[warp][digit]
@@ -104,25 +138,26 @@ __global__ void __launch_bounds__(kSortThreads) sort_move_kernel(Args a, const u
   const int digits = 1 << bits, tid = (int)threadIdx.x, lane = tid % 32, warp = tid / 32;
   const uint32_t mask = (uint32_t)digits - 1;
   for (int i = tid; i < NW * digits; i += kSortThreads) count[i] = 0;
+  if (FIRST && !hist)
+    for (int64_t i = (int64_t)blockIdx.x * kSortThreads + tid; i < 2 * (int64_t)a.items; i += (int64_t)gridDim.x * kSortThreads)
+      range[i] = 0;
   __syncthreads();
   const uint32_t tile0 = blockIdx.x * (uint32_t)kTile, e0 = tile0 + (uint32_t)warp * (32 * kSortPerThread) + (uint32_t)lane;
-  uint32_t key[kSortPerThread], val[kSortPerThread], rank[kSortPerThread];
+  uint32_t key[kSortPerThread], rank[kSortPerThread / 2];  // (two ranks a word)
 #pragma unroll
   for (int r = 0; r < kSortPerThread; ++r) {
     const uint32_t e = e0 + 32 * r;
-    key[r] = val[r] = 0;
-    if (e < entries) {
-      if (FIRST) make_entry(a, e, &key[r], &val[r]);
-      else key[r] = keys[e], val[r] = vals[e];
-    }
+    key[r] = 0;
+    if (e < entries) key[r] = FIRST && !hist ? entry_key(a, by, e) : keys[e];
   }
   uint32_t *mine = count + warp * digits;
 #pragma unroll
   for (int r = 0; r < kSortPerThread; ++r) {
     const bool there = e0 + 32 * r < entries;
-    const uint32_t d = there ? key[r] >> shift & mask : 0xffffffffu;
-    const uint32_t peers = __match_any_sync(0xffffffffu, d), below = peers & ((1u << lane) - 1);
-    rank[r] = there ? mine[d] + (uint32_t)__popc(below) : 0;
+    const uint32_t d = key[r] >> shift & mask;
+    const uint32_t peers = same_digit(d, bits, there), below = peers & ((1u << lane) - 1);
+    const uint32_t at = there ? mine[d] + (uint32_t)__popc(below) : 0;
+    rank[r / 2] = r % 2 ? rank[r / 2] | at << 16 : at;
     __syncwarp();
     if (there && below == 0) mine[d] += (uint32_t)__popc(peers);
     __syncwarp();
@@ -150,9 +185,9 @@ __global__ void __launch_bounds__(kSortThreads) sort_move_kernel(Args a, const u
 #pragma unroll
   for (int r = 0; r < kSortPerThread; ++r)
     if (e0 + 32 * r < entries) {
-      const uint32_t at = mine[key[r] >> shift & mask] + rank[r];
+      const uint32_t at = mine[key[r] >> shift & mask] + (r % 2 ? rank[r / 2] >> 16 : rank[r / 2] & 0xffffu);
       sk[at] = key[r];
-      sv[at] = val[r];
+      sv[at] = FIRST ? entry_val(a, by, e0 + 32 * r) : vals[e0 + 32 * r];
     }
   __syncthreads();
   const uint32_t here = entries - tile0 < (uint32_t)kTile ? entries - tile0 : (uint32_t)kTile;
@@ -172,7 +207,7 @@ __global__ void __launch_bounds__(kThreads) loss_items_kernel(Args a, const T *_
                                                               const float *__restrict__ lse, const float *__restrict__ grad_loss,
                                                               const uint32_t *__restrict__ keys, const uint32_t *__restrict__ vals,
                                                               uint32_t entries, int chunk, T *__restrict__ dtable,
-                                                              float *__restrict__ part) {
+                                                              float *__restrict__ part, uint32_t *__restrict__ range) {
   constexpr int LPC = P::LPC, V = P::V, U = V == 1 ? 4 : 1;
   grid_chain_enter();
   const int col = (int)threadIdx.x % LPC;
@@ -208,7 +243,10 @@ __global__ void __launch_bounds__(kThreads) loss_items_kernel(Args a, const T *_
       }
     }
   };
+  const bool writer = col == 0;
+  if (writer && s > 0 && !open && keys[s - 1] < (uint32_t)a.items) range[a.items + keys[s - 1]] = s;
   if (cur >= (uint32_t)a.items) return;
+  if (writer && !open) range[cur] = s;
   begin(cur);
   for (uint32_t i = s; i < e; i += U) {
     uint32_t key[U], val[U];
@@ -232,7 +270,9 @@ __global__ void __launch_bounds__(kThreads) loss_items_kernel(Args a, const T *_
       if (key[u] != cur) {
         finish(!open);
         open = first = false;
+        if (writer) range[a.items + cur] = i + u;
         if (key[u] >= (uint32_t)a.items) return;  // (what follows is no candidate)
+        if (writer) range[key[u]] = i + u;
         begin(key[u]);
       }
       float l = 0.f;
@@ -250,16 +290,143 @@ __global__ void __launch_bounds__(kThreads) loss_items_kernel(Args a, const T *_
     }
   }
   finish(!open && !(e < entries && keys[e] == cur));
+  if (writer && e == entries) range[a.items + cur] = e;
 }
 
-__device__ __forceinline__ uint32_t lower_bound(const uint32_t *keys, uint32_t n, uint32_t key) {
-  uint32_t lo = 0, len = n;
-  while (len) {
-    const uint32_t half = len / 2;
-    if (keys[lo + half] < key) lo += half + 1, len -= half + 1;
-    else len = half;
+// The same on the matrix units: a warp walks a chunk 16 entries at a time, their hidden rows the first operand, the item's
+// row the second.  Sixteen entries of more than one item go through once an item, the others' weights zero.
+template <int NC>
+__global__ void __launch_bounds__(kThreads) loss_items_mma_kernel(Args a, const __nv_bfloat16 *__restrict__ hidden,
+                                                                  const __nv_bfloat16 *__restrict__ table,
+                                                                  const float *__restrict__ lse,
+                                                                  const float *__restrict__ grad_loss,
+                                                                  const uint32_t *__restrict__ keys,
+                                                                  const uint32_t *__restrict__ vals, uint32_t entries, int chunk,
+                                                                  __nv_bfloat16 *__restrict__ dtable, float *__restrict__ part,
+                                                                  uint32_t *__restrict__ range) {
+  grid_chain_enter();
+  const int lane = (int)threadIdx.x % 32, g = lane / 4, q = lane % 4;
+  const int64_t c0 = (int64_t)blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
+  if (c0 * chunk >= entries) return;
+  const uint32_t none = (uint32_t)a.items, s = (uint32_t)(c0 * chunk);
+  const uint32_t e = entries - s < (uint32_t)chunk ? entries : s + (uint32_t)chunk;
+  const float scale = grad_scale(a, lse, grad_loss);
+  // 32 entries, one a lane
+  struct Entries {
+    uint32_t key, val;
+    float top;
+  };
+  auto entries_from = [&](uint32_t i) {
+    Entries x = {none, 0, 0.f};
+    if (i + lane < e) x.key = keys[i + lane], x.val = vals[i + lane];
+    if (x.key < none) x.top = lse[x.val & 0x7fffffffu] * kLog2e;
+    return x;
+  };
+  struct Batch {  // of 16 entries, those of rows g and g + 8
+    Rows16<NC> h;
+    uint32_t key[2], val[2];
+    float top[2];
+  };
+  auto load = [&](const Entries &x, int half, Batch &b) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int from = half + g + 8 * k;
+      b.key[k] = __shfl_sync(0xffffffffu, x.key, from);
+      b.val[k] = __shfl_sync(0xffffffffu, x.val, from);
+      b.top[k] = __shfl_sync(0xffffffffu, x.top, from);
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        const int col = 32 * c + 8 * q;
+        b.h.w[k][c] = load16(hidden + (int64_t)(b.val[k] & 0x7fffffffu) * a.sh + col, b.key[k] < none && col < a.cols);
+      }
+    }
+  };
+  uint4 w[NC];
+  float2 acc[NC][4];
+  uint32_t cur = keys[s], before = s > 0 ? keys[s - 1] : 0xffffffffu;
+  bool open = before == cur, first = true;  // open: the item's entries began in a chunk before
+  auto begin = [&](uint32_t item) {
+    cur = item;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      w[c] = load16(table + cur * a.st + 32 * c + 8 * q, 32 * c + 8 * q < a.cols);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[c][i] = make_float2(0.f, 0.f);
+    }
+  };
+  auto finish = [&](bool whole) {
+    float sum[NC];
+    scatter16<NC>(acc, sum);
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      const int col = 32 * c + 8 * q + g;
+      if (col >= a.cols) continue;
+      if (whole) dtable[cur * a.sdt + col] = __float2bfloat16(sum[c] * scale);
+      else part[(c0 * 2 + (first ? 0 : 1)) * a.cols + col] = sum[c];
+    }
+  };
+  // where items start and end, from 32 entries and the key before them
+  auto mark = [&](const Entries &x, uint32_t i) {
+    uint32_t left = __shfl_up_sync(0xffffffffu, x.key, 1);
+    if (lane == 0) left = before;
+    if (i + lane < e) {
+      if (x.key != left) {
+        if (x.key < none) range[x.key] = i + lane;
+        if (left < none) range[none + left] = i + lane;
+      }
+      if (i + lane + 1 == entries && x.key < none) range[none + x.key] = entries;
+    }
+    before = __shfl_sync(0xffffffffu, x.key, 31);
+  };
+  auto walk = [&](const Batch &b, uint32_t keys16, int half) {
+    for (;;) {
+      const float2 l = dots16<NC>(b.h, w);
+      float2 p;
+      p.x = exp2f(l.x * kLog2e - b.top[0]) - (b.val[0] >> 31 ? 1.f : 0.f);
+      p.y = exp2f(l.y * kLog2e - b.top[1]) - (b.val[1] >> 31 ? 1.f : 0.f);
+      const uint32_t others = __ballot_sync(0xffffffffu, (lane & 16) == half && keys16 != cur);
+      if (!others) {
+        weigh16<NC>(b.h, p, acc);
+        return;
+      }
+      // (a weight of zero would not do: another item's row may hold what is no number)
+      Rows16<NC> h = b.h;
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+        if (b.key[k] != cur) {
+          (k ? p.y : p.x) = 0.f;
+#pragma unroll
+          for (int c = 0; c < NC; ++c) h.w[k][c] = make_uint4(0, 0, 0, 0);
+        }
+      weigh16<NC>(h, p, acc);
+      // the next item among the 16, if there is one (they are sorted)
+      const uint32_t later = __ballot_sync(0xffffffffu, (lane & 16) == half && keys16 > cur && keys16 < none);
+      if (!later) return;
+      finish(!open);
+      open = first = false;
+      begin(__shfl_sync(0xffffffffu, keys16, __ffs(later) - 1));
+    }
+  };
+  Entries x = entries_from(s);
+  mark(x, s);
+  if (cur >= none) return;
+  begin(cur);
+  Batch b[2];
+  load(x, 0, b[0]);
+  for (uint32_t i = s; i < e; i += 32) {
+    const bool second = i + 16 < e, third = i + 32 < e;
+    Entries next = {none, 0, 0.f};
+    if (third) next = entries_from(i + 32);
+    if (second) load(x, 16, b[1]);
+    walk(b[0], x.key, 0);
+    if (third) {
+      mark(next, i + 32);
+      load(next, 0, b[0]);
+    }
+    if (second) walk(b[1], x.key, 16);
+    x = next;
   }
-  return lo;
+  finish(!open && !(e < entries && keys[e] == cur));
 }
 
 // Items without entries (zeros) and those whose entries reach over a chunk's end: their chunks' sums, in order.  A group of
@@ -267,7 +434,7 @@ __device__ __forceinline__ uint32_t lower_bound(const uint32_t *keys, uint32_t n
 template <typename T, int W, typename P>
 __global__ void __launch_bounds__(kThreads) loss_join_kernel(Args a, const float *__restrict__ lse,
                                                              const float *__restrict__ grad_loss,
-                                                             const uint32_t *__restrict__ keys, uint32_t entries, int chunk,
+                                                             const uint32_t *__restrict__ ranges, uint32_t entries, int chunk,
                                                              const float *__restrict__ part, T *__restrict__ dtable) {
   constexpr int LPC = P::LPC, V = P::V, NG = kThreads / LPC, WF = W < 4 ? W : 4;
   constexpr uint32_t kAlone = 16;  // chunks that a group of lanes adds up by itself
@@ -279,7 +446,7 @@ __global__ void __launch_bounds__(kThreads) loss_join_kernel(Args a, const float
   const int64_t item = (int64_t)blockIdx.x * NG + grp;
   if (col == 0) {
     uint2 r = make_uint2(0, 0);
-    if (item < a.items) r = make_uint2(lower_bound(keys, entries, (uint32_t)item), lower_bound(keys, entries, (uint32_t)item + 1));
+    if (item < a.items && entries) r = make_uint2(ranges[item], ranges[a.items + item]);
     range[grp] = r;
   }
   __syncthreads();
@@ -352,7 +519,7 @@ __global__ void __launch_bounds__(kThreads) loss_join_kernel(Args a, const float
 
 }  // namespace
 
-SortPlan sort_plan(const Args &a) {
+SortPlan sort_plan(const Args &a, int lanes) {
   SortPlan p;
   int bits = 1;
   while (bits < 31 && (int64_t)1 << bits <= a.items) ++bits;  // numbers 0 .. items
@@ -360,11 +527,10 @@ SortPlan sort_plan(const Args &a) {
   p.bits = (bits + p.passes - 1) / p.passes;
   p.entries = (int64_t)a.rows * (a.n + 1);
   p.tiles = (p.entries + kTile - 1) / kTile;
-  // long chunks leave fewer sums to join, short ones make more groups of lanes: twice as many as run at a time, if there
-  // are that many
-  const int64_t at_once = kSMs * 2048LL / lanes_of(a.groups);
+  // long chunks leave fewer sums to join, short ones make more groups of lanes: enough for 1024 threads an SM twice over, if
+  // there are that many
   p.chunk = 128;
-  while (p.chunk > 16 && p.entries / p.chunk < 2 * at_once) p.chunk /= 2;
+  while (p.chunk > 32 && p.entries / p.chunk * lanes < 2LL * kSMs * 1024) p.chunk /= 2;
   p.chunks = (p.entries + p.chunk - 1) / p.chunk;
   return p;
 }
@@ -377,7 +543,7 @@ Scratch carve(const Args &a, void *base) {
     off += (bytes + 255) / 256 * 256;
     return r;
   };
-  const SortPlan p = sort_plan(a);
+  const SortPlan p = sort_plan(a, lanes_of(a.groups));  // (narrow groups take the shortest chunks)
   const size_t list = (size_t)p.entries * sizeof(uint32_t);
   s.sums = reinterpret_cast<double2 *>(take(kForwardBytes));
   for (int i = 0; i < 2; ++i) {
@@ -386,6 +552,7 @@ Scratch carve(const Args &a, void *base) {
   }
   s.hist = reinterpret_cast<uint32_t *>(take((size_t)p.tiles * ((size_t)1 << p.bits) * sizeof(uint32_t)));
   s.totals = reinterpret_cast<uint32_t *>(take(kMaxDigits * sizeof(uint32_t)));
+  s.range = reinterpret_cast<uint32_t *>(take((size_t)a.items * 2 * sizeof(uint32_t)));
   s.part = reinterpret_cast<float *>(take((size_t)p.chunks * 2 * a.cols * sizeof(float)));
   s.bytes = off;
   return s;
@@ -393,8 +560,10 @@ Scratch carve(const Args &a, void *base) {
 
 int launch_items(const Args &a, int dtype, const void *hidden, const void *table, const float *lse, const float *grad_loss,
                  void *dtable, int width, const Scratch &s, cudaStream_t st) {
-  const SortPlan p = sort_plan(a);
+  const int nc = mma_chunks(dtype, width, a.cols);
+  const SortPlan p = sort_plan(a, nc ? 32 : lanes_of(a.groups));
   const uint32_t entries = (uint32_t)p.entries;
+  const Split by = split_by((uint32_t)a.n + 1);
   int at = 1;  // the buffer that holds the list
   if (!allow_smem(sort_move_kernel<true>, kMoveSmem) || !allow_smem(sort_move_kernel<false>, kMoveSmem)) return BLOSSOM_ERR_CUDA;
   for (int i = 0; entries && i < p.passes; ++i) {
@@ -404,33 +573,42 @@ int launch_items(const Args &a, int dtype, const void *hidden, const void *table
     if (hist) {
       {
         LaunchScope ls(K_LOSS_SORT, st);
-        launch_chained(i ? sort_count_kernel<false> : sort_count_kernel<true>, grid, block, 0, st, a,
-                       (const uint32_t *)s.keys[at], entries, shift, p.bits, hist);
+        launch_chained(i ? sort_count_kernel<false> : sort_count_kernel<true>, grid, block, 0, st, a, by, s.keys[at], entries,
+                       shift, p.bits, hist, s.range);
       }
       LaunchScope ls(K_LOSS_SORT, st);
       launch_chained(sort_scan_kernel, dim3(1u << p.bits), block, 0, st, hist, (int)p.tiles, s.totals);
     }
     LaunchScope ls(K_LOSS_SORT, st);
-    launch_chained(i ? sort_move_kernel<false> : sort_move_kernel<true>, grid, block, kMoveSmem, st, a,
+    launch_chained(i ? sort_move_kernel<false> : sort_move_kernel<true>, grid, block, kMoveSmem, st, a, by,
                    (const uint32_t *)s.keys[at], (const uint32_t *)s.vals[at], entries, shift, p.bits, (const uint32_t *)hist,
-                   (const uint32_t *)s.totals, s.keys[to], s.vals[to]);
+                   (const uint32_t *)s.totals, s.keys[to], s.vals[to], s.range);
     at = to;
+  }
+  const uint32_t *keys = s.keys[at], *vals = s.vals[at];
+  if (entries && nc) {
+    with_chunks(nc, [&](auto chunks) {
+      constexpr int NC = decltype(chunks)::value, per = kThreads / 32;
+      LaunchScope ls(K_LOSS_ITEMS, st);
+      launch_chained(loss_items_mma_kernel<NC>, dim3((unsigned)((p.chunks + per - 1) / per)), dim3(kThreads), 0, st, a,
+                     static_cast<const __nv_bfloat16 *>(hidden), static_cast<const __nv_bfloat16 *>(table), lse, grad_loss,
+                     keys, vals, entries, p.chunk, static_cast<__nv_bfloat16 *>(dtable), s.part, s.range);
+    });
   }
   with_plan(a.groups, [&](auto plan) {
     using P = decltype(plan);
     rows::with_type(dtype, width, [&](auto t, auto w) {
       using T = decltype(t);
       constexpr int W = decltype(w)::value, per = kThreads / P::LPC;
-      if (entries) {
+      if (entries && !nc) {
         LaunchScope ls(K_LOSS_ITEMS, st);
         launch_chained(loss_items_kernel<T, W, P>, dim3((unsigned)((p.chunks + per - 1) / per)), dim3(kThreads), 0, st, a,
-                       static_cast<const T *>(hidden), static_cast<const T *>(table), lse, grad_loss,
-                       (const uint32_t *)s.keys[at], (const uint32_t *)s.vals[at], entries, p.chunk, static_cast<T *>(dtable),
-                       s.part);
+                       static_cast<const T *>(hidden), static_cast<const T *>(table), lse, grad_loss, keys, vals, entries,
+                       p.chunk, static_cast<T *>(dtable), s.part, s.range);
       }
       LaunchScope ls(K_LOSS_ITEMS, st);
       launch_chained(loss_join_kernel<T, W, P>, dim3((unsigned)(((int64_t)a.items + per - 1) / per)), dim3(kThreads), 0, st, a,
-                     lse, grad_loss, (const uint32_t *)s.keys[at], entries, p.chunk, (const float *)s.part,
+                     lse, grad_loss, (const uint32_t *)s.range, entries, p.chunk, (const float *)s.part,
                      static_cast<T *>(dtable));
     });
   });

@@ -141,6 +141,124 @@ __global__ void __launch_bounds__(kThreads) loss_rows_kernel(Args a, const T *__
   }
 }
 
+// The same on the matrix units: a warp scores 16 candidates at a time, the next 16 rows are under way meanwhile.
+template <int NC, bool GRAD>
+__global__ void __launch_bounds__(kThreads) loss_rows_mma_kernel(Args a, const __nv_bfloat16 *__restrict__ hidden,
+                                                                 const __nv_bfloat16 *__restrict__ table,
+                                                                 float *__restrict__ lse, float *__restrict__ dh,
+                                                                 double2 *__restrict__ sums) {
+  __shared__ double2 warp_sums[kThreads / 32];
+  grid_chain_enter();
+  const int lane = (int)threadIdx.x % 32, warp = (int)threadIdx.x / 32, g = lane / 4, q = lane % 4;
+  double2 mine = make_double2(0.0, 0.0);
+  for (int64_t r = (int64_t)blockIdx.x * (kThreads / 32) + warp; r < a.rows; r += (int64_t)gridDim.x * (kThreads / 32)) {
+    const int row = (int)r, target = row_target(a, row);
+    float row_lse = 0.f, grad[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) grad[c] = 0.f;
+    if (target >= 0) {
+      uint4 h[NC];
+#pragma unroll
+      for (int c = 0; c < NC; ++c) h[c] = load16(hidden + row * a.sh + 32 * c + 8 * q, 32 * c + 8 * q < a.cols);
+      float2 acc[NC][4];
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[c][i] = make_float2(0.f, 0.f);
+      // candidates c0 .. c0 + 31, one a lane
+      auto ids_from = [&](int c0) { return c0 + lane <= a.n ? candidate(a, row, target, c0 + lane) : -1; };
+      // 16 rows; those of what is no candidate are not read
+      auto load = [&](int ids, int half, Rows16<NC> &w, int2 &at) {
+        at.x = __shfl_sync(0xffffffffu, ids, half + g);
+        at.y = __shfl_sync(0xffffffffu, ids, half + g + 8);
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          const int col = 32 * c + 8 * q;
+          w.w[0][c] = load16(table + at.x * a.st + col, at.x >= 0 && col < a.cols);
+          w.w[1][c] = load16(table + at.y * a.st + col, at.y >= 0 && col < a.cols);
+        }
+      };
+      float top = -INFINITY, total = 0.f, own = 0.f;  // of a quad: its rows of every 16
+      auto score = [&](const Rows16<NC> &w, int2 at) {
+        float2 l = dots16<NC>(w, h);
+        l.x = at.x >= 0 ? l.x * kLog2e : -INFINITY;  // in units of log 2
+        l.y = at.y >= 0 ? l.y * kLog2e : -INFINITY;
+        // The reference point only moves if it has to by more than 2^10: the sums stay far from the type's limits, and their
+        // relative rounding does not depend on it.
+        const float high = fmaxf(top, fmaxf(l.x, l.y));
+        if (high > top + 10.f) {
+          const float shrink = exp2f(top - high);
+          total *= shrink;
+          if (GRAD) {
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) acc[c][i].x *= shrink, acc[c][i].y *= shrink;
+          }
+          top = high;
+        }
+        const float2 p = make_float2(at.x >= 0 ? exp2f(l.x - top) : 0.f, at.y >= 0 ? exp2f(l.y - top) : 0.f);
+        total += p.x + p.y;
+        if (GRAD) weigh16<NC>(w, p, acc);
+        return l.x;
+      };
+      Rows16<NC> w[2];
+      int2 at[2];
+      int ids = ids_from(0);
+      load(ids, 0, w[0], at[0]);
+      for (int c0 = 0; c0 <= a.n; c0 += 32) {
+        const bool second = c0 + 16 <= a.n, third = c0 + 32 <= a.n;
+        int next = -1;
+        if (third) next = ids_from(c0 + 32);
+        if (second) load(ids, 16, w[1], at[1]);
+        const float first = score(w[0], at[0]);
+        if (c0 == 0) own = __shfl_sync(0xffffffffu, first, 0);
+        if (third) load(next, 0, w[0], at[0]);
+        if (second) score(w[1], at[1]);
+        ids = next;
+      }
+      float high = top;
+#pragma unroll
+      for (int o = 4; o < 32; o <<= 1) high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, o));
+      const float weight = exp2f(top - high);  // (0 for a quad that met no candidate)
+      total *= weight;
+#pragma unroll
+      for (int o = 4; o < 32; o <<= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+      const float lse2 = high + log2f(total);
+      row_lse = lse2 * kLn2;
+      mine.x += (double)((lse2 - own) * kLn2);
+      mine.y += 1.0;
+      if (GRAD) {
+        const float inv = weight / total;
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[c][i].x *= inv, acc[c][i].y *= inv;
+        scatter16<NC>(acc, grad);
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          const int col = 32 * c + 8 * q + g;
+          if (col < a.cols) grad[c] -= __bfloat162float(table[target * a.st + col]);
+        }
+      }
+    }
+    if (lane == 0) lse[row] = row_lse;
+    if (GRAD) {
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        const int col = 32 * c + 8 * q + g;
+        if (col < a.cols) dh[(int64_t)row * a.cols + col] = grad[c];
+      }
+    }
+  }
+  if (lane == 0) warp_sums[warp] = mine;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < kThreads / 32; ++i) mine.x += warp_sums[i].x, mine.y += warp_sums[i].y;
+    sums[blockIdx.x] = mine;
+  }
+}
+
 // The mean, from the CTAs' sums in a fixed order.
 __global__ void __launch_bounds__(kThreads) loss_mean_kernel(int ctas, const double2 *__restrict__ sums, float *__restrict__ loss,
                                                              float *__restrict__ count) {
@@ -244,17 +362,27 @@ extern "C" int blossom_sampled_loss_fwd(const blossom_loss_params *params, const
     rows::Alignment al;
     al.rows_at(hidden, a.sh, esz);
     al.rows_at(table, a.st, esz);
-    loss::with_plan(a.groups, [&](auto plan) {
-      using P = decltype(plan);
-      rows::with_type(params->dtype, al.elements(a.cols, esz), [&](auto t, auto w) {
-        using T = decltype(t);
-        constexpr int W = decltype(w)::value;
-        LaunchScope ls(K_LOSS_ROWS, st);
-        launch_chained(grad_hidden ? loss::loss_rows_kernel<T, W, P, true> : loss::loss_rows_kernel<T, W, P, false>,
-                       dim3((unsigned)ctas), dim3(loss::kThreads), 0, st, a, static_cast<const T *>(hidden),
-                       static_cast<const T *>(table), lse, grad_hidden, sums);
+    const int width = al.elements(a.cols, esz), nc = loss::mma_chunks(params->dtype, width, a.cols);
+    LaunchScope ls(K_LOSS_ROWS, st);
+    if (nc) {
+      loss::with_chunks(nc, [&](auto chunks) {
+        constexpr int NC = decltype(chunks)::value;
+        launch_chained(grad_hidden ? loss::loss_rows_mma_kernel<NC, true> : loss::loss_rows_mma_kernel<NC, false>,
+                       dim3((unsigned)ctas), dim3(loss::kThreads), 0, st, a, static_cast<const __nv_bfloat16 *>(hidden),
+                       static_cast<const __nv_bfloat16 *>(table), lse, grad_hidden, sums);
       });
-    });
+    } else {
+      loss::with_plan(a.groups, [&](auto plan) {
+        using P = decltype(plan);
+        rows::with_type(params->dtype, width, [&](auto t, auto w) {
+          using T = decltype(t);
+          constexpr int W = decltype(w)::value;
+          launch_chained(grad_hidden ? loss::loss_rows_kernel<T, W, P, true> : loss::loss_rows_kernel<T, W, P, false>,
+                         dim3((unsigned)ctas), dim3(loss::kThreads), 0, st, a, static_cast<const T *>(hidden),
+                         static_cast<const T *>(table), lse, grad_hidden, sums);
+        });
+      });
+    }
   }
   LaunchScope ls(K_LOSS_MEAN, st);
   launch_chained(loss::loss_mean_kernel, dim3(1), dim3(loss::kThreads), 0, st, ctas, (const double2 *)sums, loss_out,

@@ -228,6 +228,23 @@ def test_a_row_that_is_no_number_shows():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype,cols", [("bf16", 64), ("bf16", 50), ("fp32", 64)])
+def test_a_row_that_is_no_number_spoils_its_own_items_alone(dtype, cols):
+    import torch
+    from paper_2512_13368_b200.autograd import blossom_sampled_loss
+    h, w, t, neg = make(300, cols, 4000, 6, dtype, 8, noise=False)
+    h2 = h.clone()
+    h2[57, 3] = float("nan")
+    a, b = w.clone().requires_grad_(True), w.clone().requires_grad_(True)
+    g = torch.autograd.grad(blossom_sampled_loss(h, a, t, neg), a)[0]
+    bad = torch.autograd.grad(blossom_sampled_loss(h2, b, t, neg), b)[0]
+    mine = torch.zeros(4000, dtype=torch.bool, device="cuda")
+    mine[t[57]] = True
+    mine[neg[57]] = True
+    assert torch.equal(g[~mine], bad[~mine]) and bool(bad[mine].isnan().any(1).all())
+
+
+@pytest.mark.gpu
 def test_nothing_to_do():
     import torch
     from paper_2512_13368_b200.autograd import blossom_sampled_loss
