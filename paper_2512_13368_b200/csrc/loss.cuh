@@ -9,7 +9,7 @@ using rows::kSMs;
 using rows::load_group;
 using rows::store_group;
 
-constexpr int kMaxCols = 1024, kMaxRowCtas = kSMs * 8;
+constexpr int kMaxCols = 1024, kMaxRowCtas = kSMs * 16, kMmaThreads = 128;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct Args {
@@ -59,9 +59,36 @@ template <int NC>
 struct Rows16 {
   uint4 w[2][NC];
 };
-__device__ __forceinline__ uint4 load16(const __nv_bfloat16 *p, bool there) {
-  return there ? *reinterpret_cast<const uint4 *>(p) : make_uint4(0, 0, 0, 0);
-}
+// Where a lane finds its columns of a row.  Columns that are not there are read as the row's first ones and meet a zero of the
+// vector (a row that is no number somewhere is none in its product anyway).
+template <int NC, bool FULL>
+struct Lanes16 {
+  const char *base;
+  uint32_t stride;  // bytes
+  uint32_t off[NC];
+  __device__ __forceinline__ Lanes16(const __nv_bfloat16 *p, int64_t elements, int cols)
+      : base(reinterpret_cast<const char *>(p)), stride((uint32_t)(elements * 2)) {
+    const int q = (int)threadIdx.x % 4;
+    if (FULL) base += 16 * q;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) off[c] = FULL ? 64 * c : 32 * c + 8 * q < cols ? 64 * c + 16 * q : 0;
+  }
+  __device__ __forceinline__ void load(uint32_t row, uint4 (&w)[NC]) const {
+    const char *p = base + (uint64_t)row * stride;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) w[c] = *reinterpret_cast<const uint4 *>(p + off[c]);
+  }
+  // the vector, zero where there are no columns
+  __device__ __forceinline__ void vector(uint32_t row, int cols, uint4 (&w)[NC]) const {
+    load(row, w);
+    if (!FULL) {
+      const int q = (int)threadIdx.x % 4;
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+        if (32 * c + 8 * q >= cols) w[c] = make_uint4(0, 0, 0, 0);
+    }
+  }
+};
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                          uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -112,16 +139,23 @@ __device__ __forceinline__ void scatter16(const float2 (&acc)[NC][4], float (&ou
     out[c] = (g & 1 ? b[1] : b[0]) + __shfl_xor_sync(0xffffffffu, g & 1 ? b[0] : b[1], 4);
   }
 }
-// Chunks of 32 columns where the matrix units take the rows (bf16, 16-byte aligned rows of up to 128 columns), else 0.
-inline int mma_chunks(int dtype, int width, int cols) {
-  return dtype == BLOSSOM_DTYPE_BF16 && width == 8 && cols <= 128 ? (cols <= 32 ? 1 : cols <= 64 ? 2 : 4) : 0;
+// Chunks of 32 columns where the matrix units take the rows (bf16, 16-byte aligned rows of up to 128 columns less than 4 GiB
+// apart), else 0.
+inline int mma_chunks(const Args &a, int dtype, int width) {
+  if (dtype != BLOSSOM_DTYPE_BF16 || width != 8 || a.cols > 128 || a.sh > 0x7fffffffLL || a.st > 0x7fffffffLL) return 0;
+  return a.cols <= 32 ? 1 : a.cols <= 64 ? 2 : 4;
 }
+// f(chunks, all of their columns are there)
 template <typename F>
-inline void with_chunks(int nc, F &&f) {
+inline void with_chunks(int nc, int cols, F &&f) {
   using std::integral_constant;
-  if (nc == 1) f(integral_constant<int, 1>());
-  else if (nc == 2) f(integral_constant<int, 2>());
-  else f(integral_constant<int, 4>());
+  auto full = [&](auto n) {
+    if (cols == 32 * decltype(n)::value) f(n, integral_constant<bool, true>());
+    else f(n, integral_constant<bool, false>());
+  };
+  if (nc == 1) full(integral_constant<int, 1>());
+  else if (nc == 2) full(integral_constant<int, 2>());
+  else full(integral_constant<int, 4>());
 }
 
 // Device scratch; the forward uses `sums` alone.

@@ -110,9 +110,11 @@ __global__ void __launch_bounds__(kSortThreads) sort_scan_kernel(uint32_t *__res
 }
 
 // Lanes that hold the same digit as this one, among those that hold any: one ballot a bit.
-__device__ __forceinline__ uint32_t same_digit(uint32_t d, int bits, bool there) {
+template <int BITS>
+__device__ __forceinline__ uint32_t same_digit(uint32_t d, bool there) {
   uint32_t peers = __ballot_sync(0xffffffffu, there);
-  for (int b = 0; b < bits; ++b) {
+#pragma unroll
+  for (int b = 0; b < BITS; ++b) {
     const bool bit = d >> b & 1;
     const uint32_t v = __ballot_sync(0xffffffffu, bit);
     peers &= bit ? v : ~v;
@@ -121,26 +123,24 @@ __device__ __forceinline__ uint32_t same_digit(uint32_t d, int bits, bool there)
 }
 
 // A tile's entries to their places, in order: ranks within a warp by matching digits, then warps, then digits; the tile is put
-// in order in shared memory first, so that it leaves in runs.  FIRST: the values are made here, and where there is
-// one tile (hist null, its own counts are all) the keys too.
-template <bool FIRST>
+// in order in shared memory first, so that it leaves in runs.  FIRST: the values are made here.  hist null: there is one tile,
+// whose own counts are all.
+template <int BITS, bool FIRST>
 __global__ void __launch_bounds__(kSortThreads, 2) sort_move_kernel(Args a, Split by, const uint32_t *__restrict__ keys,
                                                                     const uint32_t *__restrict__ vals, uint32_t entries,
-                                                                    int shift, int bits, const uint32_t *__restrict__ hist,
+                                                                    int shift, const uint32_t *__restrict__ hist,
                                                                     const uint32_t *__restrict__ totals,
                                                                     uint32_t *__restrict__ keys_out,
-                                                                    uint32_t *__restrict__ vals_out, uint32_t *__restrict__ range) {
+                                                                    uint32_t *__restrict__ vals_out) {
   constexpr int NW = kSortThreads / 32;
   extern __shared__ uint32_t sm[];
   uint32_t *sk = sm, *sv = sm + kTile, *offset = sm + 2 * kTile, *count = offset + kMaxDigits;  // count[warp][digit]
   __shared__ uint32_t warp_totals[NW];
   grid_chain_enter();
-  const int digits = 1 << bits, tid = (int)threadIdx.x, lane = tid % 32, warp = tid / 32;
-  const uint32_t mask = (uint32_t)digits - 1;
+  constexpr int digits = 1 << BITS;
+  constexpr uint32_t mask = (uint32_t)digits - 1;
+  const int tid = (int)threadIdx.x, lane = tid % 32, warp = tid / 32;
   for (int i = tid; i < NW * digits; i += kSortThreads) count[i] = 0;
-  if (FIRST && !hist)
-    for (int64_t i = (int64_t)blockIdx.x * kSortThreads + tid; i < 2 * (int64_t)a.items; i += (int64_t)gridDim.x * kSortThreads)
-      range[i] = 0;
   __syncthreads();
   const uint32_t tile0 = blockIdx.x * (uint32_t)kTile, e0 = tile0 + (uint32_t)warp * (32 * kSortPerThread) + (uint32_t)lane;
   uint32_t key[kSortPerThread], rank[kSortPerThread / 2];  // (two ranks a word)
@@ -148,14 +148,14 @@ __global__ void __launch_bounds__(kSortThreads, 2) sort_move_kernel(Args a, Spli
   for (int r = 0; r < kSortPerThread; ++r) {
     const uint32_t e = e0 + 32 * r;
     key[r] = 0;
-    if (e < entries) key[r] = FIRST && !hist ? entry_key(a, by, e) : keys[e];
+    if (e < entries) key[r] = keys[e];
   }
   uint32_t *mine = count + warp * digits;
 #pragma unroll
   for (int r = 0; r < kSortPerThread; ++r) {
     const bool there = e0 + 32 * r < entries;
     const uint32_t d = key[r] >> shift & mask;
-    const uint32_t peers = same_digit(d, bits, there), below = peers & ((1u << lane) - 1);
+    const uint32_t peers = same_digit<BITS>(d, there), below = peers & ((1u << lane) - 1);
     const uint32_t at = there ? mine[d] + (uint32_t)__popc(below) : 0;
     rank[r / 2] = r % 2 ? rank[r / 2] | at << 16 : at;
     __syncwarp();
@@ -187,15 +187,24 @@ __global__ void __launch_bounds__(kSortThreads, 2) sort_move_kernel(Args a, Spli
     if (e0 + 32 * r < entries) {
       const uint32_t at = mine[key[r] >> shift & mask] + (r % 2 ? rank[r / 2] >> 16 : rank[r / 2] & 0xffffu);
       sk[at] = key[r];
-      sv[at] = FIRST ? entry_val(a, by, e0 + 32 * r) : vals[e0 + 32 * r];
+      sv[at] = FIRST ? e0 + 32 * r : vals[e0 + 32 * r];
     }
   __syncthreads();
   const uint32_t here = entries - tile0 < (uint32_t)kTile ? entries - tile0 : (uint32_t)kTile;
   for (uint32_t i = (uint32_t)tid; i < here; i += kSortThreads) {
     const uint32_t k = sk[i], at = offset[k >> shift & mask] + i;
     keys_out[at] = k;
-    vals_out[at] = sv[i];
+    vals_out[at] = FIRST ? entry_val(a, by, sv[i]) : sv[i];
   }
+}
+using MoveKernel = void (*)(Args, Split, const uint32_t *, const uint32_t *, uint32_t, int, const uint32_t *, const uint32_t *,
+                            uint32_t *, uint32_t *);
+template <bool FIRST>
+MoveKernel move_kernel(int bits) {
+  static const MoveKernel k[9] = {sort_move_kernel<1, FIRST>, sort_move_kernel<2, FIRST>, sort_move_kernel<3, FIRST>,
+                                  sort_move_kernel<4, FIRST>, sort_move_kernel<5, FIRST>, sort_move_kernel<6, FIRST>,
+                                  sort_move_kernel<7, FIRST>, sort_move_kernel<8, FIRST>, sort_move_kernel<9, FIRST>};
+  return k[bits - 1];
 }
 constexpr size_t kMoveSmem = (2 * kTile + kMaxDigits + kSortThreads / 32 * kMaxDigits) * sizeof(uint32_t);
 
@@ -294,52 +303,35 @@ __global__ void __launch_bounds__(kThreads) loss_items_kernel(Args a, const T *_
 }
 
 // The same on the matrix units: a warp walks a chunk 16 entries at a time, their hidden rows the first operand, the item's
-// row the second.  Sixteen entries of more than one item go through once an item, the others' weights zero.
-template <int NC>
-__global__ void __launch_bounds__(kThreads) loss_items_mma_kernel(Args a, const __nv_bfloat16 *__restrict__ hidden,
-                                                                  const __nv_bfloat16 *__restrict__ table,
-                                                                  const float *__restrict__ lse,
-                                                                  const float *__restrict__ grad_loss,
-                                                                  const uint32_t *__restrict__ keys,
-                                                                  const uint32_t *__restrict__ vals, uint32_t entries, int chunk,
-                                                                  __nv_bfloat16 *__restrict__ dtable, float *__restrict__ part,
-                                                                  uint32_t *__restrict__ range) {
+// row the second; the next 16 rows are under way meanwhile.  Sixteen entries of more than one item go through once an item.
+template <int NC, bool FULL>
+__global__ void __launch_bounds__(kMmaThreads, NC == 1 ? 8 : NC == 2 ? 5 : 3)
+    loss_items_mma_kernel(Args a, const __nv_bfloat16 *__restrict__ hidden, const __nv_bfloat16 *__restrict__ table,
+                          const float *__restrict__ lse, const float *__restrict__ grad_loss, const uint32_t *__restrict__ keys,
+                          const uint32_t *__restrict__ vals, uint32_t entries, int chunk, __nv_bfloat16 *__restrict__ dtable,
+                          float *__restrict__ part, uint32_t *__restrict__ range) {
   grid_chain_enter();
   const int lane = (int)threadIdx.x % 32, g = lane / 4, q = lane % 4;
-  const int64_t c0 = (int64_t)blockIdx.x * (kThreads / 32) + threadIdx.x / 32;
+  const int64_t c0 = (int64_t)blockIdx.x * (kMmaThreads / 32) + threadIdx.x / 32;
   if (c0 * chunk >= entries) return;
   const uint32_t none = (uint32_t)a.items, s = (uint32_t)(c0 * chunk);
   const uint32_t e = entries - s < (uint32_t)chunk ? entries : s + (uint32_t)chunk;
-  const float scale = grad_scale(a, lse, grad_loss);
-  // 32 entries, one a lane
-  struct Entries {
+  const Lanes16<NC, FULL> from_hidden(hidden, a.sh, a.cols), from_table(table, a.st, a.cols);
+  struct Entries {  // 32 of them, one a lane; what lies behind the chunk is no candidate of the first position
     uint32_t key, val;
     float top;
   };
   auto entries_from = [&](uint32_t i) {
     Entries x = {none, 0, 0.f};
-    if (i + lane < e) x.key = keys[i + lane], x.val = vals[i + lane];
-    if (x.key < none) x.top = lse[x.val & 0x7fffffffu] * kLog2e;
+    if (i + lane < e) {
+      x.key = keys[i + lane], x.val = vals[i + lane];
+      x.top = lse[x.val & 0x7fffffffu] * kLog2e;
+    }
     return x;
   };
-  struct Batch {  // of 16 entries, those of rows g and g + 8
-    Rows16<NC> h;
-    uint32_t key[2], val[2];
-    float top[2];
-  };
-  auto load = [&](const Entries &x, int half, Batch &b) {
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      const int from = half + g + 8 * k;
-      b.key[k] = __shfl_sync(0xffffffffu, x.key, from);
-      b.val[k] = __shfl_sync(0xffffffffu, x.val, from);
-      b.top[k] = __shfl_sync(0xffffffffu, x.top, from);
-#pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        const int col = 32 * c + 8 * q;
-        b.h.w[k][c] = load16(hidden + (int64_t)(b.val[k] & 0x7fffffffu) * a.sh + col, b.key[k] < none && col < a.cols);
-      }
-    }
+  auto load = [&](const Entries &x, int half, Rows16<NC> &h) {
+    from_hidden.load(__shfl_sync(0xffffffffu, x.val, half + g) & 0x7fffffffu, h.w[0]);
+    from_hidden.load(__shfl_sync(0xffffffffu, x.val, half + g + 8) & 0x7fffffffu, h.w[1]);
   };
   uint4 w[NC];
   float2 acc[NC][4];
@@ -347,16 +339,16 @@ __global__ void __launch_bounds__(kThreads) loss_items_mma_kernel(Args a, const 
   bool open = before == cur, first = true;  // open: the item's entries began in a chunk before
   auto begin = [&](uint32_t item) {
     cur = item;
+    from_table.vector(item, a.cols, w);
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      w[c] = load16(table + cur * a.st + 32 * c + 8 * q, 32 * c + 8 * q < a.cols);
+    for (int c = 0; c < NC; ++c)
 #pragma unroll
       for (int i = 0; i < 4; ++i) acc[c][i] = make_float2(0.f, 0.f);
-    }
   };
   auto finish = [&](bool whole) {
     float sum[NC];
     scatter16<NC>(acc, sum);
+    const float scale = whole ? grad_scale(a, lse, grad_loss) : 1.f;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
       const int col = 32 * c + 8 * q + g;
@@ -378,52 +370,54 @@ __global__ void __launch_bounds__(kThreads) loss_items_mma_kernel(Args a, const 
     }
     before = __shfl_sync(0xffffffffu, x.key, 31);
   };
-  auto walk = [&](const Batch &b, uint32_t keys16, int half) {
+  auto walk = [&](const Rows16<NC> &h, const Entries &x, int half) {
+    const float2 top = make_float2(__shfl_sync(0xffffffffu, x.top, half + g), __shfl_sync(0xffffffffu, x.top, half + g + 8));
+    const uint32_t targets = __ballot_sync(0xffffffffu, x.val >> 31) >> half;
     for (;;) {
-      const float2 l = dots16<NC>(b.h, w);
+      const float2 l = dots16<NC>(h, w);
       float2 p;
-      p.x = exp2f(l.x * kLog2e - b.top[0]) - (b.val[0] >> 31 ? 1.f : 0.f);
-      p.y = exp2f(l.y * kLog2e - b.top[1]) - (b.val[1] >> 31 ? 1.f : 0.f);
-      const uint32_t others = __ballot_sync(0xffffffffu, (lane & 16) == half && keys16 != cur);
-      if (!others) {
-        weigh16<NC>(b.h, p, acc);
+      p.x = exp2f(l.x * kLog2e - top.x) - (targets >> g & 1 ? 1.f : 0.f);
+      p.y = exp2f(l.y * kLog2e - top.y) - (targets >> g & 0x100 ? 1.f : 0.f);
+      const uint32_t others = __ballot_sync(0xffffffffu, x.key != cur) >> half;
+      if (!(others & 0xffffu)) {
+        weigh16<NC>(h, p, acc);
         return;
       }
       // (a weight of zero would not do: another item's row may hold what is no number)
-      Rows16<NC> h = b.h;
+      Rows16<NC> own = h;
 #pragma unroll
       for (int k = 0; k < 2; ++k)
-        if (b.key[k] != cur) {
+        if (others >> (g + 8 * k) & 1) {
           (k ? p.y : p.x) = 0.f;
 #pragma unroll
-          for (int c = 0; c < NC; ++c) h.w[k][c] = make_uint4(0, 0, 0, 0);
+          for (int c = 0; c < NC; ++c) own.w[k][c] = make_uint4(0, 0, 0, 0);
         }
-      weigh16<NC>(h, p, acc);
+      weigh16<NC>(own, p, acc);
       // the next item among the 16, if there is one (they are sorted)
-      const uint32_t later = __ballot_sync(0xffffffffu, (lane & 16) == half && keys16 > cur && keys16 < none);
+      const uint32_t later = __ballot_sync(0xffffffffu, (lane & 16) == half && x.key > cur && x.key < none);
       if (!later) return;
       finish(!open);
       open = first = false;
-      begin(__shfl_sync(0xffffffffu, keys16, __ffs(later) - 1));
+      begin(__shfl_sync(0xffffffffu, x.key, __ffs(later) - 1));
     }
   };
   Entries x = entries_from(s);
   mark(x, s);
   if (cur >= none) return;
   begin(cur);
-  Batch b[2];
-  load(x, 0, b[0]);
+  Rows16<NC> h[2];
+  load(x, 0, h[0]);
   for (uint32_t i = s; i < e; i += 32) {
     const bool second = i + 16 < e, third = i + 32 < e;
     Entries next = {none, 0, 0.f};
     if (third) next = entries_from(i + 32);
-    if (second) load(x, 16, b[1]);
-    walk(b[0], x.key, 0);
+    if (second) load(x, 16, h[1]);
+    walk(h[0], x, 0);
     if (third) {
       mark(next, i + 32);
-      load(next, 0, b[0]);
+      load(next, 0, h[0]);
     }
-    if (second) walk(b[1], x.key, 16);
+    if (second) walk(h[1], x, 16);
     x = next;
   }
   finish(!open && !(e < entries && keys[e] == cur));
@@ -560,38 +554,39 @@ Scratch carve(const Args &a, void *base) {
 
 int launch_items(const Args &a, int dtype, const void *hidden, const void *table, const float *lse, const float *grad_loss,
                  void *dtable, int width, const Scratch &s, cudaStream_t st) {
-  const int nc = mma_chunks(dtype, width, a.cols);
+  const int nc = mma_chunks(a, dtype, width);
   const SortPlan p = sort_plan(a, nc ? 32 : lanes_of(a.groups));
   const uint32_t entries = (uint32_t)p.entries;
   const Split by = split_by((uint32_t)a.n + 1);
   int at = 1;  // the buffer that holds the list
-  if (!allow_smem(sort_move_kernel<true>, kMoveSmem) || !allow_smem(sort_move_kernel<false>, kMoveSmem)) return BLOSSOM_ERR_CUDA;
+  const MoveKernel moves[2] = {move_kernel<true>(p.bits), move_kernel<false>(p.bits)};
+  if (!allow_smem(moves[0], kMoveSmem) || !allow_smem(moves[1], kMoveSmem)) return BLOSSOM_ERR_CUDA;
   for (int i = 0; entries && i < p.passes; ++i) {
     const int shift = i * p.bits, to = at ^ 1;
     uint32_t *hist = p.tiles > 1 ? s.hist : nullptr;
     const dim3 grid((unsigned)p.tiles), block(kSortThreads);
+    if (hist || i == 0) {  // (the first makes the keys too)
+      LaunchScope ls(K_LOSS_SORT, st);
+      launch_chained(i ? sort_count_kernel<false> : sort_count_kernel<true>, grid, block, 0, st, a, by, s.keys[at], entries,
+                     shift, p.bits, s.hist, s.range);
+    }
     if (hist) {
-      {
-        LaunchScope ls(K_LOSS_SORT, st);
-        launch_chained(i ? sort_count_kernel<false> : sort_count_kernel<true>, grid, block, 0, st, a, by, s.keys[at], entries,
-                       shift, p.bits, hist, s.range);
-      }
       LaunchScope ls(K_LOSS_SORT, st);
       launch_chained(sort_scan_kernel, dim3(1u << p.bits), block, 0, st, hist, (int)p.tiles, s.totals);
     }
     LaunchScope ls(K_LOSS_SORT, st);
-    launch_chained(i ? sort_move_kernel<false> : sort_move_kernel<true>, grid, block, kMoveSmem, st, a, by,
-                   (const uint32_t *)s.keys[at], (const uint32_t *)s.vals[at], entries, shift, p.bits, (const uint32_t *)hist,
-                   (const uint32_t *)s.totals, s.keys[to], s.vals[to], s.range);
+    launch_chained(moves[i > 0], grid, block, kMoveSmem, st, a, by, (const uint32_t *)s.keys[at],
+                   (const uint32_t *)s.vals[at], entries, shift, (const uint32_t *)hist,
+                   (const uint32_t *)s.totals, s.keys[to], s.vals[to]);
     at = to;
   }
   const uint32_t *keys = s.keys[at], *vals = s.vals[at];
   if (entries && nc) {
-    with_chunks(nc, [&](auto chunks) {
-      constexpr int NC = decltype(chunks)::value, per = kThreads / 32;
+    with_chunks(nc, a.cols, [&](auto chunks, auto all) {
+      constexpr int NC = decltype(chunks)::value, per = kMmaThreads / 32;
       LaunchScope ls(K_LOSS_ITEMS, st);
-      launch_chained(loss_items_mma_kernel<NC>, dim3((unsigned)((p.chunks + per - 1) / per)), dim3(kThreads), 0, st, a,
-                     static_cast<const __nv_bfloat16 *>(hidden), static_cast<const __nv_bfloat16 *>(table), lse, grad_loss,
+      launch_chained(loss_items_mma_kernel<NC, decltype(all)::value>, dim3((unsigned)((p.chunks + per - 1) / per)), dim3(kMmaThreads), 0, st,
+                     a, static_cast<const __nv_bfloat16 *>(hidden), static_cast<const __nv_bfloat16 *>(table), lse, grad_loss,
                      keys, vals, entries, p.chunk, static_cast<__nv_bfloat16 *>(dtable), s.part, s.range);
     });
   }

@@ -5,6 +5,8 @@
 // running maximum, sum and weighted sum of rows, and the groups are joined at the end.  Every candidate's row is read
 // once.  Bound: the candidates' rows come from L2 at best (128 bytes each for 64 columns of bf16), 2.1 GB for 131072
 // positions of 128 candidates, against 0.17 GB that HBM has to move.
+#include <float.h>
+
 #include "loss.cuh"
 
 namespace blossom {
@@ -141,48 +143,45 @@ __global__ void __launch_bounds__(kThreads) loss_rows_kernel(Args a, const T *__
   }
 }
 
-// The same on the matrix units: a warp scores 16 candidates at a time, the next 16 rows are under way meanwhile.
-template <int NC, bool GRAD>
-__global__ void __launch_bounds__(kThreads) loss_rows_mma_kernel(Args a, const __nv_bfloat16 *__restrict__ hidden,
-                                                                 const __nv_bfloat16 *__restrict__ table,
-                                                                 float *__restrict__ lse, float *__restrict__ dh,
-                                                                 double2 *__restrict__ sums) {
-  __shared__ double2 warp_sums[kThreads / 32];
+// The same on the matrix units: a warp scores 16 candidates at a time, the next 16 rows are under way meanwhile.  What is no
+// candidate is read as the target's row and weighs nothing.
+template <int NC, bool FULL, bool GRAD>
+__global__ void __launch_bounds__(kMmaThreads, NC == 1 ? 8 : NC == 2 ? 5 : 3)
+    loss_rows_mma_kernel(Args a, const __nv_bfloat16 *__restrict__ hidden, const __nv_bfloat16 *__restrict__ table,
+                         float *__restrict__ lse, float *__restrict__ dh, double2 *__restrict__ sums) {
+  __shared__ double2 warp_sums[kMmaThreads / 32];
   grid_chain_enter();
   const int lane = (int)threadIdx.x % 32, warp = (int)threadIdx.x / 32, g = lane / 4, q = lane % 4;
+  const Lanes16<NC, FULL> from_hidden(hidden, a.sh, a.cols), from_table(table, a.st, a.cols);
   double2 mine = make_double2(0.0, 0.0);
-  for (int64_t r = (int64_t)blockIdx.x * (kThreads / 32) + warp; r < a.rows; r += (int64_t)gridDim.x * (kThreads / 32)) {
+  for (int64_t r = (int64_t)blockIdx.x * (kMmaThreads / 32) + warp; r < a.rows; r += (int64_t)gridDim.x * (kMmaThreads / 32)) {
     const int row = (int)r, target = row_target(a, row);
     float row_lse = 0.f, grad[NC];
 #pragma unroll
     for (int c = 0; c < NC; ++c) grad[c] = 0.f;
     if (target >= 0) {
       uint4 h[NC];
-#pragma unroll
-      for (int c = 0; c < NC; ++c) h[c] = load16(hidden + row * a.sh + 32 * c + 8 * q, 32 * c + 8 * q < a.cols);
+      from_hidden.vector((uint32_t)row, a.cols, h);
       float2 acc[NC][4];
 #pragma unroll
       for (int c = 0; c < NC; ++c)
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[c][i] = make_float2(0.f, 0.f);
-      // candidates c0 .. c0 + 31, one a lane
-      auto ids_from = [&](int c0) { return c0 + lane <= a.n ? candidate(a, row, target, c0 + lane) : -1; };
-      // 16 rows; those of what is no candidate are not read
-      auto load = [&](int ids, int half, Rows16<NC> &w, int2 &at) {
-        at.x = __shfl_sync(0xffffffffu, ids, half + g);
-        at.y = __shfl_sync(0xffffffffu, ids, half + g + 8);
-#pragma unroll
-        for (int c = 0; c < NC; ++c) {
-          const int col = 32 * c + 8 * q;
-          w.w[0][c] = load16(table + at.x * a.st + col, at.x >= 0 && col < a.cols);
-          w.w[1][c] = load16(table + at.y * a.st + col, at.y >= 0 && col < a.cols);
-        }
+      // candidates c0 .. c0 + 31, one a lane; there: a bit for each
+      auto ids_from = [&](int c0, uint32_t &there) {
+        const int id = c0 + lane <= a.n ? candidate(a, row, target, c0 + lane) : -1;
+        there = __ballot_sync(0xffffffffu, id >= 0);
+        return id >= 0 ? id : target;
       };
-      float top = -INFINITY, total = 0.f, own = 0.f;  // of a quad: its rows of every 16
-      auto score = [&](const Rows16<NC> &w, int2 at) {
+      auto load = [&](int ids, int half, Rows16<NC> &w) {
+        from_table.load((uint32_t)__shfl_sync(0xffffffffu, ids, half + g), w.w[0]);
+        from_table.load((uint32_t)__shfl_sync(0xffffffffu, ids, half + g + 8), w.w[1]);
+      };
+      float top = -FLT_MAX, total = 0.f, own = 0.f;  // of a quad: its two rows of every 16
+      auto score = [&](const Rows16<NC> &w, uint32_t there) {
         float2 l = dots16<NC>(w, h);
-        l.x = at.x >= 0 ? l.x * kLog2e : -INFINITY;  // in units of log 2
-        l.y = at.y >= 0 ? l.y * kLog2e : -INFINITY;
+        l.x = there >> g & 1 ? l.x * kLog2e : -INFINITY;  // in units of log 2
+        l.y = there >> g & 0x100 ? l.y * kLog2e : -INFINITY;
         // The reference point only moves if it has to by more than 2^10: the sums stay far from the type's limits, and their
         // relative rounding does not depend on it.
         const float high = fmaxf(top, fmaxf(l.x, l.y));
@@ -197,25 +196,26 @@ __global__ void __launch_bounds__(kThreads) loss_rows_mma_kernel(Args a, const _
           }
           top = high;
         }
-        const float2 p = make_float2(at.x >= 0 ? exp2f(l.x - top) : 0.f, at.y >= 0 ? exp2f(l.y - top) : 0.f);
+        const float2 p = make_float2(exp2f(l.x - top), exp2f(l.y - top));
         total += p.x + p.y;
         if (GRAD) weigh16<NC>(w, p, acc);
         return l.x;
       };
       Rows16<NC> w[2];
-      int2 at[2];
-      int ids = ids_from(0);
-      load(ids, 0, w[0], at[0]);
+      uint32_t there, there_next = 0;
+      int ids = ids_from(0, there);
+      load(ids, 0, w[0]);
       for (int c0 = 0; c0 <= a.n; c0 += 32) {
         const bool second = c0 + 16 <= a.n, third = c0 + 32 <= a.n;
-        int next = -1;
-        if (third) next = ids_from(c0 + 32);
-        if (second) load(ids, 16, w[1], at[1]);
-        const float first = score(w[0], at[0]);
+        int next = target;
+        if (third) next = ids_from(c0 + 32, there_next);
+        if (second) load(ids, 16, w[1]);
+        const float first = score(w[0], there);
         if (c0 == 0) own = __shfl_sync(0xffffffffu, first, 0);
-        if (third) load(next, 0, w[0], at[0]);
-        if (second) score(w[1], at[1]);
+        if (third) load(next, 0, w[0]);
+        if (second) score(w[1], there >> 16);
         ids = next;
+        there = there_next;
       }
       float high = top;
 #pragma unroll
@@ -254,7 +254,7 @@ __global__ void __launch_bounds__(kThreads) loss_rows_mma_kernel(Args a, const _
   if (lane == 0) warp_sums[warp] = mine;
   __syncthreads();
   if (threadIdx.x == 0) {
-    for (int i = 1; i < kThreads / 32; ++i) mine.x += warp_sums[i].x, mine.y += warp_sums[i].y;
+    for (int i = 1; i < kMmaThreads / 32; ++i) mine.x += warp_sums[i].x, mine.y += warp_sums[i].y;
     sums[blockIdx.x] = mine;
   }
 }
@@ -356,19 +356,21 @@ extern "C" int blossom_sampled_loss_fwd(const blossom_loss_params *params, const
   const cudaStream_t st = (cudaStream_t)stream;
   const size_t esz = params->dtype == BLOSSOM_DTYPE_FP32 ? 4 : 2;
   double2 *sums = static_cast<double2 *>(workspace);
-  const int64_t want = ((int64_t)a.rows + 7) / 8;
-  const int ctas = (int)(want < loss::kMaxRowCtas ? want : loss::kMaxRowCtas);
+  rows::Alignment al;
+  al.rows_at(hidden, a.sh, esz);
+  al.rows_at(table, a.st, esz);
+  const int width = al.elements(a.cols, esz), nc = loss::mma_chunks(a, params->dtype, width);
+  const int warps = (nc ? loss::kMmaThreads : loss::kThreads) / 32;  // a row each
+  const int64_t want = ((int64_t)a.rows + warps - 1) / warps, most = loss::kSMs * 64 / warps;
+  const int ctas = (int)(want < most ? want : most);
   if (ctas) {
-    rows::Alignment al;
-    al.rows_at(hidden, a.sh, esz);
-    al.rows_at(table, a.st, esz);
-    const int width = al.elements(a.cols, esz), nc = loss::mma_chunks(params->dtype, width, a.cols);
     LaunchScope ls(K_LOSS_ROWS, st);
     if (nc) {
-      loss::with_chunks(nc, [&](auto chunks) {
+      loss::with_chunks(nc, a.cols, [&](auto chunks, auto all) {
         constexpr int NC = decltype(chunks)::value;
-        launch_chained(grad_hidden ? loss::loss_rows_mma_kernel<NC, true> : loss::loss_rows_mma_kernel<NC, false>,
-                       dim3((unsigned)ctas), dim3(loss::kThreads), 0, st, a, static_cast<const __nv_bfloat16 *>(hidden),
+        constexpr bool FULL = decltype(all)::value;
+        launch_chained(grad_hidden ? loss::loss_rows_mma_kernel<NC, FULL, true> : loss::loss_rows_mma_kernel<NC, FULL, false>,
+                       dim3((unsigned)ctas), dim3(loss::kMmaThreads), 0, st, a, static_cast<const __nv_bfloat16 *>(hidden),
                        static_cast<const __nv_bfloat16 *>(table), lse, grad_hidden, sums);
       });
     } else {
