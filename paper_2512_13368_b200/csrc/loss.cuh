@@ -50,42 +50,49 @@ inline void with_plan(int groups, F &&f) {
 }
 inline int lanes_of(int groups) { return groups <= 4 ? 4 : groups <= 8 ? 8 : groups <= 16 ? 16 : 32; }
 
-// ---- bf16 rows of up to 32 NC columns on the matrix units ---------------------------------------------
-// A warp scores 16 rows against one vector.  Lane 4 g + q loads 16 bytes at columns 32 c + 8 q of the rows g and g + 8: as the
-// order in which a product's columns are added up is free, those are the first operand of two m16n8k16 products a
-// chunk c as they come, without a detour through shared memory; the vector, laid out alike, is the second operand in all
-// 8 of its columns, so that every lane of a quad ends up with the products of its own two rows.
-template <int NC>
+// ---- bf16 rows of up to 64 NL columns on the matrix units ---------------------------------------------
+// A warp scores 16 rows against one vector.  Lane 8 r + s loads 16 bytes at column 8 s of the rows r, 4 + r, 8 + r and 12 + r,
+// so that every load takes whole 128-byte lines.  As the order in which a product's columns are added up is free, two rows'
+// registers are the first operand of two m16n8k16 products as they come, without a detour through shared memory: its
+// row g = 2 r + s / 4 is the half s / 4 of a row.  The vector, laid out alike, is the second operand: its first half
+// in the even columns, its second in the odd ones, of which a lane keeps the one that belongs to its half.
+template <int NL>
 struct Rows16 {
-  uint4 w[2][NC];
+  uint4 w[4][NL];
 };
 // Where a lane finds its columns of a row.  Columns that are not there are read as the row's first ones and meet a zero of the
 // vector (a row that is no number somewhere is none in its product anyway).
-template <int NC, bool FULL>
+template <int NL, bool FULL>
 struct Lanes16 {
   const char *base;
   uint32_t stride;  // bytes
-  uint32_t off[NC];
+  uint32_t off[NL];
   __device__ __forceinline__ Lanes16(const __nv_bfloat16 *p, int64_t elements, int cols)
       : base(reinterpret_cast<const char *>(p)), stride((uint32_t)(elements * 2)) {
-    const int q = (int)threadIdx.x % 4;
-    if (FULL) base += 16 * q;
+    const int s = (int)threadIdx.x % 8;
+    if (FULL) base += 16 * s;
 #pragma unroll
-    for (int c = 0; c < NC; ++c) off[c] = FULL ? 64 * c : 32 * c + 8 * q < cols ? 64 * c + 16 * q : 0;
+    for (int c = 0; c < NL; ++c) off[c] = FULL ? 128 * c : 64 * c + 8 * s < cols ? 128 * c + 16 * s : 0;
   }
-  __device__ __forceinline__ void load(uint32_t row, uint4 (&w)[NC]) const {
+  __device__ __forceinline__ void load(uint32_t row, uint4 (&w)[NL]) const {
     const char *p = base + (uint64_t)row * stride;
 #pragma unroll
-    for (int c = 0; c < NC; ++c) w[c] = *reinterpret_cast<const uint4 *>(p + off[c]);
+    for (int c = 0; c < NL; ++c) w[c] = *reinterpret_cast<const uint4 *>(p + off[c]);
+  }
+  // rows named by one lane each, `from` on
+  __device__ __forceinline__ void load16(uint32_t rows, int from, Rows16<NL> &w) const {
+    const int r = ((int)threadIdx.x % 32) / 8;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) load(__shfl_sync(0xffffffffu, rows, from + 4 * j + r), w.w[j]);
   }
   // the vector, zero where there are no columns
-  __device__ __forceinline__ void vector(uint32_t row, int cols, uint4 (&w)[NC]) const {
+  __device__ __forceinline__ void vector(uint32_t row, int cols, uint4 (&w)[NL]) const {
     load(row, w);
     if (!FULL) {
-      const int q = (int)threadIdx.x % 4;
+      const int s = (int)threadIdx.x % 8;
 #pragma unroll
-      for (int c = 0; c < NC; ++c)
-        if (32 * c + 8 * q >= cols) w[c] = make_uint4(0, 0, 0, 0);
+      for (int c = 0; c < NL; ++c)
+        if (64 * c + 8 * s >= cols) w[c] = make_uint4(0, 0, 0, 0);
     }
   }
 };
@@ -95,67 +102,71 @@ __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// <row g, v> and <row g + 8, v>
-template <int NC>
-__device__ __forceinline__ float2 dots16(const Rows16<NC> &r, const uint4 (&v)[NC]) {
-  float d[4] = {0.f, 0.f, 0.f, 0.f};
+// l[j] = <row 4 j + r, v>
+template <int NL>
+__device__ __forceinline__ void dots16(const Rows16<NL> &r, const uint4 (&v)[NL], float (&l)[4]) {
+  const bool odd = threadIdx.x & 4;
 #pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    mma16816(d, r.w[0][c].x, r.w[1][c].x, r.w[0][c].y, r.w[1][c].y, v[c].x, v[c].y);
-    mma16816(d, r.w[0][c].z, r.w[1][c].z, r.w[0][c].w, r.w[1][c].w, v[c].z, v[c].w);
+  for (int j = 0; j < 4; j += 2) {
+    float d[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < NL; ++c) {
+      mma16816(d, r.w[j][c].x, r.w[j + 1][c].x, r.w[j][c].y, r.w[j + 1][c].y, v[c].x, v[c].y);
+      mma16816(d, r.w[j][c].z, r.w[j + 1][c].z, r.w[j][c].w, r.w[j + 1][c].w, v[c].z, v[c].w);
+    }
+    l[j] = odd ? d[1] : d[0];
+    l[j + 1] = odd ? d[3] : d[2];
   }
-  return make_float2(d[0], d[2]);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) l[j] += __shfl_xor_sync(0xffffffffu, l[j], 4);
 }
-// acc += p.x * row g + p.y * row g + 8, in single precision (the weights keep their 24 bits)
-template <int NC>
-__device__ __forceinline__ void weigh16(const Rows16<NC> &r, float2 p, float2 (&acc)[NC][4]) {
+// acc += sum_j p[j] * row 4 j + r, in single precision (the weights keep their 24 bits)
+template <int NL>
+__device__ __forceinline__ void weigh16(const Rows16<NL> &r, const float (&p)[4], float2 (&acc)[NL][4]) {
 #pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const float2 pp = k ? make_float2(p.y, p.y) : make_float2(p.x, p.x);
+  for (int j = 0; j < 4; ++j) {
+    const float2 pp = make_float2(p[j], p[j]);
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      const uint32_t x[4] = {r.w[k][c].x, r.w[k][c].y, r.w[k][c].z, r.w[k][c].w};
+    for (int c = 0; c < NL; ++c) {
+      const uint32_t x[4] = {r.w[j][c].x, r.w[j][c].y, r.w[j][c].z, r.w[j][c].w};
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         acc[c][i] = fma2(pp, make_float2(__uint_as_float(x[i] << 16), __uint_as_float(x[i] & 0xffff0000u)), acc[c][i]);
     }
   }
 }
-// The sum over the 8 quads, scattered: lane 4 g + q is left with column 32 c + 8 q + g of every chunk c.
-template <int NC>
-__device__ __forceinline__ void scatter16(const float2 (&acc)[NC][4], float (&out)[NC]) {
-  const int g = ((int)threadIdx.x % 32) / 4;
+// The sum over the four groups of 8 lanes, scattered: lane 8 r + s is left with the columns 64 c + 8 s + 2 r and the next.
+template <int NL>
+__device__ __forceinline__ void scatter16(const float2 (&acc)[NL][4], float2 (&out)[NL]) {
+  const bool hi = threadIdx.x & 16, mid = threadIdx.x & 8;
+  auto exchange = [](float2 keep, float2 give, int o) {
+    return make_float2(keep.x + __shfl_xor_sync(0xffffffffu, give.x, o), keep.y + __shfl_xor_sync(0xffffffffu, give.y, o));
+  };
 #pragma unroll
-  for (int c = 0; c < NC; ++c) {
-    float v[8], a[4], b[2];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[2 * i] = acc[c][i].x, v[2 * i + 1] = acc[c][i].y;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      a[i] = (g & 4 ? v[i + 4] : v[i]) + __shfl_xor_sync(0xffffffffu, g & 4 ? v[i] : v[i + 4], 16);
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-      b[i] = (g & 2 ? a[i + 2] : a[i]) + __shfl_xor_sync(0xffffffffu, g & 2 ? a[i] : a[i + 2], 8);
-    out[c] = (g & 1 ? b[1] : b[0]) + __shfl_xor_sync(0xffffffffu, g & 1 ? b[0] : b[1], 4);
+  for (int c = 0; c < NL; ++c) {
+    const float2 a = exchange(hi ? acc[c][2] : acc[c][0], hi ? acc[c][0] : acc[c][2], 16);
+    const float2 b = exchange(hi ? acc[c][3] : acc[c][1], hi ? acc[c][1] : acc[c][3], 16);
+    out[c] = exchange(mid ? b : a, mid ? a : b, 8);
   }
 }
-// Chunks of 32 columns where the matrix units take the rows (bf16, 16-byte aligned rows of up to 128 columns less than 4 GiB
+// the first of the two columns
+__device__ __forceinline__ int scattered_column(int c) { return 64 * c + 8 * ((int)threadIdx.x % 8) + 2 * (((int)threadIdx.x % 32) / 8); }
+// Lines of 64 columns where the matrix units take the rows (bf16, 16-byte aligned rows of up to 128 columns less than 4 GiB
 // apart), else 0.
-inline int mma_chunks(const Args &a, int dtype, int width) {
+inline int mma_lines(const Args &a, int dtype, int width) {
   if (dtype != BLOSSOM_DTYPE_BF16 || width != 8 || a.cols > 128 || a.sh > 0x7fffffffLL || a.st > 0x7fffffffLL) return 0;
-  return a.cols <= 32 ? 1 : a.cols <= 64 ? 2 : 4;
+  return a.cols <= 64 ? 1 : 2;
 }
-// f(chunks, all of their columns are there)
+// f(lines, all of their columns are there)
 template <typename F>
-inline void with_chunks(int nc, int cols, F &&f) {
+inline void with_lines(int lines, int cols, F &&f) {
   using std::integral_constant;
   auto full = [&](auto n) {
-    if (cols == 32 * decltype(n)::value) f(n, integral_constant<bool, true>());
+    if (cols == 64 * decltype(n)::value) f(n, integral_constant<bool, true>());
     else f(n, integral_constant<bool, false>());
   };
-  if (nc == 1) full(integral_constant<int, 1>());
-  else if (nc == 2) full(integral_constant<int, 2>());
-  else full(integral_constant<int, 4>());
+  if (lines == 1) full(integral_constant<int, 1>());
+  else full(integral_constant<int, 2>());
 }
 
 // Device scratch; the forward uses `sums` alone.

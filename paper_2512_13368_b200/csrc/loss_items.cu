@@ -304,19 +304,19 @@ __global__ void __launch_bounds__(kThreads) loss_items_kernel(Args a, const T *_
 
 // The same on the matrix units: a warp walks a chunk 16 entries at a time, their hidden rows the first operand, the item's
 // row the second; the next 16 rows are under way meanwhile.  Sixteen entries of more than one item go through once an item.
-template <int NC, bool FULL>
-__global__ void __launch_bounds__(kMmaThreads, NC == 1 ? 8 : NC == 2 ? 5 : 3)
+template <int NL, bool FULL>
+__global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 6 : 3)
     loss_items_mma_kernel(Args a, const __nv_bfloat16 *__restrict__ hidden, const __nv_bfloat16 *__restrict__ table,
                           const float *__restrict__ lse, const float *__restrict__ grad_loss, const uint32_t *__restrict__ keys,
                           const uint32_t *__restrict__ vals, uint32_t entries, int chunk, __nv_bfloat16 *__restrict__ dtable,
                           float *__restrict__ part, uint32_t *__restrict__ range) {
   grid_chain_enter();
-  const int lane = (int)threadIdx.x % 32, g = lane / 4, q = lane % 4;
+  const int lane = (int)threadIdx.x % 32, group = lane / 8;
   const int64_t c0 = (int64_t)blockIdx.x * (kMmaThreads / 32) + threadIdx.x / 32;
   if (c0 * chunk >= entries) return;
   const uint32_t none = (uint32_t)a.items, s = (uint32_t)(c0 * chunk);
   const uint32_t e = entries - s < (uint32_t)chunk ? entries : s + (uint32_t)chunk;
-  const Lanes16<NC, FULL> from_hidden(hidden, a.sh, a.cols), from_table(table, a.st, a.cols);
+  const Lanes16<NL, FULL> from_hidden(hidden, a.sh, a.cols), from_table(table, a.st, a.cols);
   struct Entries {  // 32 of them, one a lane; what lies behind the chunk is no candidate of the first position
     uint32_t key, val;
     float top;
@@ -329,32 +329,28 @@ __global__ void __launch_bounds__(kMmaThreads, NC == 1 ? 8 : NC == 2 ? 5 : 3)
     }
     return x;
   };
-  auto load = [&](const Entries &x, int half, Rows16<NC> &h) {
-    from_hidden.load(__shfl_sync(0xffffffffu, x.val, half + g) & 0x7fffffffu, h.w[0]);
-    from_hidden.load(__shfl_sync(0xffffffffu, x.val, half + g + 8) & 0x7fffffffu, h.w[1]);
-  };
-  uint4 w[NC];
-  float2 acc[NC][4];
+  uint4 w[NL];
+  float2 acc[NL][4];
   uint32_t cur = keys[s], before = s > 0 ? keys[s - 1] : 0xffffffffu;
   bool open = before == cur, first = true;  // open: the item's entries began in a chunk before
   auto begin = [&](uint32_t item) {
     cur = item;
     from_table.vector(item, a.cols, w);
 #pragma unroll
-    for (int c = 0; c < NC; ++c)
+    for (int c = 0; c < NL; ++c)
 #pragma unroll
       for (int i = 0; i < 4; ++i) acc[c][i] = make_float2(0.f, 0.f);
   };
   auto finish = [&](bool whole) {
-    float sum[NC];
-    scatter16<NC>(acc, sum);
+    float2 sum[NL];
+    scatter16<NL>(acc, sum);
     const float scale = whole ? grad_scale(a, lse, grad_loss) : 1.f;
 #pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      const int col = 32 * c + 8 * q + g;
-      if (col >= a.cols) continue;
-      if (whole) dtable[cur * a.sdt + col] = __float2bfloat16(sum[c] * scale);
-      else part[(c0 * 2 + (first ? 0 : 1)) * a.cols + col] = sum[c];
+    for (int c = 0; c < NL; ++c) {
+      const int col = scattered_column(c);
+      if (!FULL && col >= a.cols) continue;
+      if (whole) *reinterpret_cast<uint32_t *>(dtable + cur * a.sdt + col) = rows::pack2(sum[c].x * scale, sum[c].y * scale);
+      else *reinterpret_cast<float2 *>(part + (c0 * 2 + (first ? 0 : 1)) * a.cols + col) = sum[c];
     }
   };
   // where items start and end, from 32 entries and the key before them
@@ -370,29 +366,32 @@ __global__ void __launch_bounds__(kMmaThreads, NC == 1 ? 8 : NC == 2 ? 5 : 3)
     }
     before = __shfl_sync(0xffffffffu, x.key, 31);
   };
-  auto walk = [&](const Rows16<NC> &h, const Entries &x, int half) {
-    const float2 top = make_float2(__shfl_sync(0xffffffffu, x.top, half + g), __shfl_sync(0xffffffffu, x.top, half + g + 8));
-    const uint32_t targets = __ballot_sync(0xffffffffu, x.val >> 31) >> half;
+  auto walk = [&](const Rows16<NL> &h, const Entries &x, int half) {
+    float top[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) top[j] = __shfl_sync(0xffffffffu, x.top, half + 4 * j + group);
+    const uint32_t targets = __ballot_sync(0xffffffffu, x.val >> 31) >> (half + group);
     for (;;) {
-      const float2 l = dots16<NC>(h, w);
-      float2 p;
-      p.x = exp2f(l.x * kLog2e - top.x) - (targets >> g & 1 ? 1.f : 0.f);
-      p.y = exp2f(l.y * kLog2e - top.y) - (targets >> g & 0x100 ? 1.f : 0.f);
-      const uint32_t others = __ballot_sync(0xffffffffu, x.key != cur) >> half;
-      if (!(others & 0xffffu)) {
-        weigh16<NC>(h, p, acc);
+      float p[4];
+      dots16<NL>(h, w, p);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) p[j] = exp2f(p[j] * kLog2e - top[j]) - (targets >> (4 * j) & 1 ? 1.f : 0.f);
+      uint32_t others = __ballot_sync(0xffffffffu, x.key != cur) >> half & 0xffffu;
+      if (!others) {
+        weigh16<NL>(h, p, acc);
         return;
       }
       // (a weight of zero would not do: another item's row may hold what is no number)
-      Rows16<NC> own = h;
+      others >>= group;
+      Rows16<NL> own = h;
 #pragma unroll
-      for (int k = 0; k < 2; ++k)
-        if (others >> (g + 8 * k) & 1) {
-          (k ? p.y : p.x) = 0.f;
+      for (int j = 0; j < 4; ++j)
+        if (others >> (4 * j) & 1) {
+          p[j] = 0.f;
 #pragma unroll
-          for (int c = 0; c < NC; ++c) own.w[k][c] = make_uint4(0, 0, 0, 0);
+          for (int c = 0; c < NL; ++c) own.w[j][c] = make_uint4(0, 0, 0, 0);
         }
-      weigh16<NC>(own, p, acc);
+      weigh16<NL>(own, p, acc);
       // the next item among the 16, if there is one (they are sorted)
       const uint32_t later = __ballot_sync(0xffffffffu, (lane & 16) == half && x.key > cur && x.key < none);
       if (!later) return;
@@ -405,17 +404,17 @@ __global__ void __launch_bounds__(kMmaThreads, NC == 1 ? 8 : NC == 2 ? 5 : 3)
   mark(x, s);
   if (cur >= none) return;
   begin(cur);
-  Rows16<NC> h[2];
-  load(x, 0, h[0]);
+  Rows16<NL> h[2];
+  from_hidden.load16(x.val & 0x7fffffffu, 0, h[0]);
   for (uint32_t i = s; i < e; i += 32) {
     const bool second = i + 16 < e, third = i + 32 < e;
     Entries next = {none, 0, 0.f};
     if (third) next = entries_from(i + 32);
-    if (second) load(x, 16, h[1]);
+    if (second) from_hidden.load16(x.val & 0x7fffffffu, 16, h[1]);
     walk(h[0], x, 0);
     if (third) {
       mark(next, i + 32);
-      load(next, 0, h[0]);
+      from_hidden.load16(next.val & 0x7fffffffu, 0, h[0]);
     }
     if (second) walk(h[1], x, 16);
     x = next;
@@ -554,8 +553,8 @@ Scratch carve(const Args &a, void *base) {
 
 int launch_items(const Args &a, int dtype, const void *hidden, const void *table, const float *lse, const float *grad_loss,
                  void *dtable, int width, const Scratch &s, cudaStream_t st) {
-  const int nc = mma_chunks(a, dtype, width);
-  const SortPlan p = sort_plan(a, nc ? 32 : lanes_of(a.groups));
+  const int lines = mma_lines(a, dtype, width);
+  const SortPlan p = sort_plan(a, lines ? 32 : lanes_of(a.groups));
   const uint32_t entries = (uint32_t)p.entries;
   const Split by = split_by((uint32_t)a.n + 1);
   int at = 1;  // the buffer that holds the list
@@ -581,11 +580,11 @@ int launch_items(const Args &a, int dtype, const void *hidden, const void *table
     at = to;
   }
   const uint32_t *keys = s.keys[at], *vals = s.vals[at];
-  if (entries && nc) {
-    with_chunks(nc, a.cols, [&](auto chunks, auto all) {
-      constexpr int NC = decltype(chunks)::value, per = kMmaThreads / 32;
+  if (entries && lines) {
+    with_lines(lines, a.cols, [&](auto n, auto all) {
+      constexpr int NL = decltype(n)::value, per = kMmaThreads / 32;
       LaunchScope ls(K_LOSS_ITEMS, st);
-      launch_chained(loss_items_mma_kernel<NC, decltype(all)::value>, dim3((unsigned)((p.chunks + per - 1) / per)), dim3(kMmaThreads), 0, st,
+      launch_chained(loss_items_mma_kernel<NL, decltype(all)::value>, dim3((unsigned)((p.chunks + per - 1) / per)), dim3(kMmaThreads), 0, st,
                      a, static_cast<const __nv_bfloat16 *>(hidden), static_cast<const __nv_bfloat16 *>(table), lse, grad_loss,
                      keys, vals, entries, p.chunk, static_cast<__nv_bfloat16 *>(dtable), s.part, s.range);
     });
@@ -595,7 +594,7 @@ int launch_items(const Args &a, int dtype, const void *hidden, const void *table
     rows::with_type(dtype, width, [&](auto t, auto w) {
       using T = decltype(t);
       constexpr int W = decltype(w)::value, per = kThreads / P::LPC;
-      if (entries && !nc) {
+      if (entries && !lines) {
         LaunchScope ls(K_LOSS_ITEMS, st);
         launch_chained(loss_items_kernel<T, W, P>, dim3((unsigned)((p.chunks + per - 1) / per)), dim3(kThreads), 0, st, a,
                        static_cast<const T *>(hidden), static_cast<const T *>(table), lse, grad_loss, keys, vals, entries,

@@ -145,85 +145,86 @@ __global__ void __launch_bounds__(kThreads) loss_rows_kernel(Args a, const T *__
 
 // The same on the matrix units: a warp scores 16 candidates at a time, the next 16 rows are under way meanwhile.  What is no
 // candidate is read as the target's row and weighs nothing.
-template <int NC, bool FULL, bool GRAD>
-__global__ void __launch_bounds__(kMmaThreads, NC == 1 ? 8 : NC == 2 ? 5 : 3)
+template <int NL, bool FULL, bool GRAD>
+__global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 6 : 4)
     loss_rows_mma_kernel(Args a, const __nv_bfloat16 *__restrict__ hidden, const __nv_bfloat16 *__restrict__ table,
                          float *__restrict__ lse, float *__restrict__ dh, double2 *__restrict__ sums) {
   __shared__ double2 warp_sums[kMmaThreads / 32];
   grid_chain_enter();
-  const int lane = (int)threadIdx.x % 32, warp = (int)threadIdx.x / 32, g = lane / 4, q = lane % 4;
-  const Lanes16<NC, FULL> from_hidden(hidden, a.sh, a.cols), from_table(table, a.st, a.cols);
+  const int lane = (int)threadIdx.x % 32, warp = (int)threadIdx.x / 32, group = lane / 8;
+  const Lanes16<NL, FULL> from_hidden(hidden, a.sh, a.cols), from_table(table, a.st, a.cols);
   double2 mine = make_double2(0.0, 0.0);
   for (int64_t r = (int64_t)blockIdx.x * (kMmaThreads / 32) + warp; r < a.rows; r += (int64_t)gridDim.x * (kMmaThreads / 32)) {
     const int row = (int)r, target = row_target(a, row);
-    float row_lse = 0.f, grad[NC];
+    float row_lse = 0.f;
+    float2 grad[NL];
 #pragma unroll
-    for (int c = 0; c < NC; ++c) grad[c] = 0.f;
+    for (int c = 0; c < NL; ++c) grad[c] = make_float2(0.f, 0.f);
     if (target >= 0) {
-      uint4 h[NC];
+      uint4 h[NL];
       from_hidden.vector((uint32_t)row, a.cols, h);
-      float2 acc[NC][4];
+      float2 acc[NL][4];
 #pragma unroll
-      for (int c = 0; c < NC; ++c)
+      for (int c = 0; c < NL; ++c)
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[c][i] = make_float2(0.f, 0.f);
       // candidates c0 .. c0 + 31, one a lane; there: a bit for each
       auto ids_from = [&](int c0, uint32_t &there) {
         const int id = c0 + lane <= a.n ? candidate(a, row, target, c0 + lane) : -1;
         there = __ballot_sync(0xffffffffu, id >= 0);
-        return id >= 0 ? id : target;
+        return (uint32_t)(id >= 0 ? id : target);
       };
-      auto load = [&](int ids, int half, Rows16<NC> &w) {
-        from_table.load((uint32_t)__shfl_sync(0xffffffffu, ids, half + g), w.w[0]);
-        from_table.load((uint32_t)__shfl_sync(0xffffffffu, ids, half + g + 8), w.w[1]);
-      };
-      float top = -FLT_MAX, total = 0.f, own = 0.f;  // of a quad: its two rows of every 16
-      auto score = [&](const Rows16<NC> &w, uint32_t there) {
-        float2 l = dots16<NC>(w, h);
-        l.x = there >> g & 1 ? l.x * kLog2e : -INFINITY;  // in units of log 2
-        l.y = there >> g & 0x100 ? l.y * kLog2e : -INFINITY;
+      float top = -FLT_MAX, total = 0.f, own = 0.f;  // of a group of lanes: its four rows of every 16
+      auto score = [&](const Rows16<NL> &w, uint32_t there) {
+        float l[4], high = top;
+        dots16<NL>(w, h, l);
+        const float first = l[0];
+        there >>= group;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          l[j] = there >> (4 * j) & 1 ? l[j] * kLog2e : -INFINITY;  // in units of log 2
+          high = fmaxf(high, l[j]);
+        }
         // The reference point only moves if it has to by more than 2^10: the sums stay far from the type's limits, and their
         // relative rounding does not depend on it.
-        const float high = fmaxf(top, fmaxf(l.x, l.y));
         if (high > top + 10.f) {
           const float shrink = exp2f(top - high);
           total *= shrink;
           if (GRAD) {
 #pragma unroll
-            for (int c = 0; c < NC; ++c)
+            for (int c = 0; c < NL; ++c)
 #pragma unroll
               for (int i = 0; i < 4; ++i) acc[c][i].x *= shrink, acc[c][i].y *= shrink;
           }
           top = high;
         }
-        const float2 p = make_float2(exp2f(l.x - top), exp2f(l.y - top));
-        total += p.x + p.y;
-        if (GRAD) weigh16<NC>(w, p, acc);
-        return l.x;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) l[j] = exp2f(l[j] - top);
+        total += (l[0] + l[1]) + (l[2] + l[3]);
+        if (GRAD) weigh16<NL>(w, l, acc);
+        return first;
       };
-      Rows16<NC> w[2];
-      uint32_t there, there_next = 0;
-      int ids = ids_from(0, there);
-      load(ids, 0, w[0]);
+      Rows16<NL> w[2];
+      uint32_t there, there_next = 0, ids = ids_from(0, there), next = 0;
+      from_table.load16(ids, 0, w[0]);
       for (int c0 = 0; c0 <= a.n; c0 += 32) {
         const bool second = c0 + 16 <= a.n, third = c0 + 32 <= a.n;
-        int next = target;
         if (third) next = ids_from(c0 + 32, there_next);
-        if (second) load(ids, 16, w[1]);
+        if (second) from_table.load16(ids, 16, w[1]);
         const float first = score(w[0], there);
-        if (c0 == 0) own = __shfl_sync(0xffffffffu, first, 0);
-        if (third) load(next, 0, w[0]);
+        if (c0 == 0) own = __shfl_sync(0xffffffffu, first, 0) * kLog2e;
+        if (third) from_table.load16(next, 0, w[0]);
         if (second) score(w[1], there >> 16);
         ids = next;
         there = there_next;
       }
       float high = top;
 #pragma unroll
-      for (int o = 4; o < 32; o <<= 1) high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, o));
-      const float weight = exp2f(top - high);  // (0 for a quad that met no candidate)
+      for (int o = 8; o < 32; o <<= 1) high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, o));
+      const float weight = exp2f(top - high);  // (0 for a group that met no candidate)
       total *= weight;
 #pragma unroll
-      for (int o = 4; o < 32; o <<= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+      for (int o = 8; o < 32; o <<= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
       const float lse2 = high + log2f(total);
       row_lse = lse2 * kLn2;
       mine.x += (double)((lse2 - own) * kLn2);
@@ -231,23 +232,26 @@ __global__ void __launch_bounds__(kMmaThreads, NC == 1 ? 8 : NC == 2 ? 5 : 3)
       if (GRAD) {
         const float inv = weight / total;
 #pragma unroll
-        for (int c = 0; c < NC; ++c)
+        for (int c = 0; c < NL; ++c)
 #pragma unroll
           for (int i = 0; i < 4; ++i) acc[c][i].x *= inv, acc[c][i].y *= inv;
-        scatter16<NC>(acc, grad);
+        scatter16<NL>(acc, grad);
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-          const int col = 32 * c + 8 * q + g;
-          if (col < a.cols) grad[c] -= __bfloat162float(table[target * a.st + col]);
+        for (int c = 0; c < NL; ++c) {
+          const int col = scattered_column(c);
+          if (FULL || col < a.cols) {
+            const uint32_t w = *reinterpret_cast<const uint32_t *>(table + target * a.st + col);
+            grad[c].x -= __uint_as_float(w << 16), grad[c].y -= __uint_as_float(w & 0xffff0000u);
+          }
         }
       }
     }
     if (lane == 0) lse[row] = row_lse;
     if (GRAD) {
 #pragma unroll
-      for (int c = 0; c < NC; ++c) {
-        const int col = 32 * c + 8 * q + g;
-        if (col < a.cols) dh[(int64_t)row * a.cols + col] = grad[c];
+      for (int c = 0; c < NL; ++c) {
+        const int col = scattered_column(c);
+        if (FULL || col < a.cols) *reinterpret_cast<float2 *>(dh + (int64_t)row * a.cols + col) = grad[c];
       }
     }
   }
@@ -359,17 +363,17 @@ extern "C" int blossom_sampled_loss_fwd(const blossom_loss_params *params, const
   rows::Alignment al;
   al.rows_at(hidden, a.sh, esz);
   al.rows_at(table, a.st, esz);
-  const int width = al.elements(a.cols, esz), nc = loss::mma_chunks(a, params->dtype, width);
-  const int warps = (nc ? loss::kMmaThreads : loss::kThreads) / 32;  // a row each
+  const int width = al.elements(a.cols, esz), lines = loss::mma_lines(a, params->dtype, width);
+  const int warps = (lines ? loss::kMmaThreads : loss::kThreads) / 32;  // a row each
   const int64_t want = ((int64_t)a.rows + warps - 1) / warps, most = loss::kSMs * 64 / warps;
   const int ctas = (int)(want < most ? want : most);
   if (ctas) {
     LaunchScope ls(K_LOSS_ROWS, st);
-    if (nc) {
-      loss::with_chunks(nc, a.cols, [&](auto chunks, auto all) {
-        constexpr int NC = decltype(chunks)::value;
+    if (lines) {
+      loss::with_lines(lines, a.cols, [&](auto n, auto all) {
+        constexpr int NL = decltype(n)::value;
         constexpr bool FULL = decltype(all)::value;
-        launch_chained(grad_hidden ? loss::loss_rows_mma_kernel<NC, FULL, true> : loss::loss_rows_mma_kernel<NC, FULL, false>,
+        launch_chained(grad_hidden ? loss::loss_rows_mma_kernel<NL, FULL, true> : loss::loss_rows_mma_kernel<NL, FULL, false>,
                        dim3((unsigned)ctas), dim3(loss::kMmaThreads), 0, st, a, static_cast<const __nv_bfloat16 *>(hidden),
                        static_cast<const __nv_bfloat16 *>(table), lse, grad_hidden, sums);
       });
