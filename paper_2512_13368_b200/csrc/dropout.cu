@@ -25,9 +25,11 @@ int check(const blossom_rows_params *p, int max_cols, const int64_t *rng, Args *
   a->cols = p->cols;
   a->groups = (p->cols + 7) / 8;
   a->sx = st[0], a->sr = st[1], a->so = st[2], a->sdx = st[3], a->sdr = st[4];
-  a->bar = (unsigned)floor(p->dropout * 65536.0 + 0.5);
+  const double bar = floor(p->dropout * 65536.0 + 0.5);  // of 65536
+  a->drop = bar == 0.0 ? 0 : bar < 65536.0 ? 1 : 2;
+  a->bar = a->drop == 1 ? (unsigned)bar << 16 : 0;
   a->site = (unsigned)p->site;
-  a->scale = a->bar < 65536u ? (float)(65536.0 / (65536.0 - a->bar)) : 0.f;
+  a->scale = a->drop == 0 ? 1.f : a->drop == 1 ? (float)(65536.0 / (65536.0 - bar)) : 0.f;
   a->eps = (float)p->eps;
   a->inv_cols = 1.f / (float)p->cols;
   a->wide_weights = p->weight_dtype == BLOSSOM_DTYPE_FP32;
@@ -36,25 +38,41 @@ int check(const blossom_rows_params *p, int max_cols, const int64_t *rng, Args *
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kRowsInFlight = 2;  // rows a thread loads before it works on the first
 
-// A thread takes groups of 8 columns, one after another, in the order of the rows.
-template <typename T, int W>
-__global__ void __launch_bounds__(kThreads) dropout_kernel(Args a, const T *x, const int64_t *rng, T *out) {
+template <typename T, int W, typename P>
+__global__ void __launch_bounds__(P::threads) dropout_kernel(Args a, const T *x, const int64_t *rng, T *out) {
+  constexpr int U = kRowsInFlight, V = P::V;
   grid_chain_enter();
   Generator gen;
-  if (a.bar) gen.read(rng);
-  const int64_t total = (int64_t)a.rows * a.groups, step = (int64_t)gridDim.x * kThreads;
-  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += step) {
-    const int row = (int)(i / a.groups), g = (int)(i - (int64_t)row * a.groups), valid = a.cols - 8 * g;
-    float v[8];
-    load_group<T, W>(x + row * a.sx + 8 * g, valid, v);
-    if (a.bar) {
-      const uint32_t m = gen.kept(a, row, g);
+  if (a.drop == 1) gen.read(rng);
+  const int lane = (int)threadIdx.x % P::TPR;
+  const uint32_t rows = (uint32_t)a.rows, step = gridDim.x * (uint32_t)P::slots;
+  uint32_t row = blockIdx.x * (uint32_t)P::slots + threadIdx.x / P::TPR;
+  const T *px = x + row * a.sx + 8 * lane;
+  T *po = out + row * a.so + 8 * lane;
+  for (; row < rows; row += U * step, px += U * step * a.sx, po += U * step * a.so) {
+    Raw<T, W> v[U][V];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = m >> j & 1 ? v[j] * a.scale : 0.f;
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int k = 0; k < V; ++k)
+        v[u][k].load(px + u * step * a.sx + 8 * k * P::TPR, row + u * step < rows ? a.cols - 8 * (lane + k * P::TPR) : 0);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (row + u * step >= rows) break;
+#pragma unroll
+      for (int k = 0; k < V; ++k) {
+        const int g = lane + k * P::TPR;
+        Group z = v[u][k].get();
+        if (a.drop) {
+          if (a.drop == 1) drop(a, gen.bits(a, (int)(row + u * step), g), z);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) z.p[i] = a.drop == 1 ? mul2(z.p[i], both(a.scale)) : both(0.f);
+        }
+        store_group<T, W>(po + u * step * a.so + 8 * k * P::TPR, a.cols - 8 * g, z);
+      }
     }
-    store_group<T, W>(out + row * a.so + 8 * g, valid, v);
   }
 }
 
@@ -75,12 +93,16 @@ extern "C" int blossom_dropout(const blossom_rows_params *params, const void *x,
   rows::Alignment al;
   al.rows_at(x, a.sx, esz);
   al.rows_at(out, a.so, esz);
-  const int64_t ctas = ((int64_t)a.rows * a.groups + rows::kThreads - 1) / rows::kThreads, most = rows::kSMs * 8;
-  rows::with_type(params->dtype, al.elements(a.cols, esz), [&](auto t, auto w) {
-    using T = decltype(t);
-    LaunchScope ls(K_DROPOUT, (cudaStream_t)stream);
-    launch_chained(rows::dropout_kernel<T, decltype(w)::value>, dim3((unsigned)(ctas < most ? ctas : most)),
-                   dim3(rows::kThreads), 0, (cudaStream_t)stream, a, static_cast<const T *>(x), rng, static_cast<T *>(out));
+  rows::with_plan<2>(a.groups, [&](auto plan) {
+    using P = decltype(plan);
+    rows::with_type(params->dtype, al.elements(a.cols, esz), [&](auto t, auto w) {
+      using T = decltype(t);
+      const int64_t per = P::slots * rows::kRowsInFlight, ctas = (a.rows + per - 1) / per;
+      const int64_t most = rows::kSMs * (2048 / P::threads);
+      LaunchScope ls(K_DROPOUT, (cudaStream_t)stream);
+      launch_chained(rows::dropout_kernel<T, decltype(w)::value, P>, dim3((unsigned)(ctas < most ? ctas : most)),
+                     dim3(P::threads), 0, (cudaStream_t)stream, a, static_cast<const T *>(x), rng, static_cast<T *>(out));
+    });
   });
   return cudaGetLastError() == cudaSuccess ? BLOSSOM_OK : BLOSSOM_ERR_CUDA;
 }

@@ -6,7 +6,10 @@ namespace blossom {
 namespace loss {
 
 using rows::kSMs;
+using rows::both;
+using rows::Group;
 using rows::load_group;
+using rows::mul2;
 using rows::store_group;
 
 constexpr int kMaxCols = 1024, kMaxRowCtas = kSMs * 16, kMmaThreads = 128;
@@ -32,6 +35,18 @@ __device__ __forceinline__ int candidate(const Args &a, int row, int target, int
   if (j == 0) return target;
   const int64_t i = load_id(a.negatives, row * a.sn + (j - 1), a.idx8);
   return i >= 0 && i < a.items && !(a.hits && i == target) ? (int)i : -1;
+}
+
+// the lane's share of <a, b>
+template <int V>
+__device__ __forceinline__ float dot(const Group (&a)[V], const Group (&b)[V]) {
+  float2 s[2] = {both(0.f), both(0.f)};
+#pragma unroll
+  for (int v = 0; v < V; ++v)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[i & 1] = fma2(a[v].p[i], b[v].p[i], s[i & 1]);
+  const float2 t = add2(s[0], s[1]);
+  return t.x + t.y;
 }
 
 // LPC lanes hold a row, V groups of 8 columns each

@@ -228,15 +228,15 @@ __global__ void __launch_bounds__(kThreads) loss_items_kernel(Args a, const T *_
   uint32_t cur = keys[s];
   bool open = s > 0 && keys[s - 1] == cur;  // the item's entries began in a chunk before
   bool first = true;
-  float w[V][8], acc[V][8];
+  Group w[V], acc[V];
   auto begin = [&](uint32_t item) {
     cur = item;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const int g = col + v * LPC;
-      load_group<T, W>(table + cur * a.st + 8 * g, a.cols - 8 * g, w[v]);
+      w[v] = load_group<T, W>(table + cur * a.st + 8 * g, a.cols - 8 * g);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) acc[v][i] = 0.f, w[v][i] *= kLog2e;
+      for (int i = 0; i < 4; ++i) acc[v].p[i] = both(0.f), w[v].p[i] = mul2(w[v].p[i], both(kLog2e));
     }
   };
   auto finish = [&](bool whole) {
@@ -245,7 +245,7 @@ __global__ void __launch_bounds__(kThreads) loss_items_kernel(Args a, const T *_
       const int g = col + v * LPC, valid = a.cols - 8 * g;
       if (whole) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) acc[v][i] *= scale;
+        for (int i = 0; i < 4; ++i) acc[v].p[i] = mul2(acc[v].p[i], both(scale));
         store_group<T, W>(dtable + cur * a.sdt + 8 * g, valid, acc[v]);
       } else {
         store_group<float, (W < 4 ? W : 4)>(part + (c * 2 + (first ? 0 : 1)) * a.cols + 8 * g, valid, acc[v]);
@@ -259,7 +259,8 @@ __global__ void __launch_bounds__(kThreads) loss_items_kernel(Args a, const T *_
   begin(cur);
   for (uint32_t i = s; i < e; i += U) {
     uint32_t key[U], val[U];
-    float h[U][V][8], top[U];
+    Group h[U][V];
+    float top[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       key[u] = i + u < e ? keys[i + u] : (uint32_t)a.items;
@@ -270,7 +271,7 @@ __global__ void __launch_bounds__(kThreads) loss_items_kernel(Args a, const T *_
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         const int g = col + v * LPC;
-        load_group<T, W>(hidden + t * a.sh + 8 * g, there ? a.cols - 8 * g : 0, h[u][v]);
+        h[u][v] = load_group<T, W>(hidden + t * a.sh + 8 * g, there ? a.cols - 8 * g : 0);
       }
     }
 #pragma unroll
@@ -284,18 +285,14 @@ __global__ void __launch_bounds__(kThreads) loss_items_kernel(Args a, const T *_
         if (writer) range[key[u]] = i + u;
         begin(key[u]);
       }
-      float l = 0.f;
-#pragma unroll
-      for (int v = 0; v < V; ++v)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) l += w[v][j] * h[u][v][j];
+      float l = dot<V>(w, h[u]);
 #pragma unroll
       for (int o = 1; o < LPC; o <<= 1) l += __shfl_xor_sync(lanes, l, o);
       const float coef = exp2f(l - top[u]) - (val[u] >> 31 ? 1.f : 0.f);
 #pragma unroll
       for (int v = 0; v < V; ++v)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) acc[v][j] += coef * h[u][v][j];
+        for (int j = 0; j < 4; ++j) acc[v].p[j] = fma2(both(coef), h[u][v].p[j], acc[v].p[j]);
     }
   }
   finish(!open && !(e < entries && keys[e] == cur));
@@ -444,36 +441,35 @@ __global__ void __launch_bounds__(kThreads) loss_join_kernel(Args a, const float
   }
   __syncthreads();
   // the sum of every `step`-th chunk of a range, from its `from`-th on
-  auto add_up = [&](uint2 r, uint32_t from, uint32_t step, float (&acc)[V][8]) {
+  auto add_up = [&](uint2 r, uint32_t from, uint32_t step, Group (&acc)[V]) {
     const uint32_t c0 = r.x / (uint32_t)chunk, c1 = (r.y - 1) / (uint32_t)chunk;
 #pragma unroll
     for (int v = 0; v < V; ++v)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) acc[v][i] = 0.f;
+      for (int i = 0; i < 4; ++i) acc[v].p[i] = both(0.f);
 #pragma unroll 4
     for (uint32_t c = c0 + from; c <= c1; c += step) {
       const int64_t slot = (int64_t)c * 2 + (c == c0 && r.x % (uint32_t)chunk ? 1 : 0);
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         const int g = col + v * LPC;
-        float x[8];
-        load_group<float, WF>(part + slot * a.cols + 8 * g, a.cols - 8 * g, x);
+        const Group x = load_group<float, WF>(part + slot * a.cols + 8 * g, a.cols - 8 * g);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) acc[v][i] += x[i];
+        for (int i = 0; i < 4; ++i) acc[v].p[i] = add2(acc[v].p[i], x.p[i]);
       }
     }
   };
   auto chunks_of = [&](uint2 r) { return r.x == r.y ? 0u : (r.y - 1) / (uint32_t)chunk - r.x / (uint32_t)chunk + 1; };
-  auto write = [&](int64_t to, float (&acc)[V][8]) {
+  auto write = [&](int64_t to, Group (&acc)[V]) {
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const int g = col + v * LPC;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) acc[v][i] *= scale;
+      for (int i = 0; i < 4; ++i) acc[v].p[i] = mul2(acc[v].p[i], both(scale));
       store_group<T, W>(dtable + to * a.sdt + 8 * g, a.cols - 8 * g, acc[v]);
     }
   };
-  float acc[V][8];
+  Group acc[V];
   {
     const uint2 r = range[grp];
     const uint32_t n = chunks_of(r);
@@ -482,7 +478,7 @@ __global__ void __launch_bounds__(kThreads) loss_join_kernel(Args a, const float
 #pragma unroll
         for (int v = 0; v < V; ++v)
 #pragma unroll
-          for (int i = 0; i < 8; ++i) acc[v][i] = 0.f;
+          for (int i = 0; i < 4; ++i) acc[v].p[i] = both(0.f);
       } else {
         add_up(r, 0, 1, acc);
       }
@@ -496,14 +492,14 @@ __global__ void __launch_bounds__(kThreads) loss_join_kernel(Args a, const float
 #pragma unroll
     for (int v = 0; v < V; ++v)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sums[grp][8 * (col + v * LPC) + i] = acc[v][i];
+      for (int i = 0; i < 8; ++i) sums[grp][8 * (col + v * LPC) + i] = acc[v].at(i);
     __syncthreads();
     if (grp == 0) {
       for (int g = 1; g < NG; ++g)
 #pragma unroll
         for (int v = 0; v < V; ++v)
 #pragma unroll
-          for (int i = 0; i < 8; ++i) acc[v][i] += sums[g][8 * (col + v * LPC) + i];
+          for (int i = 0; i < 8; ++i) acc[v].at(i) += sums[g][8 * (col + v * LPC) + i];
       write((int64_t)blockIdx.x * NG + k, acc);
     }
     __syncthreads();

@@ -26,27 +26,28 @@ __global__ void __launch_bounds__(kThreads) loss_rows_kernel(Args a, const T *__
   double2 mine = make_double2(0.0, 0.0);
   for (int64_t r = (int64_t)blockIdx.x * (kThreads / 32) + warp; r < a.rows; r += (int64_t)gridDim.x * (kThreads / 32)) {
     const int row = (int)r, target = row_target(a, row);
-    float acc[V][8];
+    Group acc[V];
 #pragma unroll
     for (int v = 0; v < V; ++v)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) acc[v][i] = 0.f;
+      for (int i = 0; i < 4; ++i) acc[v].p[i] = both(0.f);
     float row_lse = 0.f;
     if (target >= 0) {
-      float h[V][8];
+      Group h[V];
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         const int g = col + v * LPC;
-        load_group<T, W>(hidden + row * a.sh + 8 * g, a.cols - 8 * g, h[v]);
+        h[v] = load_group<T, W>(hidden + row * a.sh + 8 * g, a.cols - 8 * g);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) h[v][i] *= kLog2e;  // logits in units of log 2
+        for (int i = 0; i < 4; ++i) h[v].p[i] = mul2(h[v].p[i], both(kLog2e));  // logits in units of log 2
       }
       float top = -INFINITY, total = 0.f, own = 0.f;
       for (int c0 = 0; c0 <= a.n; c0 += 32) {
         const int id = c0 + lane <= a.n ? candidate(a, row, target, c0 + lane) : -1;
         const int steps = (min(32, a.n + 1 - c0) + CPW - 1) / CPW;
         for (int k = 0; k < steps; k += U) {
-          float w[U][V][8], l[U];
+          Group w[U][V];
+          float l[U];
           int at[U];
 #pragma unroll
           for (int u = 0; u < U; ++u) {
@@ -54,7 +55,7 @@ __global__ void __launch_bounds__(kThreads) loss_rows_kernel(Args a, const T *__
 #pragma unroll
             for (int v = 0; v < V; ++v) {
               const int g = col + v * LPC;
-              load_group<T, W>(table + at[u] * a.st + 8 * g, at[u] >= 0 ? a.cols - 8 * g : 0, w[u][v]);
+              w[u][v] = load_group<T, W>(table + at[u] * a.st + 8 * g, at[u] >= 0 ? a.cols - 8 * g : 0);
             }
           }
           float high = top;
@@ -62,11 +63,7 @@ __global__ void __launch_bounds__(kThreads) loss_rows_kernel(Args a, const T *__
 #pragma unroll
           for (int u = 0; u < U; ++u) {
             any |= at[u] >= 0;
-            l[u] = 0.f;
-#pragma unroll
-            for (int v = 0; v < V; ++v)
-#pragma unroll
-              for (int i = 0; i < 8; ++i) l[u] += h[v][i] * w[u][v][i];
+            l[u] = dot<V>(h, w[u]);
 #pragma unroll
             for (int o = 1; o < LPC; o <<= 1) l[u] += __shfl_xor_sync(0xffffffffu, l[u], o);
             if (at[u] < 0) l[u] = -INFINITY;
@@ -80,7 +77,7 @@ __global__ void __launch_bounds__(kThreads) loss_rows_kernel(Args a, const T *__
 #pragma unroll
               for (int v = 0; v < V; ++v)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) acc[v][i] *= shrink;
+                for (int i = 0; i < 4; ++i) acc[v].p[i] = mul2(acc[v].p[i], both(shrink));
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
@@ -90,7 +87,7 @@ __global__ void __launch_bounds__(kThreads) loss_rows_kernel(Args a, const T *__
 #pragma unroll
                 for (int v = 0; v < V; ++v)
 #pragma unroll
-                  for (int i = 0; i < 8; ++i) acc[v][i] += p * w[u][v][i];
+                  for (int i = 0; i < 4; ++i) acc[v].p[i] = fma2(both(p), w[u][v].p[i], acc[v].p[i]);
               }
             }
             top = high;
@@ -114,14 +111,14 @@ __global__ void __launch_bounds__(kThreads) loss_rows_kernel(Args a, const T *__
 #pragma unroll
         for (int v = 0; v < V; ++v) {
           const int g = col + v * LPC;
-          float w[8];
-          load_group<T, W>(table + target * a.st + 8 * g, a.cols - 8 * g, w);
+          Group w = load_group<T, W>(table + target * a.st + 8 * g, a.cols - 8 * g);
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            acc[v][i] *= inv;
+            float &x = acc[v].at(i);
+            x *= inv;
 #pragma unroll
-            for (int o = LPC; o < 32; o <<= 1) acc[v][i] += __shfl_xor_sync(0xffffffffu, acc[v][i], o);
-            acc[v][i] -= w[i];
+            for (int o = LPC; o < 32; o <<= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+            x -= w.at(i);
           }
         }
       }
@@ -293,10 +290,9 @@ __global__ void __launch_bounds__(kThreads) loss_scale_kernel(Args a, const floa
   const int64_t total = (int64_t)a.rows * a.groups, step = (int64_t)gridDim.x * kThreads;
   for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += step) {
     const int row = (int)(i / a.groups), g = (int)(i - (int64_t)row * a.groups), valid = a.cols - 8 * g;
-    float v[8];
-    load_group<float, (W < 4 ? W : 4)>(dh + (int64_t)row * a.cols + 8 * g, valid, v);
+    Group v = load_group<float, (W < 4 ? W : 4)>(dh + (int64_t)row * a.cols + 8 * g, valid);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] *= scale;
+    for (int j = 0; j < 4; ++j) v.p[j] = mul2(v.p[j], both(scale));
     store_group<T, W>(out + row * a.sdh + 8 * g, valid, v);
   }
 }

@@ -13,62 +13,111 @@ namespace rows {
 namespace {
 
 template <typename T, int W, typename P>
-__global__ void __launch_bounds__(P::threads) norm_bwd_kernel(Args a, const T *__restrict__ x, const T *__restrict__ res,
-                                                              const void *__restrict__ weight,
-                                                              const int64_t *__restrict__ rng,
-                                                              const float2 *__restrict__ stats,
-                                                              const T *__restrict__ dout, T *__restrict__ dx,
-                                                              T *__restrict__ dres, float *__restrict__ part) {
-  constexpr int TPR = P::TPR;
+__global__ void __launch_bounds__(P::threads, 65536 / (P::V > 1 ? 128 : 96) / P::threads)
+    norm_bwd_kernel(Args a, const T *__restrict__ x, const T *__restrict__ res, const void *__restrict__ weight,
+                    const int64_t *__restrict__ rng, const float2 *__restrict__ stats, const T *__restrict__ dout,
+                    T *__restrict__ dx, T *__restrict__ dres, float *__restrict__ part) {
+  constexpr bool AHEAD = sizeof(T) == 2;  // the next row is under way while this one is worked on (see the forward)
+  constexpr int TPR = P::TPR, V = P::V, kGroups = TPR * V;
   __shared__ float2 buf[TPR > 32 ? TPR / 16 : 1];
-  __shared__ float2 sums[TPR <= 32 ? TPR * 8 : 1];
+  __shared__ float2 sums[TPR <= 32 ? TPR * V * 8 : 1];
+  __shared__ float4 ws[V > 1 ? 2 * kGroups : 1];  // the weights of wide rows, two quarters a group, the groups side by side
   grid_chain_enter();
   Generator gen;
-  if (a.bar) gen.read(rng);
-  const int g = (int)threadIdx.x % TPR, slot = (int)threadIdx.x / TPR, valid = a.cols - 8 * g;
+  if (a.drop == 1) gen.read(rng);
+  const int lane = (int)threadIdx.x % TPR, slot = (int)threadIdx.x / TPR;
   int turn = 0;
-  float w[8], gw[8], gb[8];
-  load_weights(weight, a.wide_weights, 8 * g, valid, 1.f, w);
-#pragma unroll
-  for (int j = 0; j < 8; ++j) gw[j] = gb[j] = 0.f;
-  // (the bound is the same for all threads of a CTA: they meet in row_sum)
-  for (int64_t r0 = (int64_t)blockIdx.x * P::slots; r0 < a.rows; r0 += (int64_t)gridDim.x * P::slots) {
-    const int64_t row = r0 + slot;
-    const bool there = row < a.rows;
-    float z[8], r[8], d[8];
-    uint32_t m = 0xffu;
-    float2 st = make_float2(0.f, 0.f);
-    if (there) st = stats[row];
-    load_group<T, W>(x + row * a.sx + 8 * g, there ? valid : 0, z);
-    load_group<T, W>(res + row * a.sr + 8 * g, res && there ? valid : 0, r);
-    load_group<T, W>(dout + row * a.so + 8 * g, there ? valid : 0, d);
-    if (a.bar) {
-      m = gen.kept(a, (int)row, g);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) z[j] = m >> j & 1 ? z[j] * a.scale : 0.f;
+  Group w1, gw[V], gb[V];
+  if constexpr (V == 1) {
+    w1 = load_weights(weight, a.wide_weights, 8 * lane, a.cols - 8 * lane, 1.f);
+  } else {
+    for (int g = (int)threadIdx.x; g < kGroups; g += P::threads) {
+      const Group w = load_weights(weight, a.wide_weights, 8 * g, a.cols - 8 * g, 1.f);
+      ws[g] = make_float4(w.p[0].x, w.p[0].y, w.p[1].x, w.p[1].y);
+      ws[kGroups + g] = make_float4(w.p[2].x, w.p[2].y, w.p[3].x, w.p[3].y);
     }
-    float2 s = make_float2(0.f, 0.f);
+    __syncthreads();
+  }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      z[j] = j < valid ? (z[j] + r[j] - st.x) * st.y : 0.f;  // n; 0 in rows and columns that are not there, like d
-      gw[j] += d[j] * z[j];
-      gb[j] += d[j];
-      d[j] *= w[j];  // a
-      s.x += d[j];
-      s.y += d[j] * z[j];
+  for (int v = 0; v < V; ++v)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) gw[v].p[i] = gb[v].p[i] = both(0.f);
+  const uint32_t rows = (uint32_t)a.rows, step = gridDim.x * (uint32_t)P::slots;
+  uint32_t left = blockIdx.x * (uint32_t)P::slots, row = left + (uint32_t)slot;
+  const T *px = x + row * a.sx + 8 * lane, *pr = res + row * a.sr + 8 * lane, *pd = dout + row * a.so + 8 * lane;
+  T *pdx = dx + row * a.sdx + 8 * lane, *pdr = dres + row * a.sdr + 8 * lane;
+  Raw<T, W> xs[V], rs[V], ds[V];
+  float2 next_stats;
+  auto load = [&](uint32_t row) {
+    const bool there = row < rows;
+    next_stats = there ? stats[row] : both(0.f);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const int valid = there ? a.cols - 8 * (lane + v * TPR) : 0;
+      xs[v].load(px + 8 * v * TPR, a.drop < 2 ? valid : 0);
+      rs[v].load(pr + 8 * v * TPR, res ? valid : 0);
+      ds[v].load(pd + 8 * v * TPR, valid);
+    }
+  };
+  if (AHEAD) load(row);
+  // (`left`, the CTA's first row, is the same for all of its threads: they meet in row_sum)
+  for (; left < rows; left += step, row += step, pdx += step * a.sdx, pdr += step * a.sdr) {
+    if (!AHEAD) load(row);
+    const float2 st = next_stats;
+    Group z[V], d[V];
+    uint4 bits[V];
+    float2 s = both(0.f);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      bits[v] = make_uint4(0, 0, 0, 0);
+      if (a.drop == 1) bits[v] = gen.bits(a, (int)row, lane + v * TPR);
+      z[v] = xs[v].get();
+      d[v] = ds[v].get();
+      if (a.drop == 1) drop(a, bits[v], z[v]);
+      const Group r = rs[v].get();
+#pragma unroll
+      for (int i = 0; i < 4; ++i) z[v].p[i] = fma2(z[v].p[i], both(a.scale), r.p[i]);
+    }
+    px += step * a.sx, pr += step * a.sr, pd += step * a.so;
+    if (AHEAD) load(row + step);
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const Group m = spread<W>(-st.x, a.cols - 8 * (lane + v * TPR));
+      Group w = w1;
+      if constexpr (V > 1) {
+        const float4 q0 = ws[lane + v * TPR], q1 = ws[kGroups + lane + v * TPR];
+        w.p[0] = make_float2(q0.x, q0.y), w.p[1] = make_float2(q0.z, q0.w);
+        w.p[2] = make_float2(q1.x, q1.y), w.p[3] = make_float2(q1.z, q1.w);
+      }
+      float2 s2[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        // n; 0 in rows and columns that are not there, like d
+        z[v].p[i] = mul2(add2(z[v].p[i], m.p[i]), both(st.y));
+        gw[v].p[i] = fma2(d[v].p[i], z[v].p[i], gw[v].p[i]);
+        gb[v].p[i] = add2(d[v].p[i], gb[v].p[i]);
+        d[v].p[i] = mul2(d[v].p[i], w.p[i]);  // a
+        s2[i] = mul2(d[v].p[i], z[v].p[i]);
+      }
+      s = add2(s, make_float2(total(d[v].p), total(s2)));
     }
     s = row_sum<TPR>(s, buf, turn);
-    if (!there) continue;
-    const float c1 = s.x * a.inv_cols, c2 = s.y * a.inv_cols;
+    if (row >= rows) continue;
+    const float2 c1 = both(-s.x * a.inv_cols), c2 = both(-s.y * a.inv_cols);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) d[j] = st.y * (d[j] - c1 - z[j] * c2);
-    if (dres) store_group<T, W>(dres + row * a.sdr + 8 * g, valid, d);
-    if (dx) {
-      if (a.bar) {
+    for (int v = 0; v < V; ++v) {
+      const int valid = a.cols - 8 * (lane + v * TPR);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) d[j] = m >> j & 1 ? d[j] * a.scale : 0.f;
+      for (int i = 0; i < 4; ++i) d[v].p[i] = mul2(fma2(z[v].p[i], c2, add2(d[v].p[i], c1)), both(st.y));
+      if (dres) store_group<T, W>(pdr + 8 * v * TPR, valid, d[v]);
+      if (dx) {
+        if (a.drop) {
+          if (a.drop == 1) drop(a, bits[v], d[v]);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) d[v].p[i] = a.drop == 1 ? mul2(d[v].p[i], both(a.scale)) : both(0.f);
+        }
+        store_group<T, W>(pdx + 8 * v * TPR, valid, d[v]);
       }
-      store_group<T, W>(dx + row * a.sdx + 8 * g, valid, d);
     }
   }
   if (!part) return;
@@ -76,19 +125,23 @@ __global__ void __launch_bounds__(P::threads) norm_bwd_kernel(Args a, const T *_
   if constexpr (TPR <= 32) {
     // over the groups of threads of a warp, which hold the same columns, then warp by warp
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
+    for (int v = 0; v < V; ++v)
 #pragma unroll
-      for (int o = TPR; o < 32; o <<= 1) {
-        gw[j] += __shfl_xor_sync(0xffffffffu, gw[j], o);
-        gb[j] += __shfl_xor_sync(0xffffffffu, gb[j], o);
-      }
+      for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int o = TPR; o < 32; o <<= 1) {
+          gw[v].at(j) = exchange_add(gw[v].at(j), o);
+          gb[v].at(j) = exchange_add(gb[v].at(j), o);
+        }
     for (int warp = 0; warp < P::threads / 32; ++warp) {
       if ((int)threadIdx.x / 32 == warp && (int)threadIdx.x % 32 < TPR) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          float2 &p = sums[8 * g + j];
-          p = warp ? make_float2(p.x + gw[j], p.y + gb[j]) : make_float2(gw[j], gb[j]);
-        }
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            float2 &p = sums[8 * (lane + v * TPR) + j];
+            p = warp ? make_float2(p.x + gw[v].at(j), p.y + gb[v].at(j)) : make_float2(gw[v].at(j), gb[v].at(j));
+          }
       }
       __syncthreads();
     }
@@ -98,27 +151,43 @@ __global__ void __launch_bounds__(P::threads) norm_bwd_kernel(Args a, const T *_
     }
   } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (j < valid) mine[8 * g + j] = gw[j], mine[a.cols + 8 * g + j] = gb[j];
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int c = 8 * (lane + v * TPR) + j;
+        if (c < a.cols) mine[c] = gw[v].at(j), mine[a.cols + c] = gb[v].at(j);
+      }
   }
 }
 
-// dweight and dbias from the CTAs' partial sums: 32 columns and 32 slices of the CTAs a block.
-__global__ void __launch_bounds__(1024) norm_weights_kernel(int cols, int ctas, const float *__restrict__ part, int wide,
-                                                            void *__restrict__ dweight, void *__restrict__ dbias) {
-  __shared__ float sums[32][33];
+// dweight and dbias from the CTAs' partial sums: 16 columns and 32 slices of the CTAs a block, 8 loads in flight a thread.
+constexpr int kSumCols = 16, kSumSlices = 32;
+__global__ void __launch_bounds__(kSumCols *kSumSlices) norm_weights_kernel(int cols, int ctas, const float *__restrict__ part,
+                                                                            int wide, void *__restrict__ dweight,
+                                                                            void *__restrict__ dbias) {
+  __shared__ float sums[kSumSlices][kSumCols + 1];
   grid_chain_enter();
-  const int tx = (int)threadIdx.x % 32, ty = (int)threadIdx.x / 32, c = (int)blockIdx.x * 32 + tx;
+  const int tx = (int)threadIdx.x % kSumCols, ty = (int)threadIdx.x / kSumCols, c = (int)blockIdx.x * kSumCols + tx;
   float s = 0.f;
   if (c < 2 * cols)
-    for (int i = ty; i < ctas; i += 32) s += part[(int64_t)i * 2 * cols + c];
+    for (int i0 = ty; i0 < ctas; i0 += 8 * kSumSlices) {
+      float v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int i = i0 + k * kSumSlices;
+        v[k] = i < ctas ? part[(int64_t)i * 2 * cols + c] : 0.f;
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) s += v[k];
+    }
   sums[ty][tx] = s;
   __syncthreads();
-  s = sums[tx][ty];  // (a warp now holds one column's slices)
+  const int lane = (int)threadIdx.x % 32, warp = (int)threadIdx.x / 32;  // a warp a column
+  s = sums[lane][warp];
 #pragma unroll
   for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-  const int col = (int)blockIdx.x * 32 + ty;
-  if (tx || col >= 2 * cols) return;
+  const int col = (int)blockIdx.x * kSumCols + warp;
+  if (lane || col >= 2 * cols) return;
   void *to = col < cols ? dweight : dbias;
   const int at = col < cols ? col : col - cols;
   if (!to) return;
@@ -131,9 +200,10 @@ __global__ void __launch_bounds__(1024) norm_weights_kernel(int cols, int ctas, 
 // CTAs of the backward: as many as run at once, fewer while they would have no rows.
 int backward_ctas(const Args &a) {
   int64_t n = 0;
-  with_plan(a.groups, [&](auto plan) {
+  with_plan<2>(a.groups, [&](auto plan) {
     using P = decltype(plan);
-    const int64_t ctas = ((int64_t)a.rows + P::slots - 1) / P::slots, most = kSMs * (P::threads < 768 ? 768 / P::threads : 1);
+    const int64_t ctas = ((int64_t)a.rows + P::slots - 1) / P::slots;
+    const int64_t most = kSMs * (65536 / (P::V > 1 ? 128 : 96) / P::threads);  // (as the kernel's bounds say)
     n = ctas < most ? ctas : most;
   });
   return (int)n;
@@ -183,7 +253,7 @@ extern "C" int blossom_add_norm_bwd(const blossom_rows_params *params, const voi
   al.rows_at(dresidual, a.sdr, esz);
   const int ctas = rows::backward_ctas(a);
   float *part = dweight || dbias ? static_cast<float *>(workspace) : nullptr;
-  rows::with_plan(a.groups, [&](auto plan) {
+  rows::with_plan<2>(a.groups, [&](auto plan) {
     using P = decltype(plan);
     rows::with_type(params->dtype, al.elements(a.cols, esz), [&](auto t, auto w) {
       using T = decltype(t);
@@ -196,7 +266,8 @@ extern "C" int blossom_add_norm_bwd(const blossom_rows_params *params, const voi
   });
   if (part) {
     LaunchScope ls(K_NORM_WEIGHTS, st);
-    launch_chained(rows::norm_weights_kernel, dim3((unsigned)((2 * a.cols + 31) / 32)), dim3(1024), 0, st, a.cols, ctas,
+    launch_chained(rows::norm_weights_kernel, dim3((unsigned)((2 * a.cols + rows::kSumCols - 1) / rows::kSumCols)),
+                   dim3(rows::kSumCols * rows::kSumSlices), 0, st, a.cols, ctas,
                    (const float *)part, a.wide_weights, dweight, dbias);
   }
   return cudaGetLastError() == cudaSuccess ? BLOSSOM_OK : BLOSSOM_ERR_CUDA;

@@ -9,58 +9,115 @@ namespace blossom {
 namespace rows {
 namespace {
 
-constexpr int kRowsInFlight = 2;  // rows a thread loads before it works on the first
+// Rows that a thread has under way at a time: two narrow ones, or one.
+template <typename P>
+struct InFlight {
+  static constexpr int rows = P::V == 1 ? 2 : 1;
+};
 
 template <typename T, int W, typename P>
-__global__ void __launch_bounds__(P::threads) norm_fwd_kernel(Args a, const T *__restrict__ x, const T *__restrict__ res,
-                                                              const void *__restrict__ weight, const void *__restrict__ bias,
-                                                              const int64_t *__restrict__ rng, T *__restrict__ out,
-                                                              float2 *__restrict__ stats) {
-  constexpr int TPR = P::TPR, U = kRowsInFlight;
-  __shared__ float2 buf[TPR > 32 ? TPR / 16 : 1];
+__global__ void __launch_bounds__(P::threads, 65536 / (P::V > 2 ? 128 : 80) / P::threads)
+    norm_fwd_kernel(Args a, const T *__restrict__ x, const T *__restrict__ res, const void *__restrict__ weight,
+                    const void *__restrict__ bias, const int64_t *__restrict__ rng, T *__restrict__ out,
+                    float2 *__restrict__ stats) {
+  // In bf16 the next rows are under way while these are worked on; in fp32, twice the bytes a column, they would take
+  // registers that the work needs.
+  constexpr bool AHEAD = sizeof(T) == 2;
+  constexpr int TPR = P::TPR, V = P::V, U = InFlight<P>::rows, kGroups = TPR * V;
+  __shared__ float buf[TPR > 32 ? TPR / 16 : 1];
+  // weight and bias of wide rows: per group of columns two quarters of each, the groups side by side (so that a warp reads
+  // consecutive addresses)
+  extern __shared__ float4 wb[];  // [4][kGroups]
   grid_chain_enter();
   Generator gen;
-  if (a.bar) gen.read(rng);
-  const int g = (int)threadIdx.x % TPR, slot = (int)threadIdx.x / TPR, valid = a.cols - 8 * g;
+  if (a.drop == 1) gen.read(rng);
+  const int lane = (int)threadIdx.x % TPR, slot = (int)threadIdx.x / TPR;
   int turn = 0;
-  float w[8], b[8];
-  load_weights(weight, a.wide_weights, 8 * g, valid, 1.f, w);
-  load_weights(bias, a.wide_weights, 8 * g, valid, 0.f, b);
-  // (the bound is the same for all threads of a CTA: they meet in row_sum)
-  for (int64_t r0 = (int64_t)blockIdx.x * (P::slots * U); r0 < a.rows; r0 += (int64_t)gridDim.x * (P::slots * U)) {
-    float z[U][8], r[U][8];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int64_t row = r0 + u * P::slots + slot;
-      load_group<T, W>(x + row * a.sx + 8 * g, row < a.rows ? valid : 0, z[u]);
-      load_group<T, W>(res + row * a.sr + 8 * g, res && row < a.rows ? valid : 0, r[u]);
+  Group w1, b1;
+  if constexpr (V == 1) {
+    w1 = load_weights(weight, a.wide_weights, 8 * lane, a.cols - 8 * lane, 1.f);
+    b1 = load_weights(bias, a.wide_weights, 8 * lane, a.cols - 8 * lane, 0.f);
+  } else {
+    for (int g = (int)threadIdx.x; g < kGroups; g += P::threads) {
+      const Group w = load_weights(weight, a.wide_weights, 8 * g, a.cols - 8 * g, 1.f);
+      const Group b = load_weights(bias, a.wide_weights, 8 * g, a.cols - 8 * g, 0.f);
+      wb[g] = make_float4(w.p[0].x, w.p[0].y, w.p[1].x, w.p[1].y);
+      wb[kGroups + g] = make_float4(w.p[2].x, w.p[2].y, w.p[3].x, w.p[3].y);
+      wb[2 * kGroups + g] = make_float4(b.p[0].x, b.p[0].y, b.p[1].x, b.p[1].y);
+      wb[3 * kGroups + g] = make_float4(b.p[2].x, b.p[2].y, b.p[3].x, b.p[3].y);
     }
+    __syncthreads();
+  }
+  const uint32_t rows = (uint32_t)a.rows, step = gridDim.x * (uint32_t)(P::slots * U);
+  uint32_t row0 = blockIdx.x * (uint32_t)(P::slots * U) + (uint32_t)slot, left = blockIdx.x * (uint32_t)(P::slots * U);
+  const T *px = x + row0 * a.sx + 8 * lane, *pr = res + row0 * a.sr + 8 * lane;
+  T *po = out + row0 * a.so + 8 * lane;
+  Raw<T, W> xs[U][V], rs[U][V];
+  auto load = [&](uint32_t row, const T *px, const T *pr) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const int valid = row + u * P::slots < rows ? a.cols - 8 * (lane + v * TPR) : 0;
+        xs[u][v].load(px + u * P::slots * a.sx + 8 * v * TPR, a.drop < 2 ? valid : 0);
+        rs[u][v].load(pr + u * P::slots * a.sr + 8 * v * TPR, res ? valid : 0);
+      }
+  };
+  if (AHEAD) load(row0, px, pr);
+  // (`left`, the CTA's first row, is the same for all of its threads: they meet in row_sum)
+  for (; left < rows; left += step, row0 += step, po += step * a.so) {
+    Group z[U][V];
+    if (!AHEAD) load(row0, px, pr);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        uint4 bits = make_uint4(0, 0, 0, 0);
+        if (a.drop == 1) bits = gen.bits(a, (int)(row0 + u * P::slots), lane + v * TPR);
+        z[u][v] = xs[u][v].get();
+        if (a.drop == 1) drop(a, bits, z[u][v]);
+        const Group r = rs[u][v].get();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) z[u][v].p[i] = fma2(z[u][v].p[i], both(a.scale), r.p[i]);
+      }
+    px += step * a.sx, pr += step * a.sr;
+    if (AHEAD) load(row0 + step, px, pr);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int64_t row = r0 + u * P::slots + slot;
-      if (a.bar) {
-        const uint32_t m = gen.kept(a, (int)row, g);
+      float s = 0.f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) z[u][j] = m >> j & 1 ? z[u][j] * a.scale : 0.f;
+      for (int v = 0; v < V; ++v) s += total(z[u][v].p);
+      const float mean = row_sum<TPR>(s, buf, turn) * a.inv_cols;
+      s = 0.f;
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const Group m = spread<W>(-mean, a.cols - 8 * (lane + v * TPR));
+        float2 sq[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          z[u][v].p[i] = add2(z[u][v].p[i], m.p[i]);
+          sq[i] = mul2(z[u][v].p[i], z[u][v].p[i]);
+        }
+        s += total(sq);
       }
-      float sum = 0.f, sq = 0.f;
+      const float rstd = rsqrtf(row_sum<TPR>(s, buf, turn) * a.inv_cols + a.eps);
+      if (row0 + u * P::slots < rows) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        z[u][j] += r[u][j];
-        sum += z[u][j];
-      }
-      const float mean = row_sum<TPR>(sum, buf, turn) * a.inv_cols;
+        for (int v = 0; v < V; ++v) {
+          const int g = lane + v * TPR;
+          Group w = w1, b = b1;
+          if constexpr (V > 1) {
+            const float4 q[4] = {wb[g], wb[kGroups + g], wb[2 * kGroups + g], wb[3 * kGroups + g]};
+            w.p[0] = make_float2(q[0].x, q[0].y), w.p[1] = make_float2(q[0].z, q[0].w);
+            w.p[2] = make_float2(q[1].x, q[1].y), w.p[3] = make_float2(q[1].z, q[1].w);
+            b.p[0] = make_float2(q[2].x, q[2].y), b.p[1] = make_float2(q[2].z, q[2].w);
+            b.p[2] = make_float2(q[3].x, q[3].y), b.p[3] = make_float2(q[3].z, q[3].w);
+          }
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        z[u][j] = j < valid ? z[u][j] - mean : 0.f;
-        sq += z[u][j] * z[u][j];
-      }
-      const float rstd = rsqrtf(row_sum<TPR>(sq, buf, turn) * a.inv_cols + a.eps);
-      if (row < a.rows) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) z[u][j] = z[u][j] * rstd * w[j] + b[j];
-        store_group<T, W>(out + row * a.so + 8 * g, valid, z[u]);
-        if (stats && g == 0) stats[row] = make_float2(mean, rstd);
+          for (int i = 0; i < 4; ++i) z[u][v].p[i] = fma2(mul2(z[u][v].p[i], both(rstd)), w.p[i], b.p[i]);
+          store_group<T, W>(po + u * P::slots * a.so + 8 * v * TPR, a.cols - 8 * g, z[u][v]);
+        }
+        if (stats && lane == 0) stats[row0 + u * P::slots] = make_float2(mean, rstd);
       }
     }
   }
@@ -89,18 +146,28 @@ extern "C" int blossom_add_norm_fwd(const blossom_rows_params *params, const voi
   al.rows_at(x, a.sx, esz);
   al.rows_at(residual, a.sr, esz);
   al.rows_at(out, a.so, esz);
-  rows::with_plan(a.groups, [&](auto plan) {
+  bool ok = true;
+  auto launch = [&](auto plan) {
     using P = decltype(plan);
     rows::with_type(params->dtype, al.elements(a.cols, esz), [&](auto t, auto w) {
       using T = decltype(t);
-      const int64_t per = P::slots * rows::kRowsInFlight, ctas = (a.rows + per - 1) / per;
-      const int64_t most = rows::kSMs * (2048 / P::threads);
-      LaunchScope ls(K_NORM_FWD, (cudaStream_t)stream);
-      launch_chained(rows::norm_fwd_kernel<T, decltype(w)::value, P>, dim3((unsigned)(ctas < most ? ctas : most)),
-                     dim3(P::threads), 0, (cudaStream_t)stream, a, static_cast<const T *>(x),
-                     static_cast<const T *>(residual), weight, bias, rng, static_cast<T *>(out),
-                     reinterpret_cast<float2 *>(stats));
+      if constexpr (P::V <= (sizeof(T) == 2 ? 4 : 2)) {
+        const auto kern = rows::norm_fwd_kernel<T, decltype(w)::value, P>;
+        const int64_t per = P::slots * rows::InFlight<P>::rows, ctas = (a.rows + per - 1) / per;
+        const int64_t most = rows::kSMs * (65536 / (P::V > 2 ? 128 : 80) / P::threads);  // (as many as run at once)
+        const size_t smem = P::V > 1 ? (size_t)P::TPR * P::V * 4 * sizeof(float4) : 0;
+        ok = allow_smem(kern, smem);
+        if (!ok) return;
+        LaunchScope ls(K_NORM_FWD, (cudaStream_t)stream);
+        launch_chained(kern, dim3((unsigned)(ctas < most ? ctas : most)), dim3(P::threads), smem, (cudaStream_t)stream, a,
+                       static_cast<const T *>(x), static_cast<const T *>(residual), weight, bias, rng,
+                       static_cast<T *>(out), reinterpret_cast<float2 *>(stats));
+      }
     });
-  });
+  };
+  // (half the bytes a column in bf16: twice the columns a thread for as much under way)
+  if (esz == 2) rows::with_plan<4>(a.groups, launch);
+  else rows::with_plan<2>(a.groups, launch);
+  if (!ok) return BLOSSOM_ERR_CUDA;
   return cudaGetLastError() == cudaSuccess ? BLOSSOM_OK : BLOSSOM_ERR_CUDA;
 }

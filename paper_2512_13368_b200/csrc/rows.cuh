@@ -12,77 +12,123 @@ constexpr int kMaxCols = 8192;
 struct Args {
   int rows, cols, groups;  // groups of 8 columns, the last one possibly short
   int64_t sx, sr, so, sdx, sdr;  // element strides: x, residual, out / dout, dx, dresidual
-  unsigned bar, site;      // an element is kept if its 16 bits are >= bar
+  int drop;                // 0: everything is kept, 1: by the generator, 2: nothing is
+  unsigned bar, site;      // an element is kept if its 16 bits are >= bar / 65536 (bar: those bits above 16 zeros)
   float scale;             // of the kept ones
   float eps, inv_cols;
   int wide_weights;        // weight and bias are fp32 (else bf16)
 };
 
-// ---- a group of 8 columns, W elements an access -------------------------------------------------
+// ---- a group of 8 columns in four pairs, W elements an access --------------------------------------
 // W is the widest of 16 bytes, two elements and one that every row's address and length is a multiple of.
-template <typename T, int W>
-__device__ __forceinline__ void load_group(const T *p, int valid, float (&v)[8]) {
-#pragma unroll
-  for (int j = 0; j < 8; j += W) {
-    if (j < valid) {
-      if constexpr (sizeof(T) == 4 && W == 4) {
-        const float4 q = *reinterpret_cast<const float4 *>(p + j);
-        v[j] = q.x, v[j + 1] = q.y, v[j + 2] = q.z, v[j + 3] = q.w;
-      } else if constexpr (sizeof(T) == 4 && W == 2) {
-        const float2 q = *reinterpret_cast<const float2 *>(p + j);
-        v[j] = q.x, v[j + 1] = q.y;
-      } else if constexpr (sizeof(T) == 4) {
-        v[j] = p[j];
-      } else if constexpr (W == 8) {
-        const uint4 q = *reinterpret_cast<const uint4 *>(p);
-        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[2 * i] = __uint_as_float(w[i] << 16), v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-      } else if constexpr (W == 2) {
-        const uint32_t w = *reinterpret_cast<const uint32_t *>(p + j);
-        v[j] = __uint_as_float(w << 16), v[j + 1] = __uint_as_float(w & 0xffff0000u);
-      } else {
-        v[j] = __bfloat162float(p[j]);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < W; ++i) v[j + i] = 0.f;
-    }
-  }
+struct Group {
+  float2 p[4];
+  __device__ __forceinline__ float &at(int j) { return j & 1 ? p[j / 2].y : p[j / 2].x; }
+};
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  uint64_t d;
+  asm("mul.rn.ftz.f32x2 %0, %1, %2;"
+      : "=l"(d)
+      : "l"(*reinterpret_cast<uint64_t *>(&a)), "l"(*reinterpret_cast<uint64_t *>(&b)));
+  return *reinterpret_cast<float2 *>(&d);
+}
+__device__ __forceinline__ float2 halves(uint32_t w) {  // two bf16
+  return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
 }
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
   const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);  // round to nearest even, once
   return *reinterpret_cast<const uint32_t *>(&h);
 }
+// As it comes from memory: loads that are under way hold half as many registers in bf16.
 template <typename T, int W>
-__device__ __forceinline__ void store_group(T *p, int valid, const float (&v)[8]) {
+struct Raw {
+  uint32_t w[2 * sizeof(T)];
+  __device__ __forceinline__ void load(const T *p, int valid) {
+    constexpr int words = W * (int)sizeof(T) / 4;  // an access has (0: half a one)
+#pragma unroll
+    for (int j = 0; j < 8; j += W) {
+      const int at = j * (int)sizeof(T) / 4;
+      if (j < valid) {
+        if constexpr (words == 4) {
+          const uint4 q = *reinterpret_cast<const uint4 *>(p + j);
+          w[at] = q.x, w[at + 1] = q.y, w[at + 2] = q.z, w[at + 3] = q.w;
+        } else if constexpr (words == 2) {
+          const uint2 q = *reinterpret_cast<const uint2 *>(p + j);
+          w[at] = q.x, w[at + 1] = q.y;
+        } else if constexpr (words == 1) {
+          w[at] = *reinterpret_cast<const uint32_t *>(p + j);
+        } else {
+          const uint32_t h = *reinterpret_cast<const uint16_t *>(p + j);
+          w[at] = j & 1 ? w[at] | h << 16 : h;
+        }
+      } else if constexpr (words > 0) {
+#pragma unroll
+        for (int i = 0; i < words; ++i) w[at + i] = 0;
+      } else if (!(j & 1)) {
+        w[at] = 0;
+      }
+    }
+  }
+  __device__ __forceinline__ Group get() const {
+    Group v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (sizeof(T) == 4) v.p[i] = make_float2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+      else v.p[i] = halves(w[i]);
+    }
+    return v;
+  }
+};
+template <typename T, int W>
+__device__ __forceinline__ Group load_group(const T *p, int valid) {
+  Raw<T, W> r;
+  r.load(p, valid);
+  return r.get();
+}
+template <typename T, int W>
+__device__ __forceinline__ void store_group(T *p, int valid, const Group &g) {
+  Group v = g;
 #pragma unroll
   for (int j = 0; j < 8; j += W) {
     if (j < valid) {
       if constexpr (sizeof(T) == 4 && W == 4) {
-        *reinterpret_cast<float4 *>(p + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+        *reinterpret_cast<float4 *>(p + j) = make_float4(v.at(j), v.at(j + 1), v.at(j + 2), v.at(j + 3));
       } else if constexpr (sizeof(T) == 4 && W == 2) {
-        *reinterpret_cast<float2 *>(p + j) = make_float2(v[j], v[j + 1]);
+        *reinterpret_cast<float2 *>(p + j) = v.p[j / 2];
       } else if constexpr (sizeof(T) == 4) {
-        p[j] = v[j];
+        p[j] = v.at(j);
       } else if constexpr (W == 8) {
-        *reinterpret_cast<uint4 *>(p) = make_uint4(pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7]));
+        *reinterpret_cast<uint4 *>(p) = make_uint4(pack2(v.p[0].x, v.p[0].y), pack2(v.p[1].x, v.p[1].y),
+                                                   pack2(v.p[2].x, v.p[2].y), pack2(v.p[3].x, v.p[3].y));
       } else if constexpr (W == 2) {
-        *reinterpret_cast<uint32_t *>(p + j) = pack2(v[j], v[j + 1]);
+        *reinterpret_cast<uint32_t *>(p + j) = pack2(v.at(j), v.at(j + 1));
       } else {
-        p[j] = __float2bfloat16(v[j]);
+        p[j] = __float2bfloat16(v.at(j));
       }
     }
   }
 }
+// what is subtracted from the columns that are there, zero for the others (whose elements are zero and stay so)
+template <int W>
+__device__ __forceinline__ Group spread(float v, int valid) {
+  Group g;
+#pragma unroll
+  for (int j = 0; j < 8; j += W)
+#pragma unroll
+    for (int i = 0; i < W; ++i) g.at(j + i) = j < valid ? v : 0.f;
+  return g;
+}
 // weight and bias come in either type, at any alignment of theirs, once per thread and group
-__device__ __forceinline__ void load_weights(const void *p, int wide, int at, int valid, float other, float (&v)[8]) {
+__device__ __forceinline__ Group load_weights(const void *p, int wide, int at, int valid, float other) {
+  Group v;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    v[i] = other;
+    v.at(i) = other;
     if (p && i < valid)
-      v[i] = wide ? static_cast<const float *>(p)[at + i] : __bfloat162float(static_cast<const __nv_bfloat16 *>(p)[at + i]);
+      v.at(i) = wide ? static_cast<const float *>(p)[at + i] : __bfloat162float(static_cast<const __nv_bfloat16 *>(p)[at + i]);
   }
+  return v;
 }
 
 // ---- which elements a dropout keeps ------------------------------------------------------------
@@ -105,69 +151,74 @@ struct Generator {
     key = make_uint2((uint32_t)a, (uint32_t)(a >> 32));
     step = make_uint2((uint32_t)b, (uint32_t)(b >> 32));
   }
-  // bit i: column i of the group is kept.  16 bits decide an element, so that one evaluation serves the 8 elements
-  // of a 16-byte access in bf16 (32 bits each would double the generator's share of the kernel's instructions)
-  __device__ __forceinline__ uint32_t kept(const Args &a, int row, int group) const {
-    const uint4 w = philox(make_uint4((uint32_t)group | a.site << 16, (uint32_t)row, step.x, step.y), key);
-    const uint32_t x[4] = {w.x, w.y, w.z, w.w};
-    uint32_t m = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      m |= (uint32_t)((x[i] & 0xffffu) >= a.bar) << (2 * i);
-      m |= (uint32_t)((x[i] >> 16) >= a.bar) << (2 * i + 1);
-    }
-    return m;
+  // 16 bits decide an element, so that one evaluation serves the 8 elements of a 16-byte access in bf16 (32 bits each would
+  // double the generator's share of the kernel's instructions)
+  __device__ __forceinline__ uint4 bits(const Args &a, int row, int group) const {
+    return philox(make_uint4((uint32_t)group | a.site << 16, (uint32_t)row, step.x, step.y), key);
   }
 };
+// zero where an element is dropped, whatever it was; the kept ones are yet to be scaled
+__device__ __forceinline__ void drop(const Args &a, uint4 bits, Group &v) {
+  const uint32_t x[4] = {bits.x, bits.y, bits.z, bits.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v.p[i].x = (x[i] << 16) >= a.bar ? v.p[i].x : 0.f;  // (bar's low 16 bits are zero)
+    v.p[i].y = x[i] >= a.bar ? v.p[i].y : 0.f;
+  }
+}
 
 // ---- sums over a row's TPR threads ---------------------------------------------------------------
 // Every thread gets the same bits: within a warp by exchange, across warps added up in the order of the warps.  buf: two
-// slots of TPR / 32 pairs that alternate, so that one barrier a sum suffices.
-template <int TPR>
-__device__ __forceinline__ float2 row_sum(float2 v, float2 *buf, int &turn) {
+// slots of TPR / 32 sums that alternate, so that one barrier a sum suffices.
+__device__ __forceinline__ float total(const float2 (&v)[4]) {
+  const float2 s = add2(add2(v[0], v[1]), add2(v[2], v[3]));
+  return s.x + s.y;
+}
+__device__ __forceinline__ float exchange_add(float v, int o) { return v + __shfl_xor_sync(0xffffffffu, v, o); }
+__device__ __forceinline__ float2 exchange_add(float2 v, int o) {
+  return add2(v, make_float2(__shfl_xor_sync(0xffffffffu, v.x, o), __shfl_xor_sync(0xffffffffu, v.y, o)));
+}
+__device__ __forceinline__ float plus(float a, float b) { return a + b; }
+__device__ __forceinline__ float2 plus(float2 a, float2 b) { return add2(a, b); }
+template <int TPR, typename S>
+__device__ __forceinline__ S row_sum(S v, S *buf, int &turn) {
 #pragma unroll
-  for (int o = 1; o < (TPR < 32 ? TPR : 32); o <<= 1) {
-    v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
-    v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
-  }
+  for (int o = 1; o < (TPR < 32 ? TPR : 32); o <<= 1) v = exchange_add(v, o);
   if constexpr (TPR > 32) {
     constexpr int NW = TPR / 32;
-    float2 *b = buf + turn * NW;
+    S *b = buf + turn * NW;
     turn ^= 1;
     if ((threadIdx.x & 31) == 0) b[threadIdx.x >> 5] = v;
     __syncthreads();
     v = b[0];
 #pragma unroll
-    for (int i = 1; i < NW; ++i) v.x += b[i].x, v.y += b[i].y;
+    for (int i = 1; i < NW; ++i) v = plus(v, b[i]);
   }
-  return v;
-}
-template <int TPR>
-__device__ __forceinline__ float row_sum(float v, float2 *buf, int &turn) {
-  if constexpr (TPR > 32) return row_sum<TPR>(make_float2(v, 0.f), buf, turn).x;
-#pragma unroll
-  for (int o = 1; o < (TPR < 32 ? TPR : 32); o <<= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
 
 // ---- shapes ----------------------------------------------------------------------------------
-// A thread holds one group of 8 columns of a row, TPR threads a row: groups of threads as narrow as the row, so that narrow
-// rows share a warp; rows of more than 256 columns take a CTA of their own.
-template <int TPR_>
+// TPR threads a row, V groups of 8 columns a thread: groups of threads as narrow as the row, so that narrow rows share a
+// warp; then more columns a thread, so that a row's sums are exchanged once for all of them; then a CTA a row.
+template <int TPR_, int V_>
 struct Plan {
-  static constexpr int TPR = TPR_, threads = TPR_ > 32 ? TPR_ : 256, slots = threads / TPR_;
+  static constexpr int TPR = TPR_, V = V_, threads = TPR_ > 32 ? TPR_ : 128, slots = threads / TPR_;
 };
-template <typename F>
+template <int VMAX, typename F>
 inline void with_plan(int groups, F &&f) {
-  if (groups <= 4) f(Plan<4>());
-  else if (groups <= 8) f(Plan<8>());
-  else if (groups <= 16) f(Plan<16>());
-  else if (groups <= 32) f(Plan<32>());
-  else if (groups <= 64) f(Plan<64>());
-  else if (groups <= 128) f(Plan<128>());
-  else if (groups <= 256) f(Plan<256>());
-  else if (groups <= 512) f(Plan<512>());
-  else f(Plan<1024>());
+  if (groups <= 4) return f(Plan<4, 1>());
+  if (groups <= 8) return f(Plan<8, 1>());
+  if (groups <= 16) return f(Plan<16, 1>());
+  if (groups <= 32) return f(Plan<32, 1>());
+  constexpr int V = VMAX;
+  if constexpr (VMAX > 2)
+    if (groups <= 64) return f(Plan<32, 2>());
+  if (groups <= 32 * V) return f(Plan<32, V>());
+  if (groups <= 64 * V) return f(Plan<64, V>());
+  if (groups <= 128 * V) return f(Plan<128, V>());
+  if (groups <= 256 * V) return f(Plan<256, V>());
+  if constexpr (VMAX < 4)
+    if (groups <= 512 * V) return f(Plan<512, V>());
 }
 
 // Elements an access may take: 16 bytes, two elements or one.
