@@ -321,7 +321,7 @@ typedef struct {
   int32_t mask_hits;        /* 1: a negative equal to the row's target is no candidate                   */
   int64_t ignore_index;     /* a target that takes no part, e.g. -100 or the padding item                */
   int64_t hidden_stride, table_stride, dhidden_stride, dtable_stride; /* elements per row, 0 = cols          */
-  int64_t negatives_stride; /* elements per row, 0 = the same n negatives for every row                    */
+  int64_t negatives_stride; /* elements per row (< 2^31), 0 = the same n negatives for every row           */
 } blossom_loss_params;
 
 /* One size serves both calls, of which the forward uses the first BLOSSOM_LOSS_FORWARD_BYTES and asks for no more; 0 for

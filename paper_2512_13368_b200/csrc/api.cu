@@ -472,7 +472,7 @@ const char *blossom_kernel_name(int id) {
       "summary", "score_select", "fwd_simt", "bwd_dq_simt", "bwd_dkdv_simt", "gate_grad",
       "fwd_tc", "bwd_dq_tc", "bwd_dkdv_tc", "score_fast", "bwd_prep", "tc_meta", "rope", "bwd_short",
       "copy_rows", "dropout", "norm_fwd", "norm_bwd", "norm_weights",
-      "loss_rows", "loss_mean", "loss_scale", "loss_sort", "loss_items"};
+      "loss_rows", "loss_mean", "loss_sort", "loss_items", "loss_join"};
   return (id >= 0 && id < K_COUNT) ? names[id] : "unknown";
 }
 

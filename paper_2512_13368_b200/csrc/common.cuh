@@ -79,7 +79,7 @@ enum KernelId {
   K_SUMMARY = 0, K_SCORE_SELECT, K_FWD_SIMT, K_BWD_DQ_SIMT, K_BWD_DKDV_SIMT, K_GATE_GRAD,
   K_FWD_TC, K_BWD_DQ_TC, K_BWD_DKDV_TC, K_SCORE_FAST, K_BWD_PREP, K_TC_META, K_ROPE, K_BWD_SHORT,
   K_COPY_ROWS, K_DROPOUT, K_NORM_FWD, K_NORM_BWD, K_NORM_WEIGHTS,
-  K_LOSS_ROWS, K_LOSS_MEAN, K_LOSS_SCALE, K_LOSS_SORT, K_LOSS_ITEMS,
+  K_LOSS_ROWS, K_LOSS_MEAN, K_LOSS_SORT, K_LOSS_ITEMS, K_LOSS_JOIN,
   K_COUNT
 };
 void prof_mark(int id, int phase, cudaStream_t st);  // no-op unless a profile is running

@@ -17,7 +17,8 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct Args {
   int rows, cols, groups, items, n;
-  int64_t ignore, sh, st, sn, sdh, sdt;  // strides: hidden, table, negatives, dhidden, dtable
+  int64_t ignore, sh, st, sdh, sdt;  // strides: hidden, table, dhidden, dtable
+  uint32_t sn;                       // negatives
   int idx8, hits;
   const void *targets, *negatives;
 };
@@ -28,13 +29,13 @@ __device__ __forceinline__ int64_t load_id(const void *p, int64_t i, int idx8) {
 // the row's target, or -1 if the row takes no part
 __device__ __forceinline__ int row_target(const Args &a, int row) {
   const int64_t t = load_id(a.targets, row, a.idx8);
-  return t >= 0 && t < a.items && t != a.ignore ? (int)t : -1;
+  return (uint64_t)t < (uint64_t)a.items && t != a.ignore ? (int)t : -1;
 }
 // candidate j of a row that takes part (j = 0: its target), or -1 if it is none
 __device__ __forceinline__ int candidate(const Args &a, int row, int target, int j) {
   if (j == 0) return target;
-  const int64_t i = load_id(a.negatives, row * a.sn + (j - 1), a.idx8);
-  return i >= 0 && i < a.items && !(a.hits && i == target) ? (int)i : -1;
+  const int64_t i = load_id(a.negatives, (int64_t)((uint64_t)(uint32_t)row * a.sn + (uint32_t)(j - 1)), a.idx8);
+  return (uint64_t)i < (uint64_t)a.items && !(a.hits && i == target) ? (int)i : -1;
 }
 
 // the lane's share of <a, b>
@@ -203,13 +204,13 @@ struct SortPlan {
   int chunk;  // sorted entries that a warp or a group of lanes adds up
   int64_t chunks;
 };
-constexpr int kSortThreads = 512, kSortPerThread = 16, kTile = kSortThreads * kSortPerThread, kMaxDigits = 512;
+constexpr int kSortThreads = 256, kSortPerThread = 16, kTile = kSortThreads * kSortPerThread, kMaxDigits = 512;
 
 SortPlan sort_plan(const Args &a, int lanes);  // lanes: of a group that walks a chunk
 Scratch carve(const Args &a, void *base);
-// dtable from the candidates, sorted by item
-int launch_items(const Args &a, int dtype, const void *hidden, const void *table, const float *lse, const float *grad_loss,
-                 void *dtable, int width, const Scratch &s, cudaStream_t st);
+// dtable from the candidates, sorted by item; dhidden from grad_hidden; either may be null
+int launch_items(const Args &a, int dtype, const void *hidden, const void *table, const float *lse, const float *grad_hidden,
+                 const float *grad_loss, void *dhidden, void *dtable, int width, const Scratch &s, cudaStream_t st);
 
 // g / count, the factor of every gradient
 __device__ __forceinline__ float grad_scale(const Args &a, const float *lse, const float *grad_loss) {

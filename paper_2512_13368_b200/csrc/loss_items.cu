@@ -12,6 +12,9 @@ namespace blossom {
 namespace loss {
 namespace {
 
+// Up to so many tiles a block of the second kernel adds their counts up itself (64 loads a digit, against a launch).
+constexpr int kTilesWithoutScan = 64;
+
 // ---- the sort ------------------------------------------------------------------------------------
 // Entry e of the unsorted list is candidate e % (n + 1) of position e / (n + 1); what is no candidate gets the item
 // number `items` and ends up behind all others.
@@ -24,12 +27,6 @@ inline Split split_by(uint32_t d) {
   while (((uint64_t)1 << l) < d) ++l;
   return Split{(uint32_t)((((uint64_t)1 << (31 + l)) + d - 1) / d), (uint32_t)(31 + l)};
 }
-__device__ __forceinline__ uint32_t entry_key(const Args &a, const Split &by, uint32_t e) {
-  const uint32_t t = by(e), j = e - t * (uint32_t)(a.n + 1);
-  const int target = row_target(a, (int)t);
-  const int c = target >= 0 ? candidate(a, (int)t, target, (int)j) : -1;
-  return c >= 0 ? (uint32_t)c : (uint32_t)a.items;
-}
 __device__ __forceinline__ uint32_t entry_val(const Args &a, const Split &by, uint32_t e) {
   const uint32_t t = by(e);
   return t | (e == t * (uint32_t)(a.n + 1) ? 0x80000000u : 0u);
@@ -41,37 +38,51 @@ __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(Args a, Split 
                                                                   int shift, int bits, uint32_t *__restrict__ hist,
                                                                   uint32_t *__restrict__ range) {
   __shared__ uint32_t count[kMaxDigits];
+  __shared__ int targets[FIRST ? kTile + 1 : 1];  // of the positions that the tile belongs to
   grid_chain_enter();
-  const int digits = 1 << bits;
-  const uint32_t mask = (uint32_t)digits - 1, none = (uint32_t)a.items;
-  if ((int)threadIdx.x < digits) count[threadIdx.x] = 0;
-  if (FIRST)
-    for (int64_t i = (int64_t)blockIdx.x * kSortThreads + threadIdx.x; i < 2 * (int64_t)a.items; i += (int64_t)gridDim.x * kSortThreads)
+  const int digits = 1 << bits, tid = (int)threadIdx.x;
+  const uint32_t mask = (uint32_t)digits - 1, none = (uint32_t)a.items, tile0 = blockIdx.x * (uint32_t)kTile;
+  for (int d = tid; d < digits; d += kSortThreads) count[d] = 0;
+  uint32_t t0 = 0;
+  if (FIRST) {
+    t0 = by(tile0);
+    const uint32_t last = by((entries - tile0 < (uint32_t)kTile ? entries : tile0 + kTile) - 1);
+    for (uint32_t t = t0 + (uint32_t)tid; t <= last; t += kSortThreads) targets[t - t0] = row_target(a, (int)t);
+    for (int64_t i = (int64_t)blockIdx.x * kSortThreads + tid; i < 2 * (int64_t)a.items; i += (int64_t)gridDim.x * kSortThreads)
       range[i] = 0;
+  }
   __syncthreads();
-  const uint32_t e0 = blockIdx.x * (uint32_t)kTile + threadIdx.x;
   uint32_t key[kSortPerThread];
 #pragma unroll
   for (int r = 0; r < kSortPerThread; ++r) {
-    const uint32_t e = e0 + kSortThreads * r;
-    key[r] = 0;
-    if (e < entries) key[r] = FIRST ? entry_key(a, by, e) : keys[e];
+    const uint32_t e = tile0 + (uint32_t)tid + kSortThreads * r;
+    key[r] = none;
+    if (e < entries) {
+      if (FIRST) {
+        const uint32_t t = by(e);
+        const int target = targets[t - t0];
+        if (target >= 0) key[r] = (uint32_t)candidate(a, (int)t, target, (int)(e - t * (uint32_t)(a.n + 1)));
+        key[r] = min(key[r], none);  // (-1: no candidate)
+      } else {
+        key[r] = keys[e];
+      }
+    }
   }
 #pragma unroll
   for (int r = 0; r < kSortPerThread; ++r) {
-    const uint32_t e = e0 + kSortThreads * r;
+    const uint32_t e = tile0 + (uint32_t)tid + kSortThreads * r;
     const bool there = e < entries, padding = there && key[r] == none;
     if (FIRST && there) keys[e] = key[r];
     // (padding comes in long runs of one key: one addition a warp; items are mostly different ones)
     const uint32_t pads = __ballot_sync(0xffffffffu, padding);
-    if (padding && threadIdx.x % 32 == __ffs(pads) - 1) atomicAdd(&count[none >> shift & mask], (uint32_t)__popc(pads));
+    if (padding && tid % 32 == __ffs(pads) - 1) atomicAdd(&count[none >> shift & mask], (uint32_t)__popc(pads));
     if (there && !padding) atomicAdd(&count[key[r] >> shift & mask], 1u);
   }
   __syncthreads();
-  if ((int)threadIdx.x < digits) hist[(size_t)threadIdx.x * gridDim.x + blockIdx.x] = count[threadIdx.x];
+  for (int d = tid; d < digits; d += kSortThreads) hist[(size_t)d * gridDim.x + blockIdx.x] = count[d];
 }
 
-// Sum over the threads before this one of a 512-thread block, and the block's total.
+// Sum over the threads before this one of a block of kSortThreads, and the block's total.
 __device__ __forceinline__ uint32_t block_prefix(uint32_t v, uint32_t *warp_totals, uint32_t *total) {
   const int lane = (int)threadIdx.x % 32, warp = (int)threadIdx.x / 32;
   uint32_t s = v;
@@ -97,13 +108,24 @@ __device__ __forceinline__ uint32_t block_prefix(uint32_t v, uint32_t *warp_tota
 // hist[digit][*] becomes the number of the digit's entries in the tiles before; totals[digit] that in all of them.
 __global__ void __launch_bounds__(kSortThreads) sort_scan_kernel(uint32_t *__restrict__ hist, int tiles,
                                                                  uint32_t *__restrict__ totals) {
+  constexpr int PER = 8;  // counts a thread, one after another
   __shared__ uint32_t warp_totals[kSortThreads / 32];
   grid_chain_enter();
   uint32_t *h = hist + (size_t)blockIdx.x * tiles, carry = 0, total;
-  for (int i0 = 0; i0 < tiles; i0 += kSortThreads) {
-    const int i = i0 + (int)threadIdx.x;
-    const uint32_t before = block_prefix(i < tiles ? h[i] : 0, warp_totals, &total);
-    if (i < tiles) h[i] = carry + before;
+  for (int i0 = 0; i0 < tiles; i0 += kSortThreads * PER) {
+    const int i = i0 + (int)threadIdx.x * PER;
+    uint32_t v[PER], sum = 0;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+      v[k] = i + k < tiles ? h[i + k] : 0;
+      sum += v[k];
+    }
+    uint32_t before = carry + block_prefix(sum, warp_totals, &total);
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+      if (i + k < tiles) h[i + k] = before;
+      before += v[k];
+    }
     carry += total;
   }
   if (threadIdx.x == 0) totals[blockIdx.x] = carry;
@@ -123,22 +145,22 @@ __device__ __forceinline__ uint32_t same_digit(uint32_t d, bool there) {
 }
 
 // A tile's entries to their places, in order: ranks within a warp by matching digits, then warps, then digits; the tile is put
-// in order in shared memory first, so that it leaves in runs.  FIRST: the values are made here.  hist null: there is one tile,
-// whose own counts are all.
+// in order in shared memory first, so that it leaves in runs.  FIRST: the values are made here.  totals null: there are
+// few tiles, whose counts are added up here instead of by a kernel in between.
 template <int BITS, bool FIRST>
-__global__ void __launch_bounds__(kSortThreads, 2) sort_move_kernel(Args a, Split by, const uint32_t *__restrict__ keys,
+__global__ void __launch_bounds__(kSortThreads, 4) sort_move_kernel(Args a, Split by, const uint32_t *__restrict__ keys,
                                                                     const uint32_t *__restrict__ vals, uint32_t entries,
                                                                     int shift, const uint32_t *__restrict__ hist,
                                                                     const uint32_t *__restrict__ totals,
                                                                     uint32_t *__restrict__ keys_out,
                                                                     uint32_t *__restrict__ vals_out) {
-  constexpr int NW = kSortThreads / 32;
+  constexpr int NW = kSortThreads / 32, digits = 1 << BITS, DPT = digits > kSortThreads ? digits / kSortThreads : 1;
+  constexpr uint32_t mask = (uint32_t)digits - 1;
   extern __shared__ uint32_t sm[];
-  uint32_t *sk = sm, *sv = sm + kTile, *offset = sm + 2 * kTile, *count = offset + kMaxDigits;  // count[warp][digit]
+  uint32_t *sk = sm, *sv = sm + kTile, *offset = sm + 2 * kTile;
+  uint16_t *count = reinterpret_cast<uint16_t *>(offset + digits);  // [warp][digit]
   __shared__ uint32_t warp_totals[NW];
   grid_chain_enter();
-  constexpr int digits = 1 << BITS;
-  constexpr uint32_t mask = (uint32_t)digits - 1;
   const int tid = (int)threadIdx.x, lane = tid % 32, warp = tid / 32;
   for (int i = tid; i < NW * digits; i += kSortThreads) count[i] = 0;
   __syncthreads();
@@ -147,10 +169,9 @@ __global__ void __launch_bounds__(kSortThreads, 2) sort_move_kernel(Args a, Spli
 #pragma unroll
   for (int r = 0; r < kSortPerThread; ++r) {
     const uint32_t e = e0 + 32 * r;
-    key[r] = 0;
-    if (e < entries) key[r] = keys[e];
+    key[r] = e < entries ? keys[e] : 0;
   }
-  uint32_t *mine = count + warp * digits;
+  uint16_t *mine = count + warp * digits;
 #pragma unroll
   for (int r = 0; r < kSortPerThread; ++r) {
     const bool there = e0 + 32 * r < entries;
@@ -159,28 +180,55 @@ __global__ void __launch_bounds__(kSortThreads, 2) sort_move_kernel(Args a, Spli
     const uint32_t at = there ? mine[d] + (uint32_t)__popc(below) : 0;
     rank[r / 2] = r % 2 ? rank[r / 2] | at << 16 : at;
     __syncwarp();
-    if (there && below == 0) mine[d] += (uint32_t)__popc(peers);
+    if (there && below == 0) mine[d] = (uint16_t)(at + __popc(peers));
     __syncwarp();
   }
   __syncthreads();
-  uint32_t in_tile = 0, all;
-  if (tid < digits)
-    for (int w = 0; w < NW; ++w) {
-      const uint32_t c = count[w * digits + tid];
-      count[w * digits + tid] = in_tile;  // of the warps before
-      in_tile += c;
+  // the thread's digits: their entries in the warps before, in the tile, and where they go
+  const int d0 = tid * DPT;
+  uint32_t in_tile[DPT], sum = 0, all;
+#pragma unroll
+  for (int k = 0; k < DPT; ++k) {
+    in_tile[k] = 0;
+    if (d0 < digits)
+      for (int w = 0; w < NW; ++w) {
+        const uint32_t c = count[w * digits + d0 + k];
+        count[w * digits + d0 + k] = (uint16_t)in_tile[k];
+        in_tile[k] += c;
+      }
+    sum += in_tile[k];
+  }
+  uint32_t tile_base = block_prefix(sum, warp_totals, &all);
+  uint32_t total[DPT], before[DPT];  // in all tiles, in the tiles before
+  sum = 0;
+#pragma unroll
+  for (int k = 0; k < DPT; ++k) {
+    total[k] = before[k] = 0;
+    if (d0 < digits) {
+      const uint32_t *h = hist + (size_t)(d0 + k) * gridDim.x;
+      if (totals) {
+        total[k] = totals[d0 + k], before[k] = h[blockIdx.x];
+      } else {
+#pragma unroll 8
+        for (unsigned i = 0; i < gridDim.x; ++i) {
+          const uint32_t c = h[i];
+          total[k] += c;
+          before[k] += i < blockIdx.x ? c : 0;
+        }
+      }
     }
-  const uint32_t tile_base = block_prefix(in_tile, warp_totals, &all);
-  uint32_t global_base = tile_base;
-  if (hist) {
-    const uint32_t total = tid < digits ? totals[tid] : 0;
-    global_base = block_prefix(total, warp_totals, &all);
-    if (tid < digits) global_base += hist[(size_t)tid * gridDim.x + blockIdx.x];
+    sum += total[k];
   }
-  if (tid < digits) {
-    for (int w = 0; w < NW; ++w) count[w * digits + tid] += tile_base;
-    offset[tid] = global_base - tile_base;
-  }
+  uint32_t global_base = block_prefix(sum, warp_totals, &all);
+  if (d0 < digits)
+#pragma unroll
+    for (int k = 0; k < DPT; ++k) {
+      const int d = d0 + k;
+      for (int w = 0; w < NW; ++w) count[w * digits + d] += (uint16_t)tile_base;
+      offset[d] = global_base + before[k] - tile_base;
+      tile_base += in_tile[k];
+      global_base += total[k];
+    }
   __syncthreads();
 #pragma unroll
   for (int r = 0; r < kSortPerThread; ++r)
@@ -197,6 +245,89 @@ __global__ void __launch_bounds__(kSortThreads, 2) sort_move_kernel(Args a, Spli
     vals_out[at] = FIRST ? entry_val(a, by, sv[i]) : sv[i];
   }
 }
+// Few entries: the whole sort in one block, in shared memory.
+constexpr int kSmallThreads = 1024, kSmallPerThread = 8, kSmallEntries = kSmallThreads * kSmallPerThread, kSmallBits = 8;
+constexpr size_t kSmallSmem = 2 * kSmallEntries * sizeof(uint32_t) + ((kSmallThreads / 32) << kSmallBits) * sizeof(uint16_t);
+__global__ void __launch_bounds__(kSmallThreads) sort_small_kernel(Args a, Split by, uint32_t entries, int passes,
+                                                                   uint32_t *__restrict__ keys_out,
+                                                                   uint32_t *__restrict__ vals_out, uint32_t *__restrict__ range) {
+  constexpr int NW = kSmallThreads / 32, digits = 1 << kSmallBits;
+  extern __shared__ uint32_t sm[];
+  uint32_t *sk = sm, *sv = sm + kSmallEntries;
+  uint16_t *count = reinterpret_cast<uint16_t *>(sm + 2 * kSmallEntries);  // [warp][digit]
+  __shared__ uint32_t warp_totals[digits / 32];
+  grid_chain_enter();
+  const int tid = (int)threadIdx.x, lane = tid % 32, warp = tid / 32;
+  for (int64_t i = tid; i < 2 * (int64_t)a.items; i += kSmallThreads) range[i] = 0;
+  const uint32_t e0 = (uint32_t)warp * (32 * kSmallPerThread) + (uint32_t)lane, none = (uint32_t)a.items;
+  uint32_t key[kSmallPerThread], val[kSmallPerThread], rank[kSmallPerThread];
+#pragma unroll
+  for (int r = 0; r < kSmallPerThread; ++r) {
+    const uint32_t e = e0 + 32 * r;
+    key[r] = none, val[r] = 0;
+    if (e < entries) {
+      const uint32_t t = by(e);
+      const int target = row_target(a, (int)t);
+      if (target >= 0) key[r] = min((uint32_t)candidate(a, (int)t, target, (int)(e - t * (uint32_t)(a.n + 1))), none);
+      val[r] = entry_val(a, by, e);
+    }
+  }
+  uint16_t *mine = count + warp * digits;
+  for (int pass = 0; pass < passes; ++pass) {
+    const int shift = pass * kSmallBits;
+    for (int i = tid; i < NW * digits; i += kSmallThreads) count[i] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kSmallPerThread; ++r) {
+      const bool there = e0 + 32 * r < entries;
+      const uint32_t d = key[r] >> shift & (digits - 1);
+      const uint32_t peers = same_digit<kSmallBits>(d, there), below = peers & ((1u << lane) - 1);
+      rank[r] = mine[d] + (uint32_t)__popc(below);
+      __syncwarp();
+      if (there && below == 0) mine[d] = (uint16_t)(rank[r] + __popc(peers));
+      __syncwarp();
+    }
+    __syncthreads();
+    // a digit's entries in the warps before, and in the digits before
+    uint32_t sum = 0, s = 0;
+    if (tid < digits) {
+      for (int w = 0; w < NW; ++w) {
+        const uint32_t c = count[w * digits + tid];
+        count[w * digits + tid] = (uint16_t)sum;
+        sum += c;
+      }
+      s = sum;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t x = __shfl_up_sync(0xffffffffu, s, o);
+        if (lane >= o) s += x;
+      }
+      if (lane == 31) warp_totals[warp] = s;
+    }
+    __syncthreads();
+    if (tid < digits) {
+      s -= sum;
+      for (int w = 0; w < warp; ++w) s += warp_totals[w];
+      for (int w = 0; w < NW; ++w) count[w * digits + tid] += (uint16_t)s;  // (at most kSmallEntries)
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kSmallPerThread; ++r)
+      if (e0 + 32 * r < entries) {
+        const uint32_t at = mine[key[r] >> shift & (digits - 1)] + rank[r];
+        sk[at] = key[r];
+        sv[at] = val[r];
+      }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < kSmallPerThread; ++r)
+      if (e0 + 32 * r < entries) key[r] = sk[e0 + 32 * r], val[r] = sv[e0 + 32 * r];
+  }
+#pragma unroll
+  for (int r = 0; r < kSmallPerThread; ++r)
+    if (e0 + 32 * r < entries) keys_out[e0 + 32 * r] = key[r], vals_out[e0 + 32 * r] = val[r];
+}
+
 using MoveKernel = void (*)(Args, Split, const uint32_t *, const uint32_t *, uint32_t, int, const uint32_t *, const uint32_t *,
                             uint32_t *, uint32_t *);
 template <bool FIRST>
@@ -206,28 +337,31 @@ MoveKernel move_kernel(int bits) {
                                   sort_move_kernel<7, FIRST>, sort_move_kernel<8, FIRST>, sort_move_kernel<9, FIRST>};
   return k[bits - 1];
 }
-constexpr size_t kMoveSmem = (2 * kTile + kMaxDigits + kSortThreads / 32 * kMaxDigits) * sizeof(uint32_t);
+constexpr size_t move_smem(int bits) {
+  return 2 * kTile * sizeof(uint32_t) + ((size_t)1 << bits) * (sizeof(uint32_t) + kSortThreads / 32 * sizeof(uint16_t));
+}
 
 // ---- sums over an item's entries ---------------------------------------------------------------
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kItemsPerGroup = 2;
 
 template <typename T, int W, typename P>
-__global__ void __launch_bounds__(kThreads) loss_items_kernel(Args a, const T *__restrict__ hidden, const T *__restrict__ table,
-                                                              const float *__restrict__ lse, const float *__restrict__ grad_loss,
-                                                              const uint32_t *__restrict__ keys, const uint32_t *__restrict__ vals,
-                                                              uint32_t entries, int chunk, T *__restrict__ dtable,
-                                                              float *__restrict__ part, uint32_t *__restrict__ range) {
+__global__ void __launch_bounds__(kThreads, P::V == 1 ? 3 : P::V == 2 ? 2 : 1)
+    loss_items_kernel(Args a, const T *__restrict__ hidden, const T *__restrict__ table, const float *__restrict__ lse,
+                      const float *__restrict__ grad_loss, const uint32_t *__restrict__ keys, const uint32_t *__restrict__ vals,
+                      uint32_t entries, int chunk, T *__restrict__ dtable, float *__restrict__ part,
+                      uint32_t *__restrict__ range) {
   constexpr int LPC = P::LPC, V = P::V, U = V == 1 ? 4 : 1;
   grid_chain_enter();
-  const int col = (int)threadIdx.x % LPC;
-  const uint32_t lanes = LPC == 32 ? 0xffffffffu : ((1u << LPC) - 1) << ((threadIdx.x % 32) / LPC * LPC);
+  const int col = (int)threadIdx.x % LPC, base = (int)threadIdx.x % 32 / LPC * LPC;
+  const uint32_t lanes = LPC == 32 ? 0xffffffffu : ((1u << LPC) - 1) << base;
   const int64_t c = (int64_t)blockIdx.x * (kThreads / LPC) + threadIdx.x / LPC;
   if (c * chunk >= entries) return;
-  const uint32_t s = (uint32_t)(c * chunk), e = entries - s < (uint32_t)chunk ? entries : s + (uint32_t)chunk;
-  const float scale = grad_scale(a, lse, grad_loss);
+  const uint32_t none = (uint32_t)a.items, s = (uint32_t)(c * chunk);
+  const uint32_t e = entries - s < (uint32_t)chunk ? entries : s + (uint32_t)chunk;
   uint32_t cur = keys[s];
   bool open = s > 0 && keys[s - 1] == cur;  // the item's entries began in a chunk before
   bool first = true;
+  const bool writer = col == 0;
   Group w[V], acc[V];
   auto begin = [&](uint32_t item) {
     cur = item;
@@ -240,6 +374,7 @@ __global__ void __launch_bounds__(kThreads) loss_items_kernel(Args a, const T *_
     }
   };
   auto finish = [&](bool whole) {
+    const float scale = whole ? grad_scale(a, lse, grad_loss) : 1.f;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const int g = col + v * LPC, valid = a.cols - 8 * g;
@@ -252,51 +387,65 @@ __global__ void __launch_bounds__(kThreads) loss_items_kernel(Args a, const T *_
       }
     }
   };
-  const bool writer = col == 0;
-  if (writer && s > 0 && !open && keys[s - 1] < (uint32_t)a.items) range[a.items + keys[s - 1]] = s;
-  if (cur >= (uint32_t)a.items) return;
+  if (writer && s > 0 && !open && keys[s - 1] < none) range[none + keys[s - 1]] = s;
+  if (cur >= none) return;
   if (writer && !open) range[cur] = s;
   begin(cur);
-  for (uint32_t i = s; i < e; i += U) {
-    uint32_t key[U], val[U];
-    Group h[U][V];
-    float top[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      key[u] = i + u < e ? keys[i + u] : (uint32_t)a.items;
-      val[u] = i + u < e ? vals[i + u] : 0;
-      const bool there = key[u] < (uint32_t)a.items;
-      const int64_t t = val[u] & 0x7fffffffu;
-      top[u] = there ? lse[t] * kLog2e : 0.f;
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        const int g = col + v * LPC;
-        h[u][v] = load_group<T, W>(hidden + t * a.sh + 8 * g, there ? a.cols - 8 * g : 0);
-      }
+  // LPC entries, one a lane, the next ones under way
+  struct Entries {
+    uint32_t key, val;
+    float top;
+  };
+  auto entries_from = [&](uint32_t i) {
+    Entries x = {none, 0, 0.f};
+    if (i + col < e) {
+      x.key = keys[i + col], x.val = vals[i + col];
+      x.top = lse[x.val & 0x7fffffffu] * kLog2e;
     }
+    return x;
+  };
+  Entries next = entries_from(s);
+  for (uint32_t i0 = s; i0 < e; i0 += LPC) {
+    const Entries x = next;
+    if (i0 + LPC < e) next = entries_from(i0 + LPC);
+#pragma unroll 1
+    for (int k = 0; k < LPC && i0 + k < e; k += U) {
+      uint32_t key[U], val[U];
+      Group h[U][V];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (i + u >= e) break;
-      if (key[u] != cur) {
-        finish(!open);
-        open = first = false;
-        if (writer) range[a.items + cur] = i + u;
-        if (key[u] >= (uint32_t)a.items) return;  // (what follows is no candidate)
-        if (writer) range[key[u]] = i + u;
-        begin(key[u]);
+      for (int u = 0; u < U; ++u) {
+        key[u] = __shfl_sync(lanes, x.key, base + k + u);
+        val[u] = __shfl_sync(lanes, x.val, base + k + u);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          const int g = col + v * LPC;
+          h[u][v] = load_group<T, W>(hidden + (int64_t)(val[u] & 0x7fffffffu) * a.sh + 8 * g, key[u] < none ? a.cols - 8 * g : 0);
+        }
       }
-      float l = dot<V>(w, h[u]);
 #pragma unroll
-      for (int o = 1; o < LPC; o <<= 1) l += __shfl_xor_sync(lanes, l, o);
-      const float coef = exp2f(l - top[u]) - (val[u] >> 31 ? 1.f : 0.f);
+      for (int u = 0; u < U; ++u) {
+        if (i0 + k + u >= e) break;
+        if (key[u] != cur) {
+          finish(!open);
+          open = first = false;
+          if (writer) range[none + cur] = i0 + k + u;
+          if (key[u] >= none) return;  // (what follows is no candidate)
+          if (writer) range[key[u]] = i0 + k + u;
+          begin(key[u]);
+        }
+        float l = dot<V>(w, h[u]);
 #pragma unroll
-      for (int v = 0; v < V; ++v)
+        for (int o = 1; o < LPC; o <<= 1) l += __shfl_xor_sync(lanes, l, o);
+        const float coef = exp2f(l - __shfl_sync(lanes, x.top, base + k + u)) - (val[u] >> 31 ? 1.f : 0.f);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) acc[v].p[j] = fma2(both(coef), h[u][v].p[j], acc[v].p[j]);
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) acc[v].p[j] = fma2(both(coef), h[u][v].p[j], acc[v].p[j]);
+      }
     }
   }
   finish(!open && !(e < entries && keys[e] == cur));
-  if (writer && e == entries) range[a.items + cur] = e;
+  if (writer && e == entries) range[none + cur] = e;
 }
 
 // The same on the matrix units: a warp walks a chunk 16 entries at a time, their hidden rows the first operand, the item's
@@ -419,37 +568,59 @@ __global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 6 : 3)
   finish(!open && !(e < entries && keys[e] == cur));
 }
 
-// Items without entries (zeros) and those whose entries reach over a chunk's end: their chunks' sums, in order.  A group of
-// lanes an item; popular items are left to the whole block.
+// The last kernel: blocks up to `join_ctas` finish the table's gradient, those behind them scale that of the hidden rows
+// (g / count * grad_hidden, rounded once).
+// Table: items without entries (zeros) and those whose entries reach over a chunk's end: their chunks' sums, in order.  A
+// group of lanes takes two items one after another; items of many chunks are left to the whole block.
 template <typename T, int W, typename P>
 __global__ void __launch_bounds__(kThreads) loss_join_kernel(Args a, const float *__restrict__ lse,
                                                              const float *__restrict__ grad_loss,
                                                              const uint32_t *__restrict__ ranges, uint32_t entries, int chunk,
-                                                             const float *__restrict__ part, T *__restrict__ dtable) {
-  constexpr int LPC = P::LPC, V = P::V, NG = kThreads / LPC, WF = W < 4 ? W : 4;
+                                                             const float *__restrict__ part, T *__restrict__ dtable,
+                                                             unsigned join_ctas, const float *__restrict__ grad_hidden,
+                                                             T *__restrict__ dhidden) {
+  constexpr int LPC = P::LPC, V = P::V, NG = kThreads / LPC, CPW = 32 / LPC, WF = W < 4 ? W : 4;
+  constexpr int kRounds = kItemsPerGroup, kItems = NG * kRounds;  // of a block
   constexpr uint32_t kAlone = 16;  // chunks that a group of lanes adds up by itself
-  __shared__ uint2 range[NG];
+  __shared__ uint2 popular[kItems];  // their first and last chunk
+  __shared__ int popular_item[kItems];  // and which they are, bit 30: as `inside` below
+  __shared__ int populars;
   __shared__ float sums[NG][LPC * V * 8];
   grid_chain_enter();
-  const int col = (int)threadIdx.x % LPC, grp = (int)threadIdx.x / LPC;
-  const float scale = grad_scale(a, lse, grad_loss);
-  const int64_t item = (int64_t)blockIdx.x * NG + grp;
-  if (col == 0) {
-    uint2 r = make_uint2(0, 0);
-    if (item < a.items && entries) r = make_uint2(ranges[item], ranges[a.items + item]);
-    range[grp] = r;
+  const int lane = (int)threadIdx.x % 32, col = lane % LPC, sub = lane / LPC, grp = (int)threadIdx.x / LPC;
+  if (blockIdx.x >= join_ctas) {
+    const float scale = grad_scale(a, lse, grad_loss);
+    const int64_t step = (int64_t)(gridDim.x - join_ctas) * NG;
+    for (int64_t row = (int64_t)(blockIdx.x - join_ctas) * NG + grp; row < a.rows; row += step) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        const int g = col + v * LPC, valid = a.cols - 8 * g;
+        Group x = load_group<float, WF>(grad_hidden + row * a.cols + 8 * g, valid);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x.p[i] = mul2(x.p[i], both(scale));
+        store_group<T, W>(dhidden + row * a.sdh + 8 * g, valid, x);
+      }
+    }
+    return;
   }
+  if (threadIdx.x == 0) populars = 0;
   __syncthreads();
-  // the sum of every `step`-th chunk of a range, from its `from`-th on
-  auto add_up = [&](uint2 r, uint32_t from, uint32_t step, Group (&acc)[V]) {
-    const uint32_t c0 = r.x / (uint32_t)chunk, c1 = (r.y - 1) / (uint32_t)chunk;
+  const float scale = grad_scale(a, lse, grad_loss);
+  const int64_t item0 = (int64_t)blockIdx.x * kItems + threadIdx.x / 32 * (CPW * kRounds);  // of the warp, one a lane
+  uint2 range = make_uint2(0, 0);
+  if (lane < CPW * kRounds && item0 + lane < a.items && entries)
+    range = make_uint2(ranges[item0 + lane], ranges[a.items + item0 + lane]);
+  const uint32_t c0 = range.x / (uint32_t)chunk, c1 = range.y ? (range.y - 1) / (uint32_t)chunk : 0;
+  const uint32_t n = range.x == range.y ? 0 : c1 - c0 + 1;
+  // the sum of every `step`-th chunk's share, from the `from`-th on
+  auto add_up = [&](uint32_t c0, uint32_t c1, bool inside, uint32_t from, uint32_t step, Group (&acc)[V]) {
 #pragma unroll
     for (int v = 0; v < V; ++v)
 #pragma unroll
       for (int i = 0; i < 4; ++i) acc[v].p[i] = both(0.f);
 #pragma unroll 4
     for (uint32_t c = c0 + from; c <= c1; c += step) {
-      const int64_t slot = (int64_t)c * 2 + (c == c0 && r.x % (uint32_t)chunk ? 1 : 0);
+      const int64_t slot = (int64_t)c * 2 + (c == c0 && inside ? 1 : 0);
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         const int g = col + v * LPC;
@@ -459,7 +630,6 @@ __global__ void __launch_bounds__(kThreads) loss_join_kernel(Args a, const float
       }
     }
   };
-  auto chunks_of = [&](uint2 r) { return r.x == r.y ? 0u : (r.y - 1) / (uint32_t)chunk - r.x / (uint32_t)chunk + 1; };
   auto write = [&](int64_t to, Group (&acc)[V]) {
 #pragma unroll
     for (int v = 0; v < V; ++v) {
@@ -469,26 +639,35 @@ __global__ void __launch_bounds__(kThreads) loss_join_kernel(Args a, const float
       store_group<T, W>(dtable + to * a.sdt + 8 * g, a.cols - 8 * g, acc[v]);
     }
   };
+  const bool inside = range.x % (uint32_t)chunk != 0;  // the first chunk's share is that of its last item
   Group acc[V];
-  {
-    const uint2 r = range[grp];
-    const uint32_t n = chunks_of(r);
-    if (item < a.items && n != 1 && n <= kAlone) {  // (one chunk: written by the kernel before)
-      if (n == 0) {
+#pragma unroll 1
+  for (int k = 0; k < kRounds; ++k) {
+    const int from = k * CPW + sub;
+    const uint32_t many = __shfl_sync(0xffffffffu, n, from);
+    const uint32_t b0 = __shfl_sync(0xffffffffu, c0, from), b1 = __shfl_sync(0xffffffffu, c1, from);
+    const bool in = __shfl_sync(0xffffffffu, (int)inside, from);
+    if (item0 + from >= a.items || many == 1 || many > kAlone) continue;  // (one chunk: written by the kernel before)
+    if (many) {
+      add_up(b0, b1, in, 0, 1, acc);
+    } else {
 #pragma unroll
-        for (int v = 0; v < V; ++v)
+      for (int v = 0; v < V; ++v)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) acc[v].p[i] = both(0.f);
-      } else {
-        add_up(r, 0, 1, acc);
-      }
-      write(item, acc);
+        for (int i = 0; i < 4; ++i) acc[v].p[i] = both(0.f);
     }
+    write(item0 + from, acc);
   }
-  for (int k = 0; k < NG; ++k) {
-    const uint2 r = range[k];
-    if (chunks_of(r) <= kAlone) continue;  // (the same for the whole block)
-    add_up(r, (uint32_t)grp, NG, acc);
+  if (n > kAlone) {  // (in which order they are noted does not matter: each is summed by itself)
+    const int at = atomicAdd(&populars, 1);
+    popular[at] = make_uint2(c0, c1);
+    popular_item[at] = (int)threadIdx.x / 32 * (CPW * kRounds) + lane + (inside ? 1 << 30 : 0);
+  }
+  __syncthreads();
+  const int count = populars;
+  for (int k = 0; k < count; ++k) {
+    const uint2 r = popular[k];
+    add_up(r.x, r.y, popular_item[k] >> 30 & 1, (uint32_t)grp, NG, acc);
 #pragma unroll
     for (int v = 0; v < V; ++v)
 #pragma unroll
@@ -500,7 +679,7 @@ __global__ void __launch_bounds__(kThreads) loss_join_kernel(Args a, const float
         for (int v = 0; v < V; ++v)
 #pragma unroll
           for (int i = 0; i < 8; ++i) acc[v].at(i) += sums[g][8 * (col + v * LPC) + i];
-      write((int64_t)blockIdx.x * NG + k, acc);
+      write((int64_t)blockIdx.x * kItems + (popular_item[k] & 0xffff), acc);
     }
     __syncthreads();
   }
@@ -547,42 +726,51 @@ Scratch carve(const Args &a, void *base) {
   return s;
 }
 
-int launch_items(const Args &a, int dtype, const void *hidden, const void *table, const float *lse, const float *grad_loss,
-                 void *dtable, int width, const Scratch &s, cudaStream_t st) {
+int launch_items(const Args &a, int dtype, const void *hidden, const void *table, const float *lse, const float *grad_hidden,
+                 const float *grad_loss, void *dhidden, void *dtable, int width, const Scratch &s, cudaStream_t st) {
   const int lines = mma_lines(a, dtype, width);
   const SortPlan p = sort_plan(a, lines ? 32 : lanes_of(a.groups));
-  const uint32_t entries = (uint32_t)p.entries;
+  const uint32_t entries = dtable ? (uint32_t)p.entries : 0;
   const Split by = split_by((uint32_t)a.n + 1);
   int at = 1;  // the buffer that holds the list
-  const MoveKernel moves[2] = {move_kernel<true>(p.bits), move_kernel<false>(p.bits)};
-  if (!allow_smem(moves[0], kMoveSmem) || !allow_smem(moves[1], kMoveSmem)) return BLOSSOM_ERR_CUDA;
-  for (int i = 0; entries && i < p.passes; ++i) {
-    const int shift = i * p.bits, to = at ^ 1;
-    uint32_t *hist = p.tiles > 1 ? s.hist : nullptr;
-    const dim3 grid((unsigned)p.tiles), block(kSortThreads);
-    if (hist || i == 0) {  // (the first makes the keys too)
-      LaunchScope ls(K_LOSS_SORT, st);
-      launch_chained(i ? sort_count_kernel<false> : sort_count_kernel<true>, grid, block, 0, st, a, by, s.keys[at], entries,
-                     shift, p.bits, s.hist, s.range);
-    }
-    if (hist) {
-      LaunchScope ls(K_LOSS_SORT, st);
-      launch_chained(sort_scan_kernel, dim3(1u << p.bits), block, 0, st, hist, (int)p.tiles, s.totals);
-    }
+  if (entries && entries <= (uint32_t)kSmallEntries) {
+    if (!allow_smem(sort_small_kernel, kSmallSmem)) return BLOSSOM_ERR_CUDA;
     LaunchScope ls(K_LOSS_SORT, st);
-    launch_chained(moves[i > 0], grid, block, kMoveSmem, st, a, by, (const uint32_t *)s.keys[at],
-                   (const uint32_t *)s.vals[at], entries, shift, (const uint32_t *)hist,
-                   (const uint32_t *)s.totals, s.keys[to], s.vals[to]);
-    at = to;
+    launch_chained(sort_small_kernel, dim3(1), dim3(kSmallThreads), kSmallSmem, st, a, by, entries,
+                   (p.passes * p.bits + kSmallBits - 1) / kSmallBits, s.keys[at], s.vals[at], s.range);
+  } else if (entries) {
+    const MoveKernel moves[2] = {move_kernel<true>(p.bits), move_kernel<false>(p.bits)};
+    const size_t smem = move_smem(p.bits);
+    const bool scan = p.tiles > kTilesWithoutScan;
+    const dim3 grid((unsigned)p.tiles), block(kSortThreads);
+    if (!allow_smem(moves[0], smem) || !allow_smem(moves[1], smem)) return BLOSSOM_ERR_CUDA;
+    for (int i = 0; i < p.passes; ++i) {
+      const int shift = i * p.bits, to = at ^ 1;
+      {
+        LaunchScope ls(K_LOSS_SORT, st);
+        launch_chained(i ? sort_count_kernel<false> : sort_count_kernel<true>, grid, block, 0, st, a, by, s.keys[at], entries,
+                       shift, p.bits, s.hist, s.range);
+      }
+      if (scan) {
+        LaunchScope ls(K_LOSS_SORT, st);
+        launch_chained(sort_scan_kernel, dim3(1u << p.bits), block, 0, st, s.hist, (int)p.tiles, s.totals);
+      }
+      LaunchScope ls(K_LOSS_SORT, st);
+      launch_chained(moves[i > 0], grid, block, smem, st, a, by, (const uint32_t *)s.keys[at], (const uint32_t *)s.vals[at],
+                     entries, shift, (const uint32_t *)s.hist, scan ? (const uint32_t *)s.totals : (const uint32_t *)nullptr,
+                     s.keys[to], s.vals[to]);
+      at = to;
+    }
   }
   const uint32_t *keys = s.keys[at], *vals = s.vals[at];
   if (entries && lines) {
     with_lines(lines, a.cols, [&](auto n, auto all) {
       constexpr int NL = decltype(n)::value, per = kMmaThreads / 32;
       LaunchScope ls(K_LOSS_ITEMS, st);
-      launch_chained(loss_items_mma_kernel<NL, decltype(all)::value>, dim3((unsigned)((p.chunks + per - 1) / per)), dim3(kMmaThreads), 0, st,
-                     a, static_cast<const __nv_bfloat16 *>(hidden), static_cast<const __nv_bfloat16 *>(table), lse, grad_loss,
-                     keys, vals, entries, p.chunk, static_cast<__nv_bfloat16 *>(dtable), s.part, s.range);
+      launch_chained(loss_items_mma_kernel<NL, decltype(all)::value>, dim3((unsigned)((p.chunks + per - 1) / per)),
+                     dim3(kMmaThreads), 0, st, a, static_cast<const __nv_bfloat16 *>(hidden),
+                     static_cast<const __nv_bfloat16 *>(table), lse, grad_loss, keys, vals, entries, p.chunk,
+                     static_cast<__nv_bfloat16 *>(dtable), s.part, s.range);
     });
   }
   with_plan(a.groups, [&](auto plan) {
@@ -596,10 +784,14 @@ int launch_items(const Args &a, int dtype, const void *hidden, const void *table
                        static_cast<const T *>(hidden), static_cast<const T *>(table), lse, grad_loss, keys, vals, entries,
                        p.chunk, static_cast<T *>(dtable), s.part, s.range);
       }
-      LaunchScope ls(K_LOSS_ITEMS, st);
-      launch_chained(loss_join_kernel<T, W, P>, dim3((unsigned)(((int64_t)a.items + per - 1) / per)), dim3(kThreads), 0, st, a,
-                     lse, grad_loss, (const uint32_t *)s.range, entries, p.chunk, (const float *)s.part,
-                     static_cast<T *>(dtable));
+      const int64_t items = per * kItemsPerGroup, join = dtable ? (a.items + items - 1) / items : 0;
+      const int64_t rows = dhidden ? ((int64_t)a.rows + per - 1) / per : 0, most = kSMs * 8;
+      const int64_t ctas = join + (rows < most ? rows : most);
+      if (ctas == 0) return;
+      LaunchScope ls(K_LOSS_JOIN, st);
+      launch_chained(loss_join_kernel<T, W, P>, dim3((unsigned)ctas), dim3(kThreads), 0, st, a, lse, grad_loss,
+                     (const uint32_t *)s.range, entries, p.chunk, (const float *)s.part, static_cast<T *>(dtable),
+                     (unsigned)join, grad_hidden, static_cast<T *>(dhidden));
     });
   });
   return cudaGetLastError() == cudaSuccess ? BLOSSOM_OK : BLOSSOM_ERR_CUDA;

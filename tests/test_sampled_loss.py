@@ -83,7 +83,8 @@ def make(rows, cols, items, n, dtype, seed, ids="int64", noise=True, shared=Fals
 SHAPES = [(1, 64, 10, 1), (1, 1, 1, 0), (2, 3, 2, 5), (5, 8, 3, 7), (64, 64, 50001, 100), (300, 50, 1000, 31), (130, 32, 513, 9),
           (97, 33, 511, 32), (200, 128, 70000, 64), (33, 256, 200, 40), (20, 257, 99, 33), (9, 512, 30, 12), (21, 520, 30, 5),
           (6, 1024, 40, 70), (700, 64, 5000, 63), (4000, 16, 7, 20), (600, 24, 300001, 33), (1170, 64, 255, 6), (1171, 64, 256, 6),
-          (3000, 8, 2, 3), (2500, 65, 40, 12)]
+          (3000, 8, 2, 3), (2500, 65, 40, 12),
+          (9000, 16, 3000, 31), (9000, 8, 300001, 31), (65, 128, 700, 9), (129, 128, 30, 130)]
 
 
 @pytest.mark.gpu
@@ -382,7 +383,8 @@ def test_arguments_are_checked_before_any_launch():
     for bad, rc in ((dict(rows=-1), 1), (dict(cols=0), 1), (dict(cols=1025), 2), (dict(items=0), 1), (dict(items=1 << 30), 2),
                     (dict(negatives=-1), 1), (dict(dtype=4), 1), (dict(index_bytes=2), 1), (dict(mask_hits=2), 1),
                     (dict(hidden_stride=63), 1), (dict(table_stride=-64), 1), (dict(dhidden_stride=1), 1), (dict(dtable_stride=1), 1),
-                    (dict(negatives_stride=-1), 1), (dict(rows=1 << 31), 2), (dict(rows=1 << 29, negatives=3), 2)):
+                    (dict(negatives_stride=-1), 1), (dict(rows=1 << 31), 2), (dict(rows=1 << 29, negatives=3), 2),
+                    (dict(negatives_stride=1 << 31), 2)):
         p = good(**bad)
         assert E.blossom_sampled_loss_workspace_bytes(p) == 0, bad
         assert E.blossom_sampled_loss_fwd(p, A, A, A, A, A, A, A, A, 1 << 40, stream=0, check=False) == rc, bad
