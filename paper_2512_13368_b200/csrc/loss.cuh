@@ -8,9 +8,7 @@ namespace loss {
 using rows::kSMs;
 using rows::both;
 using rows::Group;
-using rows::load_group;
 using rows::mul2;
-using rows::store_group;
 
 constexpr int kMaxCols = 1024, kMaxRowCtas = kSMs * 16, kMmaThreads = 128;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -27,17 +25,21 @@ __device__ __forceinline__ int64_t load_id(const void *p, int64_t i, int idx8) {
   return idx8 ? static_cast<const int64_t *>(p)[i] : static_cast<const int32_t *>(p)[i];
 }
 // the row's target, or -1 if the row takes no part
-__device__ __forceinline__ int row_target(const Args &a, int row) {
-  const int64_t t = load_id(a.targets, row, a.idx8);
+__device__ __forceinline__ int valid_target(const Args &a, int64_t t) {
   return (uint64_t)t < (uint64_t)a.items && t != a.ignore ? (int)t : -1;
 }
-// candidate j of a row that takes part (j = 0: its target), or -1 if it is none
-__device__ __forceinline__ int candidate(const Args &a, int row, int target, int j) {
-  if (j == 0) return target;
-  const int64_t i = load_id(a.negatives, (int64_t)((uint64_t)(uint32_t)row * a.sn + (uint32_t)(j - 1)), a.idx8);
+__device__ __forceinline__ int row_target(const Args &a, int row) { return valid_target(a, load_id(a.targets, row, a.idx8)); }
+// candidate j >= 1 of a row that takes part, or -1 if it is none
+__device__ __forceinline__ int64_t load_negative(const Args &a, int row, int j) {
+  return load_id(a.negatives, (int64_t)((uint64_t)(uint32_t)row * a.sn + (uint32_t)(j - 1)), a.idx8);
+}
+__device__ __forceinline__ int valid_negative(const Args &a, int target, int64_t i) {
   return (uint64_t)i < (uint64_t)a.items && !(a.hits && i == target) ? (int)i : -1;
 }
-
+// candidate j of a row that takes part (j = 0: its target)
+__device__ __forceinline__ int candidate(const Args &a, int row, int target, int j) {
+  return j == 0 ? target : valid_negative(a, target, load_negative(a, row, j));
+}
 // the lane's share of <a, b>
 template <int V>
 __device__ __forceinline__ float dot(const Group (&a)[V], const Group (&b)[V]) {
@@ -48,6 +50,51 @@ __device__ __forceinline__ float dot(const Group (&a)[V], const Group (&b)[V]) {
     for (int i = 0; i < 4; ++i) s[i & 1] = fma2(a[v].p[i], b[v].p[i], s[i & 1]);
   const float2 t = add2(s[0], s[1]);
   return t.x + t.y;
+}
+
+// A row over LPC lanes, V times 8 columns a lane: access by access the lanes lie side by side (which columns are whose does not
+// matter here), so that narrow accesses of odd rows still touch whole sectors.
+template <typename T, int W, typename P>
+struct Strip {
+  static __device__ __forceinline__ int column(int lane, int v, int j) { return W * (lane + P::LPC * (j / W + v * (8 / W))); }
+  static __device__ __forceinline__ rows::Raw<T, W> raw(const T *row, int lane, int v, int cols, bool there = true) {
+    rows::Raw<T, W> r;
+#pragma unroll
+    for (int j = 0; j < 8; j += W) r.piece(row + column(lane, v, j), j, there && column(lane, v, j) < cols);
+    return r;
+  }
+  static __device__ __forceinline__ Group load(const T *row, int lane, int v, int cols, bool there = true) {
+    return raw(row, lane, v, cols, there).get();
+  }
+  static __device__ __forceinline__ void store(T *row, int lane, int v, int cols, const Group &g) {
+    Group x = g;
+#pragma unroll
+    for (int j = 0; j < 8; j += W)
+      if (column(lane, v, j) < cols) rows::store_piece<T, W>(row + column(lane, v, j), j, x);
+  }
+};
+
+// Single-precision sums in the columns that a strip of W elements an access has (of 8: two accesses).
+template <int W, typename P>
+__device__ __forceinline__ void store_sums(float *row, int lane, int v, int cols, const Group &g) {
+  Group x = g;
+  constexpr int WF = W < 4 ? W : 4;
+#pragma unroll
+  for (int j = 0; j < 8; j += WF) {
+    const int c = Strip<float, W, P>::column(lane, v, j / W * W) + j % W;
+    if (c < cols) rows::store_piece<float, WF>(row + c, j, x);
+  }
+}
+template <int W, typename P>
+__device__ __forceinline__ Group load_sums(const float *row, int lane, int v, int cols) {
+  rows::Raw<float, (W < 4 ? W : 4)> r;
+  constexpr int WF = W < 4 ? W : 4;
+#pragma unroll
+  for (int j = 0; j < 8; j += WF) {
+    const int c = Strip<float, W, P>::column(lane, v, j / W * W) + j % W;
+    r.piece(row + c, j, c < cols);
+  }
+  return r.get();
 }
 
 // LPC lanes hold a row, V groups of 8 columns each
@@ -114,9 +161,15 @@ struct Lanes16 {
 };
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                          uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma16816_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                               uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 // l[j] = <row 4 j + r, v>
 template <int NL>
@@ -124,11 +177,13 @@ __device__ __forceinline__ void dots16(const Rows16<NL> &r, const uint4 (&v)[NL]
   const bool odd = threadIdx.x & 4;
 #pragma unroll
   for (int j = 0; j < 4; j += 2) {
-    float d[4] = {0.f, 0.f, 0.f, 0.f};
+    float d[4];
 #pragma unroll
     for (int c = 0; c < NL; ++c) {
-      mma16816(d, r.w[j][c].x, r.w[j + 1][c].x, r.w[j][c].y, r.w[j + 1][c].y, v[c].x, v[c].y);
-      mma16816(d, r.w[j][c].z, r.w[j + 1][c].z, r.w[j][c].w, r.w[j + 1][c].w, v[c].z, v[c].w);
+      const uint4 x = r.w[j][c], y = r.w[j + 1][c];
+      if (c == 0) mma16816_first(d, x.x, y.x, x.y, y.y, v[c].x, v[c].y);
+      else mma16816(d, x.x, y.x, x.y, y.y, v[c].x, v[c].y);
+      mma16816(d, x.z, y.z, x.w, y.w, v[c].z, v[c].w);
     }
     l[j] = odd ? d[1] : d[0];
     l[j + 1] = odd ? d[3] : d[2];
@@ -190,7 +245,7 @@ struct Scratch {
   double2 *sums;                 // [kMaxRowCtas] loss and number of rows of a CTA
   uint32_t *keys[2], *vals[2];   // [entries] item and position (top bit: it is the target) of every candidate, being sorted
   uint32_t *hist, *totals;       // [digits][tiles], [digits]
-  uint32_t *range;               // [2][items] where an item's entries start and end in the sorted list (0, 0: it has none)
+  uint32_t *range;               // [2][items] where an item's entries start and end in the sorted list; not written for others
   float *part;                   // [chunks][2][cols] sums of items that reach over the end of a chunk
   size_t bytes;
 };

@@ -35,8 +35,7 @@ __device__ __forceinline__ uint32_t entry_val(const Args &a, const Split &by, ui
 // Counts of a tile's digits, to hist[digit][tile].  The first pass makes the keys.
 template <bool FIRST>
 __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(Args a, Split by, uint32_t *__restrict__ keys, uint32_t entries,
-                                                                  int shift, int bits, uint32_t *__restrict__ hist,
-                                                                  uint32_t *__restrict__ range) {
+                                                                  int shift, int bits, uint32_t *__restrict__ hist) {
   __shared__ uint32_t count[kMaxDigits];
   __shared__ int targets[FIRST ? kTile + 1 : 1];  // of the positions that the tile belongs to
   grid_chain_enter();
@@ -48,8 +47,6 @@ __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(Args a, Split 
     t0 = by(tile0);
     const uint32_t last = by((entries - tile0 < (uint32_t)kTile ? entries : tile0 + kTile) - 1);
     for (uint32_t t = t0 + (uint32_t)tid; t <= last; t += kSortThreads) targets[t - t0] = row_target(a, (int)t);
-    for (int64_t i = (int64_t)blockIdx.x * kSortThreads + tid; i < 2 * (int64_t)a.items; i += (int64_t)gridDim.x * kSortThreads)
-      range[i] = 0;
   }
   __syncthreads();
   uint32_t key[kSortPerThread];
@@ -250,15 +247,14 @@ constexpr int kSmallThreads = 1024, kSmallPerThread = 8, kSmallEntries = kSmallT
 constexpr size_t kSmallSmem = 2 * kSmallEntries * sizeof(uint32_t) + ((kSmallThreads / 32) << kSmallBits) * sizeof(uint16_t);
 __global__ void __launch_bounds__(kSmallThreads) sort_small_kernel(Args a, Split by, uint32_t entries, int passes,
                                                                    uint32_t *__restrict__ keys_out,
-                                                                   uint32_t *__restrict__ vals_out, uint32_t *__restrict__ range) {
-  constexpr int NW = kSmallThreads / 32, digits = 1 << kSmallBits;
+                                                                   uint32_t *__restrict__ vals_out) {
+  constexpr int digits = 1 << kSmallBits;
   extern __shared__ uint32_t sm[];
   uint32_t *sk = sm, *sv = sm + kSmallEntries;
   uint16_t *count = reinterpret_cast<uint16_t *>(sm + 2 * kSmallEntries);  // [warp][digit]
   __shared__ uint32_t warp_totals[digits / 32];
   grid_chain_enter();
   const int tid = (int)threadIdx.x, lane = tid % 32, warp = tid / 32;
-  for (int64_t i = tid; i < 2 * (int64_t)a.items; i += kSmallThreads) range[i] = 0;
   const uint32_t e0 = (uint32_t)warp * (32 * kSmallPerThread) + (uint32_t)lane, none = (uint32_t)a.items;
   uint32_t key[kSmallPerThread], val[kSmallPerThread], rank[kSmallPerThread];
 #pragma unroll
@@ -273,12 +269,14 @@ __global__ void __launch_bounds__(kSmallThreads) sort_small_kernel(Args a, Split
     }
   }
   uint16_t *mine = count + warp * digits;
+  const int nw = (int)((entries + 32 * kSmallPerThread - 1) / (32 * kSmallPerThread));  // warps that have entries
   for (int pass = 0; pass < passes; ++pass) {
     const int shift = pass * kSmallBits;
-    for (int i = tid; i < NW * digits; i += kSmallThreads) count[i] = 0;
+    for (int i = tid; i < nw * digits; i += kSmallThreads) count[i] = 0;
     __syncthreads();
 #pragma unroll
     for (int r = 0; r < kSmallPerThread; ++r) {
+      if (warp >= nw) break;
       const bool there = e0 + 32 * r < entries;
       const uint32_t d = key[r] >> shift & (digits - 1);
       const uint32_t peers = same_digit<kSmallBits>(d, there), below = peers & ((1u << lane) - 1);
@@ -291,7 +289,7 @@ __global__ void __launch_bounds__(kSmallThreads) sort_small_kernel(Args a, Split
     // a digit's entries in the warps before, and in the digits before
     uint32_t sum = 0, s = 0;
     if (tid < digits) {
-      for (int w = 0; w < NW; ++w) {
+      for (int w = 0; w < nw; ++w) {
         const uint32_t c = count[w * digits + tid];
         count[w * digits + tid] = (uint16_t)sum;
         sum += c;
@@ -308,7 +306,7 @@ __global__ void __launch_bounds__(kSmallThreads) sort_small_kernel(Args a, Split
     if (tid < digits) {
       s -= sum;
       for (int w = 0; w < warp; ++w) s += warp_totals[w];
-      for (int w = 0; w < NW; ++w) count[w * digits + tid] += (uint16_t)s;  // (at most kSmallEntries)
+      for (int w = 0; w < nw; ++w) count[w * digits + tid] += (uint16_t)s;  // (at most kSmallEntries)
     }
     __syncthreads();
 #pragma unroll
@@ -342,15 +340,19 @@ constexpr size_t move_smem(int bits) {
 }
 
 // ---- sums over an item's entries ---------------------------------------------------------------
-constexpr int kThreads = 256, kItemsPerGroup = 2;
+constexpr int kThreads = 256, kItemsPerGroup = 2, kDense = 8;
 
-template <typename T, int W, typename P>
-__global__ void __launch_bounds__(kThreads, P::V == 1 ? 3 : P::V == 2 ? 2 : 1)
+// DENSE: an item has several entries, its row of the table stays in registers.  Otherwise the table's rows are read entry by entry
+// like the hidden ones: one that waits for its item to begin would be a memory latency in front of nearly every entry
+// (4000 entries of 3000 items: 23 us against 7).
+template <typename T, int W, typename P, bool DENSE>
+__global__ void __launch_bounds__(kThreads, P::V <= 2 ? 2 : 1)
     loss_items_kernel(Args a, const T *__restrict__ hidden, const T *__restrict__ table, const float *__restrict__ lse,
                       const float *__restrict__ grad_loss, const uint32_t *__restrict__ keys, const uint32_t *__restrict__ vals,
                       uint32_t entries, int chunk, T *__restrict__ dtable, float *__restrict__ part,
                       uint32_t *__restrict__ range) {
-  constexpr int LPC = P::LPC, V = P::V, U = V == 1 ? 4 : 1;
+  using S = Strip<T, W, P>;
+  constexpr int LPC = P::LPC, V = P::V, U = V > 1 ? 1 : DENSE || sizeof(T) == 2 ? 4 : 2;
   grid_chain_enter();
   const int col = (int)threadIdx.x % LPC, base = (int)threadIdx.x % 32 / LPC * LPC;
   const uint32_t lanes = LPC == 32 ? 0xffffffffu : ((1u << LPC) - 1) << base;
@@ -358,36 +360,35 @@ __global__ void __launch_bounds__(kThreads, P::V == 1 ? 3 : P::V == 2 ? 2 : 1)
   if (c * chunk >= entries) return;
   const uint32_t none = (uint32_t)a.items, s = (uint32_t)(c * chunk);
   const uint32_t e = entries - s < (uint32_t)chunk ? entries : s + (uint32_t)chunk;
+  const float scale = grad_scale(a, lse, grad_loss);
   uint32_t cur = keys[s];
-  bool open = s > 0 && keys[s - 1] == cur;  // the item's entries began in a chunk before
+  const uint32_t before = s > 0 ? keys[s - 1] : none;
+  bool open = s > 0 && before == cur;  // the item's entries began in a chunk before
   bool first = true;
   const bool writer = col == 0;
-  Group w[V], acc[V];
+  Group acc[V], own[V];
   auto begin = [&](uint32_t item) {
     cur = item;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const int g = col + v * LPC;
-      w[v] = load_group<T, W>(table + cur * a.st + 8 * g, a.cols - 8 * g);
+      if (DENSE) own[v] = S::load(table + item * a.st, col, v, a.cols);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) acc[v].p[i] = both(0.f), w[v].p[i] = mul2(w[v].p[i], both(kLog2e));
+      for (int i = 0; i < 4; ++i) acc[v].p[i] = both(0.f);
     }
   };
   auto finish = [&](bool whole) {
-    const float scale = whole ? grad_scale(a, lse, grad_loss) : 1.f;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const int g = col + v * LPC, valid = a.cols - 8 * g;
       if (whole) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[v].p[i] = mul2(acc[v].p[i], both(scale));
-        store_group<T, W>(dtable + cur * a.sdt + 8 * g, valid, acc[v]);
+        S::store(dtable + cur * a.sdt, col, v, a.cols, acc[v]);
       } else {
-        store_group<float, (W < 4 ? W : 4)>(part + (c * 2 + (first ? 0 : 1)) * a.cols + 8 * g, valid, acc[v]);
+        store_sums<W, P>(part + (c * 2 + (first ? 0 : 1)) * a.cols, col, v, a.cols, acc[v]);
       }
     }
   };
-  if (writer && s > 0 && !open && keys[s - 1] < none) range[none + keys[s - 1]] = s;
+  if (writer && s > 0 && !open && before < none) range[none + before] = s;
   if (cur >= none) return;
   if (writer && !open) range[cur] = s;
   begin(cur);
@@ -411,15 +412,15 @@ __global__ void __launch_bounds__(kThreads, P::V == 1 ? 3 : P::V == 2 ? 2 : 1)
 #pragma unroll 1
     for (int k = 0; k < LPC && i0 + k < e; k += U) {
       uint32_t key[U], val[U];
-      Group h[U][V];
+      rows::Raw<T, W> h[U][V], w[U][V];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         key[u] = __shfl_sync(lanes, x.key, base + k + u);
         val[u] = __shfl_sync(lanes, x.val, base + k + u);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-          const int g = col + v * LPC;
-          h[u][v] = load_group<T, W>(hidden + (int64_t)(val[u] & 0x7fffffffu) * a.sh + 8 * g, key[u] < none ? a.cols - 8 * g : 0);
+          h[u][v] = S::raw(hidden + (int64_t)(val[u] & 0x7fffffffu) * a.sh, col, v, a.cols, key[u] < none);
+          if (!DENSE) w[u][v] = S::raw(table + key[u] * a.st, col, v, a.cols, key[u] < none);
         }
       }
 #pragma unroll
@@ -433,14 +434,20 @@ __global__ void __launch_bounds__(kThreads, P::V == 1 ? 3 : P::V == 2 ? 2 : 1)
           if (writer) range[key[u]] = i0 + k + u;
           begin(key[u]);
         }
-        float l = dot<V>(w, h[u]);
+        Group hg[V], wg[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          hg[v] = h[u][v].get();
+          wg[v] = DENSE ? own[v] : w[u][v].get();
+        }
+        float l = dot<V>(wg, hg);
 #pragma unroll
         for (int o = 1; o < LPC; o <<= 1) l += __shfl_xor_sync(lanes, l, o);
-        const float coef = exp2f(l - __shfl_sync(lanes, x.top, base + k + u)) - (val[u] >> 31 ? 1.f : 0.f);
+        const float coef = exp2f(l * kLog2e - __shfl_sync(lanes, x.top, base + k + u)) - (val[u] >> 31 ? 1.f : 0.f);
 #pragma unroll
         for (int v = 0; v < V; ++v)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) acc[v].p[j] = fma2(both(coef), h[u][v].p[j], acc[v].p[j]);
+          for (int j = 0; j < 4; ++j) acc[v].p[j] = fma2(both(coef), hg[v].p[j], acc[v].p[j]);
       }
     }
   }
@@ -463,6 +470,7 @@ __global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 6 : 3)
   const uint32_t none = (uint32_t)a.items, s = (uint32_t)(c0 * chunk);
   const uint32_t e = entries - s < (uint32_t)chunk ? entries : s + (uint32_t)chunk;
   const Lanes16<NL, FULL> from_hidden(hidden, a.sh, a.cols), from_table(table, a.st, a.cols);
+  const float scale = grad_scale(a, lse, grad_loss);
   struct Entries {  // 32 of them, one a lane; what lies behind the chunk is no candidate of the first position
     uint32_t key, val;
     float top;
@@ -490,7 +498,6 @@ __global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 6 : 3)
   auto finish = [&](bool whole) {
     float2 sum[NL];
     scatter16<NL>(acc, sum);
-    const float scale = whole ? grad_scale(a, lse, grad_loss) : 1.f;
 #pragma unroll
     for (int c = 0; c < NL; ++c) {
       const int col = scattered_column(c);
@@ -575,11 +582,13 @@ __global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 6 : 3)
 template <typename T, int W, typename P>
 __global__ void __launch_bounds__(kThreads) loss_join_kernel(Args a, const float *__restrict__ lse,
                                                              const float *__restrict__ grad_loss,
+                                                             const uint32_t *__restrict__ keys,
                                                              const uint32_t *__restrict__ ranges, uint32_t entries, int chunk,
                                                              const float *__restrict__ part, T *__restrict__ dtable,
                                                              unsigned join_ctas, const float *__restrict__ grad_hidden,
                                                              T *__restrict__ dhidden) {
-  constexpr int LPC = P::LPC, V = P::V, NG = kThreads / LPC, CPW = 32 / LPC, WF = W < 4 ? W : 4;
+  constexpr int LPC = P::LPC, V = P::V, NG = kThreads / LPC, CPW = 32 / LPC;
+  using S = Strip<T, W, P>;
   constexpr int kRounds = kItemsPerGroup, kItems = NG * kRounds;  // of a block
   constexpr uint32_t kAlone = 16;  // chunks that a group of lanes adds up by itself
   __shared__ uint2 popular[kItems];  // their first and last chunk
@@ -594,11 +603,10 @@ __global__ void __launch_bounds__(kThreads) loss_join_kernel(Args a, const float
     for (int64_t row = (int64_t)(blockIdx.x - join_ctas) * NG + grp; row < a.rows; row += step) {
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        const int g = col + v * LPC, valid = a.cols - 8 * g;
-        Group x = load_group<float, WF>(grad_hidden + row * a.cols + 8 * g, valid);
+        Group x = load_sums<W, P>(grad_hidden + row * a.cols, col, v, a.cols);
 #pragma unroll
         for (int i = 0; i < 4; ++i) x.p[i] = mul2(x.p[i], both(scale));
-        store_group<T, W>(dhidden + row * a.sdh + 8 * g, valid, x);
+        S::store(dhidden + row * a.sdh, col, v, a.cols, x);
       }
     }
     return;
@@ -608,8 +616,13 @@ __global__ void __launch_bounds__(kThreads) loss_join_kernel(Args a, const float
   const float scale = grad_scale(a, lse, grad_loss);
   const int64_t item0 = (int64_t)blockIdx.x * kItems + threadIdx.x / 32 * (CPW * kRounds);  // of the warp, one a lane
   uint2 range = make_uint2(0, 0);
-  if (lane < CPW * kRounds && item0 + lane < a.items && entries)
-    range = make_uint2(ranges[item0 + lane], ranges[a.items + item0 + lane]);
+  if (lane < CPW * kRounds && item0 + lane < a.items && entries) {
+    // (nobody has cleared the ranges: what stands at an item without entries is checked against the list)
+    const uint32_t item = (uint32_t)(item0 + lane), from = ranges[item], to = ranges[a.items + item];
+    if (from < to && to <= entries && keys[from] == item && keys[to - 1] == item && (from == 0 || keys[from - 1] != item) &&
+        (to == entries || keys[to] != item))
+      range = make_uint2(from, to);
+  }
   const uint32_t c0 = range.x / (uint32_t)chunk, c1 = range.y ? (range.y - 1) / (uint32_t)chunk : 0;
   const uint32_t n = range.x == range.y ? 0 : c1 - c0 + 1;
   // the sum of every `step`-th chunk's share, from the `from`-th on
@@ -618,13 +631,12 @@ __global__ void __launch_bounds__(kThreads) loss_join_kernel(Args a, const float
     for (int v = 0; v < V; ++v)
 #pragma unroll
       for (int i = 0; i < 4; ++i) acc[v].p[i] = both(0.f);
-#pragma unroll 4
+#pragma unroll(V == 1 ? 8 : 2)
     for (uint32_t c = c0 + from; c <= c1; c += step) {
       const int64_t slot = (int64_t)c * 2 + (c == c0 && inside ? 1 : 0);
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        const int g = col + v * LPC;
-        const Group x = load_group<float, WF>(part + slot * a.cols + 8 * g, a.cols - 8 * g);
+        const Group x = load_sums<W, P>(part + slot * a.cols, col, v, a.cols);
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[v].p[i] = add2(acc[v].p[i], x.p[i]);
       }
@@ -633,10 +645,9 @@ __global__ void __launch_bounds__(kThreads) loss_join_kernel(Args a, const float
   auto write = [&](int64_t to, Group (&acc)[V]) {
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const int g = col + v * LPC;
 #pragma unroll
       for (int i = 0; i < 4; ++i) acc[v].p[i] = mul2(acc[v].p[i], both(scale));
-      store_group<T, W>(dtable + to * a.sdt + 8 * g, a.cols - 8 * g, acc[v]);
+      S::store(dtable + to * a.sdt, col, v, a.cols, acc[v]);
     }
   };
   const bool inside = range.x % (uint32_t)chunk != 0;  // the first chunk's share is that of its last item
@@ -696,9 +707,9 @@ SortPlan sort_plan(const Args &a, int lanes) {
   p.entries = (int64_t)a.rows * (a.n + 1);
   p.tiles = (p.entries + kTile - 1) / kTile;
   // long chunks leave fewer sums to join, short ones make more groups of lanes: enough for 1024 threads an SM twice over, if
-  // there are that many
-  p.chunk = 128;
-  while (p.chunk > 32 && p.entries / p.chunk * lanes < 2LL * kSMs * 1024) p.chunk /= 2;
+  // there are that many; so few entries that they never fill the GPU go in the shortest ones
+  p.chunk = 512;
+  while (p.chunk > (p.entries <= kSmallEntries ? 8 : 32) && p.entries / p.chunk * lanes < 2LL * kSMs * 1024) p.chunk /= 2;
   p.chunks = (p.entries + p.chunk - 1) / p.chunk;
   return p;
 }
@@ -728,7 +739,8 @@ Scratch carve(const Args &a, void *base) {
 
 int launch_items(const Args &a, int dtype, const void *hidden, const void *table, const float *lse, const float *grad_hidden,
                  const float *grad_loss, void *dhidden, void *dtable, int width, const Scratch &s, cudaStream_t st) {
-  const int lines = mma_lines(a, dtype, width);
+  const bool dense = (int64_t)a.rows * (a.n + 1) / a.items >= kDense;  // (sixteen entries at a time want several an item)
+  const int lines = dense ? mma_lines(a, dtype, width) : 0;
   const SortPlan p = sort_plan(a, lines ? 32 : lanes_of(a.groups));
   const uint32_t entries = dtable ? (uint32_t)p.entries : 0;
   const Split by = split_by((uint32_t)a.n + 1);
@@ -737,7 +749,7 @@ int launch_items(const Args &a, int dtype, const void *hidden, const void *table
     if (!allow_smem(sort_small_kernel, kSmallSmem)) return BLOSSOM_ERR_CUDA;
     LaunchScope ls(K_LOSS_SORT, st);
     launch_chained(sort_small_kernel, dim3(1), dim3(kSmallThreads), kSmallSmem, st, a, by, entries,
-                   (p.passes * p.bits + kSmallBits - 1) / kSmallBits, s.keys[at], s.vals[at], s.range);
+                   (p.passes * p.bits + kSmallBits - 1) / kSmallBits, s.keys[at], s.vals[at]);
   } else if (entries) {
     const MoveKernel moves[2] = {move_kernel<true>(p.bits), move_kernel<false>(p.bits)};
     const size_t smem = move_smem(p.bits);
@@ -749,7 +761,7 @@ int launch_items(const Args &a, int dtype, const void *hidden, const void *table
       {
         LaunchScope ls(K_LOSS_SORT, st);
         launch_chained(i ? sort_count_kernel<false> : sort_count_kernel<true>, grid, block, 0, st, a, by, s.keys[at], entries,
-                       shift, p.bits, s.hist, s.range);
+                       shift, p.bits, s.hist);
       }
       if (scan) {
         LaunchScope ls(K_LOSS_SORT, st);
@@ -780,9 +792,10 @@ int launch_items(const Args &a, int dtype, const void *hidden, const void *table
       constexpr int W = decltype(w)::value, per = kThreads / P::LPC;
       if (entries && !lines) {
         LaunchScope ls(K_LOSS_ITEMS, st);
-        launch_chained(loss_items_kernel<T, W, P>, dim3((unsigned)((p.chunks + per - 1) / per)), dim3(kThreads), 0, st, a,
-                       static_cast<const T *>(hidden), static_cast<const T *>(table), lse, grad_loss, keys, vals, entries,
-                       p.chunk, static_cast<T *>(dtable), s.part, s.range);
+        launch_chained(dense ? loss_items_kernel<T, W, P, true> : loss_items_kernel<T, W, P, false>,
+                       dim3((unsigned)((p.chunks + per - 1) / per)), dim3(kThreads), 0, st, a, static_cast<const T *>(hidden),
+                       static_cast<const T *>(table), lse, grad_loss, keys, vals, entries, p.chunk, static_cast<T *>(dtable),
+                       s.part, s.range);
       }
       const int64_t items = per * kItemsPerGroup, join = dtable ? (a.items + items - 1) / items : 0;
       const int64_t rows = dhidden ? ((int64_t)a.rows + per - 1) / per : 0, most = kSMs * 8;
@@ -790,7 +803,7 @@ int launch_items(const Args &a, int dtype, const void *hidden, const void *table
       if (ctas == 0) return;
       LaunchScope ls(K_LOSS_JOIN, st);
       launch_chained(loss_join_kernel<T, W, P>, dim3((unsigned)ctas), dim3(kThreads), 0, st, a, lse, grad_loss,
-                     (const uint32_t *)s.range, entries, p.chunk, (const float *)s.part, static_cast<T *>(dtable),
+                     keys, (const uint32_t *)s.range, entries, p.chunk, (const float *)s.part, static_cast<T *>(dtable),
                      (unsigned)join, grad_hidden, static_cast<T *>(dhidden));
     });
   });

@@ -37,6 +37,7 @@ template <typename T, int W, typename P, bool GRAD>
 __global__ void __launch_bounds__(kThreads) loss_rows_kernel(Args a, const T *__restrict__ hidden, const T *__restrict__ table,
                                                              float *__restrict__ lse, float *__restrict__ dh,
                                                              double2 *__restrict__ sums, float *__restrict__ loss) {
+  using S = Strip<T, W, P>;
   constexpr int LPC = P::LPC, V = P::V, CPW = 32 / LPC, U = V == 1 ? 4 : 1;
   grid_chain_enter();
   const int lane = (int)threadIdx.x % 32, warp = (int)threadIdx.x / 32, col = lane % LPC, sub = lane / LPC;
@@ -53,8 +54,7 @@ __global__ void __launch_bounds__(kThreads) loss_rows_kernel(Args a, const T *__
       Group h[V];
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        const int g = col + v * LPC;
-        h[v] = load_group<T, W>(hidden + row * a.sh + 8 * g, a.cols - 8 * g);
+        h[v] = S::load(hidden + row * a.sh, col, v, a.cols);
 #pragma unroll
         for (int i = 0; i < 4; ++i) h[v].p[i] = mul2(h[v].p[i], both(kLog2e));  // logits in units of log 2
       }
@@ -70,10 +70,7 @@ __global__ void __launch_bounds__(kThreads) loss_rows_kernel(Args a, const T *__
           for (int u = 0; u < U; ++u) {
             at[u] = __shfl_sync(0xffffffffu, id, (k + u) * CPW + sub);
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-              const int g = col + v * LPC;
-              w[u][v] = load_group<T, W>(table + at[u] * a.st + 8 * g, at[u] >= 0 ? a.cols - 8 * g : 0);
-            }
+            for (int v = 0; v < V; ++v) w[u][v] = S::load(table + at[u] * a.st, col, v, a.cols, at[u] >= 0);
           }
           float high = top;
           bool any = false;
@@ -127,8 +124,7 @@ __global__ void __launch_bounds__(kThreads) loss_rows_kernel(Args a, const T *__
         const float inv = weight / total;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-          const int g = col + v * LPC;
-          Group w = load_group<T, W>(table + target * a.st + 8 * g, a.cols - 8 * g);
+          Group w = S::load(table + target * a.st, col, v, a.cols);
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             float &x = acc[v].at(i);
@@ -143,10 +139,7 @@ __global__ void __launch_bounds__(kThreads) loss_rows_kernel(Args a, const T *__
     if (lane == 0) lse[row] = row_lse;
     if (GRAD && sub == 0) {
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        const int g = col + v * LPC;
-        store_group<float, (W < 4 ? W : 4)>(dh + (int64_t)row * a.cols + 8 * g, a.cols - 8 * g, acc[v]);
-      }
+      for (int v = 0; v < V; ++v) store_sums<W, P>(dh + (int64_t)row * a.cols, col, v, a.cols, acc[v]);
     }
   }
   close_sums<kThreads>(mine, sums, loss, lse + a.rows);
@@ -220,8 +213,8 @@ __global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 6 : 4)
         const bool second = c0 + 16 <= a.n, third = c0 + 32 <= a.n;
         if (third) next = ids_from(c0 + 32, there_next);
         if (second) from_table.load16(ids, 16, w[1]);
-        const float first = score(w[0], there);
-        if (c0 == 0) own = __shfl_sync(0xffffffffu, first, 0) * kLog2e;
+        const float l0 = score(w[0], there);
+        if (c0 == 0) own = __shfl_sync(0xffffffffu, l0, 0) * kLog2e;
         if (third) from_table.load16(next, 0, w[0]);
         if (second) score(w[1], there >> 16);
         ids = next;

@@ -20,7 +20,7 @@ struct Args {
 };
 
 // ---- a group of 8 columns in four pairs, W elements an access --------------------------------------
-// W is the widest of 16 bytes, two elements and one that every row's address and length is a multiple of.
+// W is the widest of 16 bytes, 8 bytes, two elements and one that every row's address and length is a multiple of.
 struct Group {
   float2 p[4];
   __device__ __forceinline__ float &at(int j) { return j & 1 ? p[j / 2].y : p[j / 2].x; }
@@ -44,31 +44,33 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
 template <typename T, int W>
 struct Raw {
   uint32_t w[2 * sizeof(T)];
-  __device__ __forceinline__ void load(const T *p, int valid) {
+  // the elements j .. j + W - 1 from p, or zeros
+  __device__ __forceinline__ void piece(const T *p, int j, bool there) {
     constexpr int words = W * (int)sizeof(T) / 4;  // an access has (0: half a one)
-#pragma unroll
-    for (int j = 0; j < 8; j += W) {
-      const int at = j * (int)sizeof(T) / 4;
-      if (j < valid) {
-        if constexpr (words == 4) {
-          const uint4 q = *reinterpret_cast<const uint4 *>(p + j);
-          w[at] = q.x, w[at + 1] = q.y, w[at + 2] = q.z, w[at + 3] = q.w;
-        } else if constexpr (words == 2) {
-          const uint2 q = *reinterpret_cast<const uint2 *>(p + j);
-          w[at] = q.x, w[at + 1] = q.y;
-        } else if constexpr (words == 1) {
-          w[at] = *reinterpret_cast<const uint32_t *>(p + j);
-        } else {
-          const uint32_t h = *reinterpret_cast<const uint16_t *>(p + j);
-          w[at] = j & 1 ? w[at] | h << 16 : h;
-        }
-      } else if constexpr (words > 0) {
-#pragma unroll
-        for (int i = 0; i < words; ++i) w[at + i] = 0;
-      } else if (!(j & 1)) {
-        w[at] = 0;
+    const int at = j * (int)sizeof(T) / 4;
+    if (there) {
+      if constexpr (words == 4) {
+        const uint4 q = *reinterpret_cast<const uint4 *>(p);
+        w[at] = q.x, w[at + 1] = q.y, w[at + 2] = q.z, w[at + 3] = q.w;
+      } else if constexpr (words == 2) {
+        const uint2 q = *reinterpret_cast<const uint2 *>(p);
+        w[at] = q.x, w[at + 1] = q.y;
+      } else if constexpr (words == 1) {
+        w[at] = *reinterpret_cast<const uint32_t *>(p);
+      } else {
+        const uint32_t h = *reinterpret_cast<const uint16_t *>(p);
+        w[at] = j & 1 ? w[at] | h << 16 : h;
       }
+    } else if constexpr (words > 0) {
+#pragma unroll
+      for (int i = 0; i < words; ++i) w[at + i] = 0;
+    } else if (!(j & 1)) {
+      w[at] = 0;
     }
+  }
+  __device__ __forceinline__ void load(const T *p, int valid) {
+#pragma unroll
+    for (int j = 0; j < 8; j += W) piece(p + j, j, j < valid);
   }
   __device__ __forceinline__ Group get() const {
     Group v;
@@ -81,33 +83,30 @@ struct Raw {
   }
 };
 template <typename T, int W>
-__device__ __forceinline__ Group load_group(const T *p, int valid) {
-  Raw<T, W> r;
-  r.load(p, valid);
-  return r.get();
+__device__ __forceinline__ void store_piece(T *p, int j, Group &v) {
+  if constexpr (sizeof(T) == 4 && W == 4) {
+    *reinterpret_cast<float4 *>(p) = make_float4(v.at(j), v.at(j + 1), v.at(j + 2), v.at(j + 3));
+  } else if constexpr (sizeof(T) == 4 && W == 2) {
+    *reinterpret_cast<float2 *>(p) = v.p[j / 2];
+  } else if constexpr (sizeof(T) == 4) {
+    *p = v.at(j);
+  } else if constexpr (W == 8) {
+    *reinterpret_cast<uint4 *>(p) = make_uint4(pack2(v.p[0].x, v.p[0].y), pack2(v.p[1].x, v.p[1].y),
+                                               pack2(v.p[2].x, v.p[2].y), pack2(v.p[3].x, v.p[3].y));
+  } else if constexpr (W == 4) {
+    *reinterpret_cast<uint2 *>(p) = make_uint2(pack2(v.at(j), v.at(j + 1)), pack2(v.at(j + 2), v.at(j + 3)));
+  } else if constexpr (W == 2) {
+    *reinterpret_cast<uint32_t *>(p) = pack2(v.at(j), v.at(j + 1));
+  } else {
+    *p = __float2bfloat16(v.at(j));
+  }
 }
 template <typename T, int W>
 __device__ __forceinline__ void store_group(T *p, int valid, const Group &g) {
   Group v = g;
 #pragma unroll
-  for (int j = 0; j < 8; j += W) {
-    if (j < valid) {
-      if constexpr (sizeof(T) == 4 && W == 4) {
-        *reinterpret_cast<float4 *>(p + j) = make_float4(v.at(j), v.at(j + 1), v.at(j + 2), v.at(j + 3));
-      } else if constexpr (sizeof(T) == 4 && W == 2) {
-        *reinterpret_cast<float2 *>(p + j) = v.p[j / 2];
-      } else if constexpr (sizeof(T) == 4) {
-        p[j] = v.at(j);
-      } else if constexpr (W == 8) {
-        *reinterpret_cast<uint4 *>(p) = make_uint4(pack2(v.p[0].x, v.p[0].y), pack2(v.p[1].x, v.p[1].y),
-                                                   pack2(v.p[2].x, v.p[2].y), pack2(v.p[3].x, v.p[3].y));
-      } else if constexpr (W == 2) {
-        *reinterpret_cast<uint32_t *>(p + j) = pack2(v.at(j), v.at(j + 1));
-      } else {
-        p[j] = __float2bfloat16(v.at(j));
-      }
-    }
-  }
+  for (int j = 0; j < 8; j += W)
+    if (j < valid) store_piece<T, W>(p + j, j, v);
 }
 // what is subtracted from the columns that are there, zero for the others (whose elements are zero and stay so)
 template <int W>
@@ -221,7 +220,7 @@ inline void with_plan(int groups, F &&f) {
     if (groups <= 512 * V) return f(Plan<512, V>());
 }
 
-// Elements an access may take: 16 bytes, two elements or one.
+// Elements an access may take: 16 bytes, 8 bytes, two elements or one.
 struct Alignment {
   uint64_t bits = 0;
   void rows_at(const void *p, int64_t stride, size_t esz) {
@@ -229,7 +228,7 @@ struct Alignment {
   }
   int elements(int cols, size_t esz) const {
     const uint64_t b = bits | (uint64_t)cols * esz;
-    return b % 16 == 0 ? (int)(16 / esz) : b % (2 * esz) == 0 ? 2 : 1;
+    return b % 16 == 0 ? (int)(16 / esz) : b % 8 == 0 ? (int)(8 / esz) : b % (2 * esz) == 0 ? 2 : 1;
   }
 };
 
@@ -246,6 +245,7 @@ inline void with_type(int dtype, int w, F &&f) {
     else f(float(), integral_constant<int, 1>());
   } else {
     if (w == 8) f(__nv_bfloat16(), integral_constant<int, 8>());
+    else if (w == 4) f(__nv_bfloat16(), integral_constant<int, 4>());
     else if (w == 2) f(__nv_bfloat16(), integral_constant<int, 2>());
     else f(__nv_bfloat16(), integral_constant<int, 1>());
   }
