@@ -246,7 +246,7 @@ struct Scratch {
   uint32_t *keys[2], *vals[2];   // [entries] item and position (top bit: it is the target) of every candidate, being sorted
   uint32_t *hist, *totals;       // [digits][tiles], [digits]
   uint32_t *range;               // [2][items] where an item's entries start and end in the sorted list; not written for others
-  float *part;                   // [chunks][2][cols] sums of items that reach over the end of a chunk
+  float *part;                   // [spans][2][cols] sums of items that reach over the end of a span
   size_t bytes;
 };
 constexpr size_t kForwardBytes = BLOSSOM_LOSS_FORWARD_BYTES;
@@ -257,11 +257,12 @@ struct SortPlan {
   int passes, bits;
   int64_t entries, tiles;
   int chunk;  // sorted entries that a warp or a group of lanes adds up
-  int64_t chunks;
+  int span;   // that a block does
+  int64_t spans;
 };
 constexpr int kSortThreads = 256, kSortPerThread = 16, kTile = kSortThreads * kSortPerThread, kMaxDigits = 512;
 
-SortPlan sort_plan(const Args &a, int lanes);  // lanes: of a group that walks a chunk
+SortPlan sort_plan(const Args &a, int lanes, int threads);  // lanes of a group that walks a chunk, threads of a block
 Scratch carve(const Args &a, void *base);
 // dtable from the candidates, sorted by item; dhidden from grad_hidden; either may be null
 int launch_items(const Args &a, int dtype, const void *hidden, const void *table, const float *lse, const float *grad_hidden,

@@ -340,153 +340,216 @@ constexpr size_t move_smem(int bits) {
 }
 
 // ---- sums over an item's entries ---------------------------------------------------------------
+// A block's groups of lanes (or warps) walk consecutive chunks, together a span of the list.  An item whose entries lie in one
+// chunk is written there and then.  The others' sums meet in shared memory: a group leaves that of its first item there if
+// the item began before its chunk, and the group in whose chunk an item began adds up those of the groups behind it.
+// What reaches over the span's ends goes to scratch, at most two sums a span: [0] of the span's first item if it began
+// before the span or at its start, [1] of its last item if that began inside.
 constexpr int kThreads = 256, kItemsPerGroup = 2, kDense = 8;
 
-// DENSE: an item has several entries, its row of the table stays in registers.  Otherwise the table's rows are read entry by entry
-// like the hidden ones: one that waits for its item to begin would be a memory latency in front of nearly every entry
-// (4000 entries of 3000 items: 23 us against 7).
-template <typename T, int W, typename P, bool DENSE>
-__global__ void __launch_bounds__(kThreads, P::V <= 2 ? 2 : 1)
+template <int NG>
+struct Ends {  // of every group's chunk
+  uint32_t first[NG];  // its first item
+  bool through[NG];    // that is its only one and goes on behind it
+};
+// Adds the sums of the groups g, g + 1, ... that belong to `item`; true if the item ends in one of them.
+template <int NG, typename ADD>
+__device__ __forceinline__ bool add_groups(const Ends<NG> &ends, int g, uint32_t item, ADD &&add) {
+  for (; g < NG; ++g) {
+    if (ends.first[g] != item) return true;
+    add(g);
+    if (!ends.through[g]) return true;
+  }
+  return false;
+}
+
+template <typename T, int W, typename P>
+__global__ void __launch_bounds__(kThreads, P::V == 1 ? 4 : P::V == 2 ? 2 : 1)
     loss_items_kernel(Args a, const T *__restrict__ hidden, const T *__restrict__ table, const float *__restrict__ lse,
                       const float *__restrict__ grad_loss, const uint32_t *__restrict__ keys, const uint32_t *__restrict__ vals,
                       uint32_t entries, int chunk, T *__restrict__ dtable, float *__restrict__ part,
                       uint32_t *__restrict__ range) {
   using S = Strip<T, W, P>;
-  constexpr int LPC = P::LPC, V = P::V, U = V > 1 ? 1 : DENSE || sizeof(T) == 2 ? 4 : 2;
+  constexpr int LPC = P::LPC, V = P::V, NG = kThreads / LPC;
+  __shared__ float shared_sums[NG][V * 8][LPC];
+  __shared__ Ends<NG> ends;
   grid_chain_enter();
   const int col = (int)threadIdx.x % LPC, base = (int)threadIdx.x % 32 / LPC * LPC;
   const uint32_t lanes = LPC == 32 ? 0xffffffffu : ((1u << LPC) - 1) << base;
-  const int64_t c = (int64_t)blockIdx.x * (kThreads / LPC) + threadIdx.x / LPC;
-  if (c * chunk >= entries) return;
-  const uint32_t none = (uint32_t)a.items, s = (uint32_t)(c * chunk);
-  const uint32_t e = entries - s < (uint32_t)chunk ? entries : s + (uint32_t)chunk;
+  const int grp = (int)threadIdx.x / LPC;
+  const uint32_t none = (uint32_t)a.items;
+  const uint64_t start = ((uint64_t)blockIdx.x * NG + grp) * (uint32_t)chunk;
+  const uint32_t s = start < entries ? (uint32_t)start : entries, e = entries - s < (uint32_t)chunk ? entries : s + (uint32_t)chunk;
   const float scale = grad_scale(a, lse, grad_loss);
-  uint32_t cur = keys[s];
+  uint32_t cur = s < entries ? keys[s] : none;
   const uint32_t before = s > 0 ? keys[s - 1] : none;
-  bool open = s > 0 && before == cur;  // the item's entries began in a chunk before
-  bool first = true;
+  const bool open = cur < none && before == cur;  // the first item's entries began in a chunk before
+  bool first = true, closed = cur >= none;         // closed: what follows is no candidate
   const bool writer = col == 0;
   Group acc[V], own[V];
   auto begin = [&](uint32_t item) {
     cur = item;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      if (DENSE) own[v] = S::load(table + item * a.st, col, v, a.cols);
 #pragma unroll
       for (int i = 0; i < 4; ++i) acc[v].p[i] = both(0.f);
     }
   };
-  auto finish = [&](bool whole) {
+  auto write = [&](uint32_t item) {
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      if (whole) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[v].p[i] = mul2(acc[v].p[i], both(scale));
-        S::store(dtable + cur * a.sdt, col, v, a.cols, acc[v]);
-      } else {
-        store_sums<W, P>(part + (c * 2 + (first ? 0 : 1)) * a.cols, col, v, a.cols, acc[v]);
-      }
+      for (int i = 0; i < 4; ++i) acc[v].p[i] = mul2(acc[v].p[i], both(scale));
+      S::store(dtable + item * a.sdt, col, v, a.cols, acc[v]);
     }
   };
-  if (writer && s > 0 && !open && before < none) range[none + before] = s;
-  if (cur >= none) return;
-  if (writer && !open) range[cur] = s;
-  begin(cur);
-  // LPC entries, one a lane, the next ones under way
+  auto leave = [&](int slot) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) store_sums<W, P>(part + ((int64_t)blockIdx.x * 2 + slot) * a.cols, col, v, a.cols, acc[v]);
+  };
+  auto share = [&]() {
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) shared_sums[grp][8 * v + i][col] = acc[v].at(i);
+  };
+  auto add = [&](int g) {
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) acc[v].at(i) += shared_sums[g][8 * v + i][col];
+  };
+  if (writer) {
+    if (s > 0 && s < entries && !open && before < none) range[none + before] = s;
+    if (!closed && !open) range[cur] = s;
+    ends.first[grp] = cur;
+  }
+  if (!closed) begin(cur);
+  // LPC entries, one a lane: the positions' log-sum-exps are asked for LPC entries after the positions (whoever asks at once
+  // waits for the positions to come)
   struct Entries {
     uint32_t key, val;
     float top;
+    __device__ __forceinline__ void ask(const float *lse) { top = lse[val & 0x7fffffffu]; }
   };
   auto entries_from = [&](uint32_t i) {
     Entries x = {none, 0, 0.f};
-    if (i + col < e) {
-      x.key = keys[i + col], x.val = vals[i + col];
-      x.top = lse[x.val & 0x7fffffffu] * kLog2e;
-    }
+    if (i + col < e) x.key = keys[i + col], x.val = vals[i + col];
     return x;
   };
-  Entries next = entries_from(s);
-  for (uint32_t i0 = s; i0 < e; i0 += LPC) {
-    const Entries x = next;
-    if (i0 + LPC < e) next = entries_from(i0 + LPC);
-#pragma unroll 1
-    for (int k = 0; k < LPC && i0 + k < e; k += U) {
-      uint32_t key[U], val[U];
-      rows::Raw<T, W> h[U][V], w[U][V];
+  // The next entry's hidden row is under way, and with it the table's where a new item begins: one that waited for its item would
+  // be a memory latency in front of every item.  (More rows ahead in more registers were slower than more warps: 51180 x 100
+  // candidates x 64 fp32 313 us with four rows and 16 warps an SM, 203 with one and 32.)
+  rows::Raw<T, W> h[V], w[V];
+  bool fresh;
+  uint32_t last = none;  // the item of the entry loaded last
+  auto load = [&](uint32_t key, uint32_t val) {
+    fresh = key != last && key < none;
+    last = key;
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        key[u] = __shfl_sync(lanes, x.key, base + k + u);
-        val[u] = __shfl_sync(lanes, x.val, base + k + u);
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-          h[u][v] = S::raw(hidden + (int64_t)(val[u] & 0x7fffffffu) * a.sh, col, v, a.cols, key[u] < none);
-          if (!DENSE) w[u][v] = S::raw(table + key[u] * a.st, col, v, a.cols, key[u] < none);
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        if (i0 + k + u >= e) break;
-        if (key[u] != cur) {
-          finish(!open);
-          open = first = false;
-          if (writer) range[none + cur] = i0 + k + u;
-          if (key[u] >= none) return;  // (what follows is no candidate)
-          if (writer) range[key[u]] = i0 + k + u;
-          begin(key[u]);
-        }
-        Group hg[V], wg[V];
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-          hg[v] = h[u][v].get();
-          wg[v] = DENSE ? own[v] : w[u][v].get();
-        }
-        float l = dot<V>(wg, hg);
-#pragma unroll
-        for (int o = 1; o < LPC; o <<= 1) l += __shfl_xor_sync(lanes, l, o);
-        const float coef = exp2f(l * kLog2e - __shfl_sync(lanes, x.top, base + k + u)) - (val[u] >> 31 ? 1.f : 0.f);
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) acc[v].p[j] = fma2(both(coef), hg[v].p[j], acc[v].p[j]);
-      }
+    for (int v = 0; v < V; ++v) {
+      h[v] = S::raw(hidden + (int64_t)(val & 0x7fffffffu) * a.sh, col, v, a.cols, key < none);
+      if (fresh) w[v] = S::raw(table + key * a.st, col, v, a.cols);
     }
+  };
+  Entries x = entries_from(s), next = entries_from(s + LPC);
+  x.ask(lse);
+  load(__shfl_sync(lanes, x.key, base), __shfl_sync(lanes, x.val, base));
+  for (uint32_t i0 = s; i0 < e && !closed; i0 += LPC) {
+    next.ask(lse);
+    const Entries third = entries_from(i0 + 2 * LPC);
+#pragma unroll 1
+    for (int k = 0; k < LPC && i0 + k < e; ++k) {
+      const uint32_t key = __shfl_sync(lanes, x.key, base + k), val = __shfl_sync(lanes, x.val, base + k);
+      const float top = __shfl_sync(lanes, x.top, base + k);
+      if (key != cur) {
+        if (first && open) share();
+        else write(cur);
+        first = false;
+        if (writer) range[none + cur] = i0 + k;
+        closed = key >= none;
+        if (closed) break;
+        if (writer) range[key] = i0 + k;
+        begin(key);
+      }
+      Group hg[V];
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        if (fresh) own[v] = w[v].get();
+        hg[v] = h[v].get();
+      }
+      const bool wrap = k + 1 == LPC;
+      load(__shfl_sync(lanes, wrap ? next.key : x.key, base + (wrap ? 0 : k + 1)),
+           __shfl_sync(lanes, wrap ? next.val : x.val, base + (wrap ? 0 : k + 1)));
+      float l = dot<V>(own, hg);
+#pragma unroll
+      for (int o = 1; o < LPC; o <<= 1) l += __shfl_xor_sync(lanes, l, o);
+      const float coef = exp2f((l - top) * kLog2e) - (val >> 31 ? 1.f : 0.f);
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[v].p[j] = fma2(both(coef), hg[v].p[j], acc[v].p[j]);
+    }
+    x = next;
+    next = third;
   }
-  finish(!open && !(e < entries && keys[e] == cur));
-  if (writer && e == entries) range[none + cur] = e;
+  const bool goes_on = !closed && e < entries && keys[e] == cur;
+  if (!closed) {
+    if (first && open) share();
+    else if (!goes_on) write(cur);
+    if (writer && e == entries) range[none + cur] = e;
+  }
+  if (writer) ends.through[grp] = first && goes_on;
+  __syncthreads();
+  if (goes_on && !(first && open)) {  // the item began in this chunk
+    if (add_groups<NG>(ends, grp + 1, cur, add)) write(cur);
+    else leave(grp == 0 && first ? 0 : 1);
+  }
+  if (grp == 0 && open) {  // the span's first item began before it
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[v].p[i] = both(0.f);
+    add_groups<NG>(ends, 0, ends.first[0], add);
+    leave(0);
+  }
 }
 
 // The same on the matrix units: a warp walks a chunk 16 entries at a time, their hidden rows the first operand, the item's
-// row the second; the next 16 rows are under way meanwhile.  Sixteen entries of more than one item go through once an item.
+// row the second.  Sixteen entries of more than one item go through once an item.
 template <int NL, bool FULL>
-__global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 6 : 3)
+__global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 7 : 4)
     loss_items_mma_kernel(Args a, const __nv_bfloat16 *__restrict__ hidden, const __nv_bfloat16 *__restrict__ table,
                           const float *__restrict__ lse, const float *__restrict__ grad_loss, const uint32_t *__restrict__ keys,
                           const uint32_t *__restrict__ vals, uint32_t entries, int chunk, __nv_bfloat16 *__restrict__ dtable,
                           float *__restrict__ part, uint32_t *__restrict__ range) {
+  constexpr int NG = kMmaThreads / 32;
+  __shared__ float2 shared_sums[NG][NL][32];
+  __shared__ Ends<NG> ends;
   grid_chain_enter();
-  const int lane = (int)threadIdx.x % 32, group = lane / 8;
-  const int64_t c0 = (int64_t)blockIdx.x * (kMmaThreads / 32) + threadIdx.x / 32;
-  if (c0 * chunk >= entries) return;
-  const uint32_t none = (uint32_t)a.items, s = (uint32_t)(c0 * chunk);
-  const uint32_t e = entries - s < (uint32_t)chunk ? entries : s + (uint32_t)chunk;
+  const int lane = (int)threadIdx.x % 32, group = lane / 8, warp = (int)threadIdx.x / 32;
+  const uint32_t none = (uint32_t)a.items;
+  const uint64_t start = ((uint64_t)blockIdx.x * NG + warp) * (uint32_t)chunk;
+  const uint32_t s = start < entries ? (uint32_t)start : entries, e = entries - s < (uint32_t)chunk ? entries : s + (uint32_t)chunk;
   const Lanes16<NL, FULL> from_hidden(hidden, a.sh, a.cols), from_table(table, a.st, a.cols);
   const float scale = grad_scale(a, lse, grad_loss);
-  struct Entries {  // 32 of them, one a lane; what lies behind the chunk is no candidate of the first position
+  // 32 entries, one a lane; what lies behind the chunk is no candidate of the first position.  The positions' log-sum-exps are
+  // asked for 32 entries after the positions (whoever asks at once waits for the positions to come).
+  struct Entries {
     uint32_t key, val;
     float top;
+    __device__ __forceinline__ void ask(const float *lse) { top = lse[val & 0x7fffffffu]; }
   };
   auto entries_from = [&](uint32_t i) {
     Entries x = {none, 0, 0.f};
-    if (i + lane < e) {
-      x.key = keys[i + lane], x.val = vals[i + lane];
-      x.top = lse[x.val & 0x7fffffffu] * kLog2e;
-    }
+    if (i + lane < e) x.key = keys[i + lane], x.val = vals[i + lane];
     return x;
   };
   uint4 w[NL];
   float2 acc[NL][4];
-  uint32_t cur = keys[s], before = s > 0 ? keys[s - 1] : 0xffffffffu;
-  bool open = before == cur, first = true;  // open: the item's entries began in a chunk before
+  uint32_t cur = s < entries ? keys[s] : none, before = s > 0 ? keys[s - 1] : 0xffffffffu;
+  const bool open = cur < none && before == cur;  // the first item's entries began in a chunk before
+  bool first = true;
   auto begin = [&](uint32_t item) {
     cur = item;
     from_table.vector(item, a.cols, w);
@@ -495,16 +558,31 @@ __global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 6 : 3)
 #pragma unroll
       for (int i = 0; i < 4; ++i) acc[c][i] = make_float2(0.f, 0.f);
   };
-  auto finish = [&](bool whole) {
-    float2 sum[NL];
-    scatter16<NL>(acc, sum);
+  auto write = [&](const float2 (&sum)[NL]) {
 #pragma unroll
     for (int c = 0; c < NL; ++c) {
       const int col = scattered_column(c);
-      if (!FULL && col >= a.cols) continue;
-      if (whole) *reinterpret_cast<uint32_t *>(dtable + cur * a.sdt + col) = rows::pack2(sum[c].x * scale, sum[c].y * scale);
-      else *reinterpret_cast<float2 *>(part + (c0 * 2 + (first ? 0 : 1)) * a.cols + col) = sum[c];
+      if (FULL || col < a.cols)
+        *reinterpret_cast<uint32_t *>(dtable + cur * a.sdt + col) = rows::pack2(sum[c].x * scale, sum[c].y * scale);
     }
+  };
+  auto leave = [&](const float2 (&sum)[NL], int slot) {
+#pragma unroll
+    for (int c = 0; c < NL; ++c) {
+      const int col = scattered_column(c);
+      if (FULL || col < a.cols) *reinterpret_cast<float2 *>(part + ((int64_t)blockIdx.x * 2 + slot) * a.cols + col) = sum[c];
+    }
+  };
+  auto share = [&](const float2 (&sum)[NL]) {
+#pragma unroll
+    for (int c = 0; c < NL; ++c) shared_sums[warp][c][lane] = sum[c];
+  };
+  auto finish = [&]() {
+    float2 sum[NL];
+    scatter16<NL>(acc, sum);
+    if (first && open) share(sum);
+    else write(sum);
+    first = false;
   };
   // where items start and end, from 32 entries and the key before them
   auto mark = [&](const Entries &x, uint32_t i) {
@@ -528,7 +606,7 @@ __global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 6 : 3)
       float p[4];
       dots16<NL>(h, w, p);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) p[j] = exp2f(p[j] * kLog2e - top[j]) - (targets >> (4 * j) & 1 ? 1.f : 0.f);
+      for (int j = 0; j < 4; ++j) p[j] = exp2f((p[j] - top[j]) * kLog2e) - (targets >> (4 * j) & 1 ? 1.f : 0.f);
       uint32_t others = __ballot_sync(0xffffffffu, x.key != cur) >> half & 0xffffu;
       if (!others) {
         weigh16<NL>(h, p, acc);
@@ -548,50 +626,73 @@ __global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 6 : 3)
       // the next item among the 16, if there is one (they are sorted)
       const uint32_t later = __ballot_sync(0xffffffffu, (lane & 16) == half && x.key > cur && x.key < none);
       if (!later) return;
-      finish(!open);
-      open = first = false;
+      finish();
       begin(__shfl_sync(0xffffffffu, x.key, __ffs(later) - 1));
     }
   };
-  Entries x = entries_from(s);
+  const bool some = cur < none;  // (else there is no candidate here)
+  if (lane == 0) ends.first[warp] = cur;
+  Entries x = entries_from(s), next = entries_from(s + 32);
+  x.ask(lse);
   mark(x, s);
-  if (cur >= none) return;
-  begin(cur);
-  Rows16<NL> h[2];
-  from_hidden.load16(x.val & 0x7fffffffu, 0, h[0]);
-  for (uint32_t i = s; i < e; i += 32) {
-    const bool second = i + 16 < e, third = i + 32 < e;
-    Entries next = {none, 0, 0.f};
-    if (third) next = entries_from(i + 32);
-    if (second) from_hidden.load16(x.val & 0x7fffffffu, 16, h[1]);
-    walk(h[0], x, 0);
-    if (third) {
-      mark(next, i + 32);
-      from_hidden.load16(next.val & 0x7fffffffu, 0, h[0]);
+  float2 sum[NL];
+  bool goes_on = false;
+  if (some) {
+    begin(cur);
+    Rows16<NL> h;
+    for (uint32_t i = s; i < e; i += 32) {
+      from_hidden.load16(x.val & 0x7fffffffu, 0, h);
+      next.ask(lse);
+      const Entries after = entries_from(i + 64);
+      walk(h, x, 0);
+      if (i + 16 < e) {
+        from_hidden.load16(x.val & 0x7fffffffu, 16, h);
+        walk(h, x, 16);
+      }
+      if (i + 32 < e) mark(next, i + 32);
+      x = next;
+      next = after;
     }
-    if (second) walk(h[1], x, 16);
-    x = next;
+    goes_on = e < entries && keys[e] == cur;
+    scatter16<NL>(acc, sum);
+    if (first && open) share(sum);
+    else if (!goes_on) write(sum);
   }
-  finish(!open && !(e < entries && keys[e] == cur));
+  if (lane == 0) ends.through[warp] = first && goes_on;
+  __syncthreads();
+  auto add = [&](int g) {
+#pragma unroll
+    for (int c = 0; c < NL; ++c) sum[c] = add2(sum[c], shared_sums[g][c][lane]);
+  };
+  if (goes_on && !(first && open)) {  // the item began in this chunk
+    if (add_groups<NG>(ends, warp + 1, cur, add)) write(sum);
+    else leave(sum, warp == 0 && first ? 0 : 1);
+  }
+  if (warp == 0 && open && some) {  // the span's first item began before it
+#pragma unroll
+    for (int c = 0; c < NL; ++c) sum[c] = make_float2(0.f, 0.f);
+    add_groups<NG>(ends, 0, ends.first[0], add);
+    leave(sum, 0);
+  }
 }
 
 // The last kernel: blocks up to `join_ctas` finish the table's gradient, those behind them scale that of the hidden rows
 // (g / count * grad_hidden, rounded once).
-// Table: items without entries (zeros) and those whose entries reach over a chunk's end: their chunks' sums, in order.  A
-// group of lanes takes two items one after another; items of many chunks are left to the whole block.
+// Table: items without entries (zeros) and those whose entries reach over a span's end: their spans' sums, in order.  A
+// group of lanes takes two items one after another; items of many spans are left to the whole block.
 template <typename T, int W, typename P>
 __global__ void __launch_bounds__(kThreads) loss_join_kernel(Args a, const float *__restrict__ lse,
                                                              const float *__restrict__ grad_loss,
                                                              const uint32_t *__restrict__ keys,
-                                                             const uint32_t *__restrict__ ranges, uint32_t entries, int chunk,
+                                                             const uint32_t *__restrict__ ranges, uint32_t entries, int span,
                                                              const float *__restrict__ part, T *__restrict__ dtable,
                                                              unsigned join_ctas, const float *__restrict__ grad_hidden,
                                                              T *__restrict__ dhidden) {
   constexpr int LPC = P::LPC, V = P::V, NG = kThreads / LPC, CPW = 32 / LPC;
   using S = Strip<T, W, P>;
   constexpr int kRounds = kItemsPerGroup, kItems = NG * kRounds;  // of a block
-  constexpr uint32_t kAlone = 16;  // chunks that a group of lanes adds up by itself
-  __shared__ uint2 popular[kItems];  // their first and last chunk
+  constexpr uint32_t kAlone = 16;  // spans that a group of lanes adds up by itself
+  __shared__ uint2 popular[kItems];  // their first and last span
   __shared__ int popular_item[kItems];  // and which they are, bit 30: as `inside` below
   __shared__ int populars;
   __shared__ float sums[NG][LPC * V * 8];
@@ -623,9 +724,9 @@ __global__ void __launch_bounds__(kThreads) loss_join_kernel(Args a, const float
         (to == entries || keys[to] != item))
       range = make_uint2(from, to);
   }
-  const uint32_t c0 = range.x / (uint32_t)chunk, c1 = range.y ? (range.y - 1) / (uint32_t)chunk : 0;
+  const uint32_t c0 = range.x / (uint32_t)span, c1 = range.y ? (range.y - 1) / (uint32_t)span : 0;
   const uint32_t n = range.x == range.y ? 0 : c1 - c0 + 1;
-  // the sum of every `step`-th chunk's share, from the `from`-th on
+  // the sum of every `step`-th span's share, from the `from`-th on
   auto add_up = [&](uint32_t c0, uint32_t c1, bool inside, uint32_t from, uint32_t step, Group (&acc)[V]) {
 #pragma unroll
     for (int v = 0; v < V; ++v)
@@ -650,7 +751,7 @@ __global__ void __launch_bounds__(kThreads) loss_join_kernel(Args a, const float
       S::store(dtable + to * a.sdt, col, v, a.cols, acc[v]);
     }
   };
-  const bool inside = range.x % (uint32_t)chunk != 0;  // the first chunk's share is that of its last item
+  const bool inside = range.x % (uint32_t)span != 0;  // the first span's share is that of its last item
   Group acc[V];
 #pragma unroll 1
   for (int k = 0; k < kRounds; ++k) {
@@ -658,7 +759,7 @@ __global__ void __launch_bounds__(kThreads) loss_join_kernel(Args a, const float
     const uint32_t many = __shfl_sync(0xffffffffu, n, from);
     const uint32_t b0 = __shfl_sync(0xffffffffu, c0, from), b1 = __shfl_sync(0xffffffffu, c1, from);
     const bool in = __shfl_sync(0xffffffffu, (int)inside, from);
-    if (item0 + from >= a.items || many == 1 || many > kAlone) continue;  // (one chunk: written by the kernel before)
+    if (item0 + from >= a.items || many == 1 || many > kAlone) continue;  // (one span: written by the kernel before)
     if (many) {
       add_up(b0, b1, in, 0, 1, acc);
     } else {
@@ -698,7 +799,7 @@ __global__ void __launch_bounds__(kThreads) loss_join_kernel(Args a, const float
 
 }  // namespace
 
-SortPlan sort_plan(const Args &a, int lanes) {
+SortPlan sort_plan(const Args &a, int lanes, int threads) {
   SortPlan p;
   int bits = 1;
   while (bits < 31 && (int64_t)1 << bits <= a.items) ++bits;  // numbers 0 .. items
@@ -706,11 +807,12 @@ SortPlan sort_plan(const Args &a, int lanes) {
   p.bits = (bits + p.passes - 1) / p.passes;
   p.entries = (int64_t)a.rows * (a.n + 1);
   p.tiles = (p.entries + kTile - 1) / kTile;
-  // long chunks leave fewer sums to join, short ones make more groups of lanes: enough for 1024 threads an SM twice over, if
-  // there are that many; so few entries that they never fill the GPU go in the shortest ones
+  // enough groups of lanes for 1024 threads an SM twice over, if there are that many entries; so few that they never fill the
+  // GPU go in the shortest chunks
   p.chunk = 512;
   while (p.chunk > (p.entries <= kSmallEntries ? 8 : 32) && p.entries / p.chunk * lanes < 2LL * kSMs * 1024) p.chunk /= 2;
-  p.chunks = (p.entries + p.chunk - 1) / p.chunk;
+  p.span = p.chunk * (threads / lanes);
+  p.spans = (p.entries + p.span - 1) / p.span;
   return p;
 }
 
@@ -722,7 +824,7 @@ Scratch carve(const Args &a, void *base) {
     off += (bytes + 255) / 256 * 256;
     return r;
   };
-  const SortPlan p = sort_plan(a, lanes_of(a.groups));  // (narrow groups take the shortest chunks)
+  const SortPlan p = sort_plan(a, lanes_of(a.groups), kThreads), m = sort_plan(a, 32, kMmaThreads);
   const size_t list = (size_t)p.entries * sizeof(uint32_t);
   s.sums = reinterpret_cast<double2 *>(take(kForwardBytes));
   for (int i = 0; i < 2; ++i) {
@@ -732,7 +834,7 @@ Scratch carve(const Args &a, void *base) {
   s.hist = reinterpret_cast<uint32_t *>(take((size_t)p.tiles * ((size_t)1 << p.bits) * sizeof(uint32_t)));
   s.totals = reinterpret_cast<uint32_t *>(take(kMaxDigits * sizeof(uint32_t)));
   s.range = reinterpret_cast<uint32_t *>(take((size_t)a.items * 2 * sizeof(uint32_t)));
-  s.part = reinterpret_cast<float *>(take((size_t)p.chunks * 2 * a.cols * sizeof(float)));
+  s.part = reinterpret_cast<float *>(take((size_t)(p.spans > m.spans ? p.spans : m.spans) * 2 * a.cols * sizeof(float)));
   s.bytes = off;
   return s;
 }
@@ -741,7 +843,7 @@ int launch_items(const Args &a, int dtype, const void *hidden, const void *table
                  const float *grad_loss, void *dhidden, void *dtable, int width, const Scratch &s, cudaStream_t st) {
   const bool dense = (int64_t)a.rows * (a.n + 1) / a.items >= kDense;  // (sixteen entries at a time want several an item)
   const int lines = dense ? mma_lines(a, dtype, width) : 0;
-  const SortPlan p = sort_plan(a, lines ? 32 : lanes_of(a.groups));
+  const SortPlan p = lines ? sort_plan(a, 32, kMmaThreads) : sort_plan(a, lanes_of(a.groups), kThreads);
   const uint32_t entries = dtable ? (uint32_t)p.entries : 0;
   const Split by = split_by((uint32_t)a.n + 1);
   int at = 1;  // the buffer that holds the list
@@ -777,9 +879,9 @@ int launch_items(const Args &a, int dtype, const void *hidden, const void *table
   const uint32_t *keys = s.keys[at], *vals = s.vals[at];
   if (entries && lines) {
     with_lines(lines, a.cols, [&](auto n, auto all) {
-      constexpr int NL = decltype(n)::value, per = kMmaThreads / 32;
+      constexpr int NL = decltype(n)::value;
       LaunchScope ls(K_LOSS_ITEMS, st);
-      launch_chained(loss_items_mma_kernel<NL, decltype(all)::value>, dim3((unsigned)((p.chunks + per - 1) / per)),
+      launch_chained(loss_items_mma_kernel<NL, decltype(all)::value>, dim3((unsigned)p.spans),
                      dim3(kMmaThreads), 0, st, a, static_cast<const __nv_bfloat16 *>(hidden),
                      static_cast<const __nv_bfloat16 *>(table), lse, grad_loss, keys, vals, entries, p.chunk,
                      static_cast<__nv_bfloat16 *>(dtable), s.part, s.range);
@@ -792,8 +894,8 @@ int launch_items(const Args &a, int dtype, const void *hidden, const void *table
       constexpr int W = decltype(w)::value, per = kThreads / P::LPC;
       if (entries && !lines) {
         LaunchScope ls(K_LOSS_ITEMS, st);
-        launch_chained(dense ? loss_items_kernel<T, W, P, true> : loss_items_kernel<T, W, P, false>,
-                       dim3((unsigned)((p.chunks + per - 1) / per)), dim3(kThreads), 0, st, a, static_cast<const T *>(hidden),
+        launch_chained(loss_items_kernel<T, W, P>,
+                       dim3((unsigned)p.spans), dim3(kThreads), 0, st, a, static_cast<const T *>(hidden),
                        static_cast<const T *>(table), lse, grad_loss, keys, vals, entries, p.chunk, static_cast<T *>(dtable),
                        s.part, s.range);
       }
@@ -803,7 +905,7 @@ int launch_items(const Args &a, int dtype, const void *hidden, const void *table
       if (ctas == 0) return;
       LaunchScope ls(K_LOSS_JOIN, st);
       launch_chained(loss_join_kernel<T, W, P>, dim3((unsigned)ctas), dim3(kThreads), 0, st, a, lse, grad_loss,
-                     keys, (const uint32_t *)s.range, entries, p.chunk, (const float *)s.part, static_cast<T *>(dtable),
+                     keys, (const uint32_t *)s.range, entries, p.span, (const float *)s.part, static_cast<T *>(dtable),
                      (unsigned)join, grad_hidden, static_cast<T *>(dhidden));
     });
   });

@@ -44,6 +44,7 @@ __global__ void __launch_bounds__(kThreads) loss_rows_kernel(Args a, const T *__
   double2 mine = make_double2(0.0, 0.0);
   for (int64_t r = (int64_t)blockIdx.x * (kThreads / 32) + warp; r < a.rows; r += (int64_t)gridDim.x * (kThreads / 32)) {
     const int row = (int)r, target = row_target(a, row);
+    int id = lane <= a.n ? candidate(a, row, target, lane) : -1;  // of the candidates c0 .. c0 + 31, one a lane; -1: none
     Group acc[V];
 #pragma unroll
     for (int v = 0; v < V; ++v)
@@ -60,7 +61,8 @@ __global__ void __launch_bounds__(kThreads) loss_rows_kernel(Args a, const T *__
       }
       float top = -INFINITY, total = 0.f, own = 0.f;
       for (int c0 = 0; c0 <= a.n; c0 += 32) {
-        const int id = c0 + lane <= a.n ? candidate(a, row, target, c0 + lane) : -1;
+        int64_t next = -1;
+        if (c0 + 32 + lane <= a.n) next = load_negative(a, row, c0 + 32 + lane);
         const int steps = (min(32, a.n + 1 - c0) + CPW - 1) / CPW;
         for (int k = 0; k < steps; k += U) {
           Group w[U][V];
@@ -107,6 +109,7 @@ __global__ void __launch_bounds__(kThreads) loss_rows_kernel(Args a, const T *__
             top = high;
           }
         }
+        id = valid_negative(a, target, next);
       }
       // the groups of lanes, joined (one that has met no candidate has top = -inf and weighs nothing)
       float high = top;
@@ -145,10 +148,11 @@ __global__ void __launch_bounds__(kThreads) loss_rows_kernel(Args a, const T *__
   close_sums<kThreads>(mine, sums, loss, lse + a.rows);
 }
 
-// The same on the matrix units: a warp scores 16 candidates at a time, the next 16 rows are under way meanwhile.  What is no
-// candidate is read as the target's row and weighs nothing.
+// The same on the matrix units: a warp scores 16 candidates at a time.  What is no candidate is read as the target's row and
+// weighs nothing.  Other warps work while a warp's 16 rows are under way: with 64 registers an SM holds 32 of them, and two
+// buffers of rows a warp in 80 registers were slower (324 us against 305, 131072 x 128 candidates x 64).
 template <int NL, bool FULL, bool GRAD>
-__global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 6 : 4)
+__global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 8 : 4)
     loss_rows_mma_kernel(Args a, const __nv_bfloat16 *__restrict__ hidden, const __nv_bfloat16 *__restrict__ table,
                          float *__restrict__ lse, float *__restrict__ dh, double2 *__restrict__ sums,
                          float *__restrict__ loss) {
@@ -158,6 +162,7 @@ __global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 6 : 4)
   double2 mine = make_double2(0.0, 0.0);
   for (int64_t r = (int64_t)blockIdx.x * (kMmaThreads / 32) + warp; r < a.rows; r += (int64_t)gridDim.x * (kMmaThreads / 32)) {
     const int row = (int)r, target = row_target(a, row);
+    int id = lane <= a.n ? candidate(a, row, target, lane) : -1;  // of the candidates c0 .. c0 + 31, one a lane; -1: none
     float row_lse = 0.f;
     float2 grad[NL];
 #pragma unroll
@@ -170,9 +175,7 @@ __global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 6 : 4)
       for (int c = 0; c < NL; ++c)
 #pragma unroll
         for (int i = 0; i < 4; ++i) acc[c][i] = make_float2(0.f, 0.f);
-      // candidates c0 .. c0 + 31, one a lane; there: a bit for each
-      auto ids_from = [&](int c0, uint32_t &there) {
-        const int id = c0 + lane <= a.n ? candidate(a, row, target, c0 + lane) : -1;
+      auto rows_of = [&](int id, uint32_t &there) {  // there: a bit for each candidate
         there = __ballot_sync(0xffffffffu, id >= 0);
         return (uint32_t)(id >= 0 ? id : target);
       };
@@ -206,19 +209,20 @@ __global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 6 : 4)
         if (GRAD) weigh16<NL>(w, l, acc);
         return first;
       };
-      Rows16<NL> w[2];
-      uint32_t there, there_next = 0, ids = ids_from(0, there), next = 0;
-      from_table.load16(ids, 0, w[0]);
+      Rows16<NL> w;
       for (int c0 = 0; c0 <= a.n; c0 += 32) {
-        const bool second = c0 + 16 <= a.n, third = c0 + 32 <= a.n;
-        if (third) next = ids_from(c0 + 32, there_next);
-        if (second) from_table.load16(ids, 16, w[1]);
-        const float l0 = score(w[0], there);
+        uint32_t there;
+        const uint32_t ids = rows_of(id, there);
+        from_table.load16(ids, 0, w);
+        int64_t raw = -1;  // (the next 32 are not looked at before they are wanted: whoever looks waits)
+        if (c0 + 32 + lane <= a.n) raw = load_negative(a, row, c0 + 32 + lane);
+        const float l0 = score(w, there);
         if (c0 == 0) own = __shfl_sync(0xffffffffu, l0, 0) * kLog2e;
-        if (third) from_table.load16(next, 0, w[0]);
-        if (second) score(w[1], there >> 16);
-        ids = next;
-        there = there_next;
+        if (c0 + 16 <= a.n) {
+          from_table.load16(ids, 16, w);
+          score(w, there >> 16);
+        }
+        id = valid_negative(a, target, raw);
       }
       float high = top;
 #pragma unroll
