@@ -56,6 +56,7 @@ __global__ void __launch_bounds__(kCopyThreads) copy_rows_kernel(int H, int L, u
 extern "C" int blossom_copy_rows(int32_t B, int32_t H, int32_t L, int32_t row_bytes, const void *src, const int64_t *src_strides,
                                  void *dst, const int64_t *dst_strides, blossom_stream_t stream) {
   using namespace blossom;
+  prof_break();
   if (B < 1 || H < 1 || L < 1 || !src || !dst || !src_strides || !dst_strides) return BLOSSOM_ERR_INVALID_ARG;
   // 16-byte pieces: a row of 2^n of them, and every row of either side on a 16-byte boundary
   const int chunks = row_bytes / 16;
