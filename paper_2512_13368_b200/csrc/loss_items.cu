@@ -34,7 +34,7 @@ __device__ __forceinline__ uint32_t entry_val(const Args &a, const Split &by, ui
 
 // Counts of a tile's digits, to hist[digit][tile].  The first pass makes the keys.
 template <bool FIRST>
-__global__ void __launch_bounds__(kSortThreads) sort_count_kernel(Args a, Split by, uint32_t *__restrict__ keys, uint32_t entries,
+__global__ void __launch_bounds__(kSortThreads, 8) sort_count_kernel(Args a, Split by, uint32_t *__restrict__ keys, uint32_t entries,
                                                                   int shift, int bits, uint32_t *__restrict__ hist) {
   __shared__ uint32_t count[kMaxDigits];
   __shared__ int targets[FIRST ? kTile + 1 : 1];  // of the positions that the tile belongs to
@@ -364,7 +364,7 @@ __device__ __forceinline__ bool add_groups(const Ends<NG> &ends, int g, uint32_t
 }
 
 template <typename T, int W, typename P>
-__global__ void __launch_bounds__(kThreads, P::V == 1 ? 4 : P::V == 2 ? 2 : 1)
+__global__ void __launch_bounds__(kThreads, P::V == 1 ? (sizeof(T) == 2 ? 4 : 3) : P::V == 2 ? 2 : 1)
     loss_items_kernel(Args a, const T *__restrict__ hidden, const T *__restrict__ table, const float *__restrict__ lse,
                       const float *__restrict__ grad_loss, const uint32_t *__restrict__ keys, const uint32_t *__restrict__ vals,
                       uint32_t entries, int chunk, T *__restrict__ dtable, float *__restrict__ part,

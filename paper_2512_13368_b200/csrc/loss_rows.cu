@@ -34,11 +34,11 @@ __device__ __forceinline__ void close_sums(double2 mine, double2 *sums, float *l
 }
 
 template <typename T, int W, typename P, bool GRAD>
-__global__ void __launch_bounds__(kThreads) loss_rows_kernel(Args a, const T *__restrict__ hidden, const T *__restrict__ table,
+__global__ void __launch_bounds__(kThreads, P::V == 1 ? 4 : P::V == 2 ? 2 : 1) loss_rows_kernel(Args a, const T *__restrict__ hidden, const T *__restrict__ table,
                                                              float *__restrict__ lse, float *__restrict__ dh,
                                                              double2 *__restrict__ sums, float *__restrict__ loss) {
   using S = Strip<T, W, P>;
-  constexpr int LPC = P::LPC, V = P::V, CPW = 32 / LPC, U = V == 1 ? 4 : 1;
+  constexpr int LPC = P::LPC, V = P::V, CPW = 32 / LPC, U = V == 1 ? 2 : 1;
   grid_chain_enter();
   const int lane = (int)threadIdx.x % 32, warp = (int)threadIdx.x / 32, col = lane % LPC, sub = lane / LPC;
   double2 mine = make_double2(0.0, 0.0);
