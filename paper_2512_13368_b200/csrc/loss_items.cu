@@ -807,10 +807,9 @@ SortPlan sort_plan(const Args &a, int lanes, int threads) {
   p.bits = (bits + p.passes - 1) / p.passes;
   p.entries = (int64_t)a.rows * (a.n + 1);
   p.tiles = (p.entries + kTile - 1) / kTile;
-  // enough groups of lanes for 1024 threads an SM twice over, if there are that many entries; so few that they never fill the
-  // GPU go in the shortest chunks
+  // enough groups of lanes for 1024 threads an SM twice over, if there are that many entries
   p.chunk = 512;
-  while (p.chunk > (p.entries <= kSmallEntries ? 8 : 32) && p.entries / p.chunk * lanes < 2LL * kSMs * 1024) p.chunk /= 2;
+  while (p.chunk > (threads == kMmaThreads ? 32 : 8) && p.entries / p.chunk * lanes < 2LL * kSMs * 1024) p.chunk /= 2;
   p.span = p.chunk * (threads / lanes);
   p.spans = (p.entries + p.span - 1) / p.span;
   return p;

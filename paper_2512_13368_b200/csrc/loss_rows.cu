@@ -33,18 +33,38 @@ __device__ __forceinline__ void close_sums(double2 mine, double2 *sums, float *l
   }
 }
 
+// Few positions with many candidates: a block takes a position, its warps every NW-th 32 candidates, joined in shared memory.
+template <int NW>
+struct Shares {  // of a block's warps
+  float high[NW], total[NW];
+  // the common reference point, and the sum in its units
+  __device__ __forceinline__ void join(float &top, float &sum) const {
+    top = high[0];
+#pragma unroll
+    for (int i = 1; i < NW; ++i) top = fmaxf(top, high[i]);
+    sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) sum += total[i] * exp2f(high[i] - top);  // (0 from a warp that met no candidate)
+  }
+};
+
 template <typename T, int W, typename P, bool GRAD>
-__global__ void __launch_bounds__(kThreads, P::V == 1 ? 4 : P::V == 2 ? 2 : 1) loss_rows_kernel(Args a, const T *__restrict__ hidden, const T *__restrict__ table,
-                                                             float *__restrict__ lse, float *__restrict__ dh,
-                                                             double2 *__restrict__ sums, float *__restrict__ loss) {
+__global__ void __launch_bounds__(kThreads, P::V == 1 ? 4 : P::V == 2 ? 2 : 1)
+    loss_rows_kernel(Args a, int split, const T *__restrict__ hidden, const T *__restrict__ table, float *__restrict__ lse,
+                     float *__restrict__ dh, double2 *__restrict__ sums, float *__restrict__ loss) {
   using S = Strip<T, W, P>;
-  constexpr int LPC = P::LPC, V = P::V, CPW = 32 / LPC, U = V == 1 ? 2 : 1;
+  constexpr int LPC = P::LPC, V = P::V, CPW = 32 / LPC, U = V == 1 ? 2 : 1, NW = kThreads / 32;
+  __shared__ Shares<NW> shares;
+  __shared__ float shared_sums[GRAD ? NW : 1][V * 8][LPC];
   grid_chain_enter();
   const int lane = (int)threadIdx.x % 32, warp = (int)threadIdx.x / 32, col = lane % LPC, sub = lane / LPC;
   double2 mine = make_double2(0.0, 0.0);
-  for (int64_t r = (int64_t)blockIdx.x * (kThreads / 32) + warp; r < a.rows; r += (int64_t)gridDim.x * (kThreads / 32)) {
+  const int64_t step = split ? gridDim.x : (int64_t)gridDim.x * NW;
+  const int c_first = split ? 32 * warp : 0, c_step = split ? 32 * NW : 32;
+  for (int64_t r = split ? blockIdx.x : (int64_t)blockIdx.x * NW + warp; r < a.rows; r += step) {
     const int row = (int)r, target = row_target(a, row);
-    int id = lane <= a.n ? candidate(a, row, target, lane) : -1;  // of the candidates c0 .. c0 + 31, one a lane; -1: none
+    // of the candidates c0 .. c0 + 31, one a lane; -1: none
+    int id = c_first + lane <= a.n ? candidate(a, row, target, c_first + lane) : -1;
     Group acc[V];
 #pragma unroll
     for (int v = 0; v < V; ++v)
@@ -59,10 +79,10 @@ __global__ void __launch_bounds__(kThreads, P::V == 1 ? 4 : P::V == 2 ? 2 : 1) l
 #pragma unroll
         for (int i = 0; i < 4; ++i) h[v].p[i] = mul2(h[v].p[i], both(kLog2e));  // logits in units of log 2
       }
-      float top = -INFINITY, total = 0.f, own = 0.f;
-      for (int c0 = 0; c0 <= a.n; c0 += 32) {
-        int64_t next = -1;
-        if (c0 + 32 + lane <= a.n) next = load_negative(a, row, c0 + 32 + lane);
+      float top = -FLT_MAX, total = 0.f, own = 0.f;
+      for (int c0 = c_first; c0 <= a.n; c0 += c_step) {
+        int64_t next = -1;  // (not looked at before it is wanted: whoever looks waits)
+        if (c0 + c_step + lane <= a.n) next = load_negative(a, row, c0 + c_step + lane);
         const int steps = (min(32, a.n + 1 - c0) + CPW - 1) / CPW;
         for (int k = 0; k < steps; k += U) {
           Group w[U][V];
@@ -111,7 +131,7 @@ __global__ void __launch_bounds__(kThreads, P::V == 1 ? 4 : P::V == 2 ? 2 : 1) l
         }
         id = valid_negative(a, target, next);
       }
-      // the groups of lanes, joined (one that has met no candidate has top = -inf and weighs nothing)
+      // the groups of lanes, joined (one that has met no candidate weighs nothing)
       float high = top;
 #pragma unroll
       for (int o = LPC; o < 32; o <<= 1) high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, o));
@@ -119,26 +139,60 @@ __global__ void __launch_bounds__(kThreads, P::V == 1 ? 4 : P::V == 2 ? 2 : 1) l
       total *= weight;
 #pragma unroll
       for (int o = LPC; o < 32; o <<= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-      const float lse2 = high + log2f(total);
-      row_lse = lse2 * kLn2;
-      mine.x += (double)((lse2 - own) * kLn2);
-      mine.y += 1.0;
       if (GRAD) {
-        const float inv = weight / total;
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-          Group w = S::load(table + target * a.st, col, v, a.cols);
+        for (int v = 0; v < V; ++v)
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             float &x = acc[v].at(i);
-            x *= inv;
+            x *= weight;
 #pragma unroll
             for (int o = LPC; o < 32; o <<= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-            x -= w.at(i);
           }
+      }
+      if (split) {
+        if (lane == 0) shares.high[warp] = high, shares.total[warp] = total;
+        if (GRAD && sub == 0) {
+#pragma unroll
+          for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) shared_sums[warp][8 * v + i][col] = acc[v].at(i);
+        }
+        __syncthreads();
+        if (warp == 0) {
+          shares.join(high, total);
+          if (GRAD) {
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                float x = 0.f;
+#pragma unroll
+                for (int w = 0; w < NW; ++w) x += shared_sums[w][8 * v + i][col] * exp2f(shares.high[w] - high);
+                acc[v].at(i) = x;
+              }
+          }
+        }
+        __syncthreads();  // (the next row's shares may come)
+      }
+      const float lse2 = high + log2f(total);
+      row_lse = lse2 * kLn2;
+      if (!split || warp == 0) {
+        mine.x += (double)((lse2 - own) * kLn2);
+        mine.y += 1.0;
+      }
+      if (GRAD) {
+        const float inv = 1.f / total;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+          const Group w = S::load(table + target * a.st, col, v, a.cols);
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            acc[v].p[i] = fma2(acc[v].p[i], both(inv), make_float2(-w.p[i].x, -w.p[i].y));
         }
       }
     }
+    if (split && warp > 0) continue;
     if (lane == 0) lse[row] = row_lse;
     if (GRAD && sub == 0) {
 #pragma unroll
@@ -153,16 +207,22 @@ __global__ void __launch_bounds__(kThreads, P::V == 1 ? 4 : P::V == 2 ? 2 : 1) l
 // buffers of rows a warp in 80 registers were slower (324 us against 305, 131072 x 128 candidates x 64).
 template <int NL, bool FULL, bool GRAD>
 __global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 8 : 4)
-    loss_rows_mma_kernel(Args a, const __nv_bfloat16 *__restrict__ hidden, const __nv_bfloat16 *__restrict__ table,
+    loss_rows_mma_kernel(Args a, int split, const __nv_bfloat16 *__restrict__ hidden, const __nv_bfloat16 *__restrict__ table,
                          float *__restrict__ lse, float *__restrict__ dh, double2 *__restrict__ sums,
                          float *__restrict__ loss) {
+  constexpr int NW = kMmaThreads / 32;
+  __shared__ Shares<NW> shares;
+  __shared__ float2 shared_sums[NW][NL][32];
   grid_chain_enter();
   const int lane = (int)threadIdx.x % 32, warp = (int)threadIdx.x / 32, group = lane / 8;
   const Lanes16<NL, FULL> from_hidden(hidden, a.sh, a.cols), from_table(table, a.st, a.cols);
   double2 mine = make_double2(0.0, 0.0);
-  for (int64_t r = (int64_t)blockIdx.x * (kMmaThreads / 32) + warp; r < a.rows; r += (int64_t)gridDim.x * (kMmaThreads / 32)) {
+  const int64_t step = split ? gridDim.x : (int64_t)gridDim.x * NW;
+  const int c_first = split ? 32 * warp : 0, c_step = split ? 32 * NW : 32;
+  for (int64_t r = split ? blockIdx.x : (int64_t)blockIdx.x * NW + warp; r < a.rows; r += step) {
     const int row = (int)r, target = row_target(a, row);
-    int id = lane <= a.n ? candidate(a, row, target, lane) : -1;  // of the candidates c0 .. c0 + 31, one a lane; -1: none
+    // of the candidates c0 .. c0 + 31, one a lane; -1: none
+    int id = c_first + lane <= a.n ? candidate(a, row, target, c_first + lane) : -1;
     float row_lse = 0.f;
     float2 grad[NL];
 #pragma unroll
@@ -210,12 +270,12 @@ __global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 8 : 4)
         return first;
       };
       Rows16<NL> w;
-      for (int c0 = 0; c0 <= a.n; c0 += 32) {
+      for (int c0 = c_first; c0 <= a.n; c0 += c_step) {
         uint32_t there;
         const uint32_t ids = rows_of(id, there);
         from_table.load16(ids, 0, w);
         int64_t raw = -1;  // (the next 32 are not looked at before they are wanted: whoever looks waits)
-        if (c0 + 32 + lane <= a.n) raw = load_negative(a, row, c0 + 32 + lane);
+        if (c0 + c_step + lane <= a.n) raw = load_negative(a, row, c0 + c_step + lane);
         const float l0 = score(w, there);
         if (c0 == 0) own = __shfl_sync(0xffffffffu, l0, 0) * kLog2e;
         if (c0 + 16 <= a.n) {
@@ -231,27 +291,52 @@ __global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 8 : 4)
       total *= weight;
 #pragma unroll
       for (int o = 8; o < 32; o <<= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-      const float lse2 = high + log2f(total);
-      row_lse = lse2 * kLn2;
-      mine.x += (double)((lse2 - own) * kLn2);
-      mine.y += 1.0;
       if (GRAD) {
-        const float inv = weight / total;
 #pragma unroll
         for (int c = 0; c < NL; ++c)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) acc[c][i].x *= inv, acc[c][i].y *= inv;
+          for (int i = 0; i < 4; ++i) acc[c][i] = mul2(acc[c][i], both(weight));
         scatter16<NL>(acc, grad);
+      }
+      if (split) {
+        if (lane == 0) shares.high[warp] = high, shares.total[warp] = total;
+        if (GRAD) {
+#pragma unroll
+          for (int c = 0; c < NL; ++c) shared_sums[warp][c][lane] = grad[c];
+        }
+        __syncthreads();
+        if (warp == 0) {
+          shares.join(high, total);
+          if (GRAD) {
+#pragma unroll
+            for (int c = 0; c < NL; ++c) {
+              grad[c] = both(0.f);
+#pragma unroll
+              for (int w = 0; w < NW; ++w) grad[c] = fma2(shared_sums[w][c][lane], both(exp2f(shares.high[w] - high)), grad[c]);
+            }
+          }
+        }
+        __syncthreads();  // (the next row's shares may come)
+      }
+      const float lse2 = high + log2f(total);
+      row_lse = lse2 * kLn2;
+      if (!split || warp == 0) {
+        mine.x += (double)((lse2 - own) * kLn2);
+        mine.y += 1.0;
+      }
+      if (GRAD) {
+        const float inv = 1.f / total;
 #pragma unroll
         for (int c = 0; c < NL; ++c) {
           const int col = scattered_column(c);
           if (FULL || col < a.cols) {
-            const uint32_t w = *reinterpret_cast<const uint32_t *>(table + target * a.st + col);
-            grad[c].x -= __uint_as_float(w << 16), grad[c].y -= __uint_as_float(w & 0xffff0000u);
+            const float2 w = rows::halves(*reinterpret_cast<const uint32_t *>(table + target * a.st + col));
+            grad[c] = fma2(grad[c], both(inv), make_float2(-w.x, -w.y));
           }
         }
       }
     }
+    if (split && warp > 0) continue;
     if (lane == 0) lse[row] = row_lse;
     if (GRAD) {
 #pragma unroll
@@ -349,17 +434,19 @@ extern "C" int blossom_sampled_loss_fwd(const blossom_loss_params *params, const
   const int width = al.elements(a.cols, esz), lines = loss::mma_lines(a, params->dtype, width);
   const int warps = (lines ? loss::kMmaThreads : loss::kThreads) / 32;  // a row each
   const int64_t want = ((int64_t)a.rows + warps - 1) / warps, most = loss::kSMs * 64 / warps;
-  const int ctas = (int)(want < most ? want : most);
+  // (a block a row while the rows alone do not give every SM its warps)
+  const int split = a.n >= 32 && a.rows <= loss::kSMs * 8;
+  const int ctas = split ? a.rows : (int)(want < most ? want : most);
   auto launch = [&](auto kern, int threads, auto... args) {
     LaunchScope ls(K_LOSS_ROWS, st);
-    launch_chained(kern, dim3((unsigned)ctas), dim3((unsigned)threads), 0, st, args..., loss_out);
+    launch_chained(kern, dim3((unsigned)ctas), dim3((unsigned)threads), 0, st, a, split, args..., loss_out);
   };
   if (ctas && lines) {
     loss::with_lines(lines, a.cols, [&](auto n, auto all) {
       constexpr int NL = decltype(n)::value;
       constexpr bool FULL = decltype(all)::value;
       launch(grad_hidden ? loss::loss_rows_mma_kernel<NL, FULL, true> : loss::loss_rows_mma_kernel<NL, FULL, false>,
-             loss::kMmaThreads, a, static_cast<const __nv_bfloat16 *>(hidden), static_cast<const __nv_bfloat16 *>(table), lse,
+             loss::kMmaThreads, static_cast<const __nv_bfloat16 *>(hidden), static_cast<const __nv_bfloat16 *>(table), lse,
              grad_hidden, sums);
     });
   } else if (ctas) {
@@ -368,7 +455,7 @@ extern "C" int blossom_sampled_loss_fwd(const blossom_loss_params *params, const
       rows::with_type(params->dtype, width, [&](auto t, auto w) {
         using T = decltype(t);
         constexpr int W = decltype(w)::value;
-        launch(grad_hidden ? loss::loss_rows_kernel<T, W, P, true> : loss::loss_rows_kernel<T, W, P, false>, loss::kThreads, a,
+        launch(grad_hidden ? loss::loss_rows_kernel<T, W, P, true> : loss::loss_rows_kernel<T, W, P, false>, loss::kThreads,
                static_cast<const T *>(hidden), static_cast<const T *>(table), lse, grad_hidden, sums);
       });
     });
