@@ -598,15 +598,20 @@ __global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 7 : 4)
     before = __shfl_sync(0xffffffffu, x.key, 31);
   };
   auto walk = [&](const Rows16<NL> &h, const Entries &x, int half) {
-    float top[4];
+    const float minus = -x.top * kLog2e;
+    float shift[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) top[j] = __shfl_sync(0xffffffffu, x.top, half + 4 * j + group);
-    const uint32_t targets = __ballot_sync(0xffffffffu, x.val >> 31) >> (half + group);
+    for (int j = 0; j < 4; ++j) shift[j] = __shfl_sync(0xffffffffu, minus, half + 4 * j + group);
+    const uint32_t targets = __ballot_sync(0xffffffffu, x.val >> 31) >> half & 0xffffu;
     for (;;) {
       float p[4];
       dots16<NL>(h, w, p);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) p[j] = exp2f((p[j] - top[j]) * kLog2e) - (targets >> (4 * j) & 1 ? 1.f : 0.f);
+      for (int j = 0; j < 4; ++j) p[j] = exp2f(fmaf(p[j], kLog2e, shift[j]));
+      if (targets) {  // (the same for the warp)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) p[j] -= targets >> (4 * j + group) & 1 ? 1.f : 0.f;
+      }
       uint32_t others = __ballot_sync(0xffffffffu, x.key != cur) >> half & 0xffffu;
       if (!others) {
         weigh16<NL>(h, p, acc);

@@ -206,7 +206,7 @@ __global__ void __launch_bounds__(kThreads, P::V == 1 ? 4 : P::V == 2 ? 2 : 1)
 // weighs nothing.  Other warps work while a warp's 16 rows are under way: with 64 registers an SM holds 32 of them, and two
 // buffers of rows a warp in 80 registers were slower (324 us against 305, 131072 x 128 candidates x 64).
 template <int NL, bool FULL, bool GRAD>
-__global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 8 : 4)
+__global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 8 : 5)
     loss_rows_mma_kernel(Args a, int split, const __nv_bfloat16 *__restrict__ hidden, const __nv_bfloat16 *__restrict__ table,
                          float *__restrict__ lse, float *__restrict__ dh, double2 *__restrict__ sums,
                          float *__restrict__ loss) {
@@ -239,21 +239,24 @@ __global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 8 : 4)
         there = __ballot_sync(0xffffffffu, id >= 0);
         return (uint32_t)(id >= 0 ? id : target);
       };
-      float top = -FLT_MAX, total = 0.f, own = 0.f;  // of a group of lanes: its four rows of every 16
+      // of a group of lanes: its four rows of every 16; logits as they come (top: half the lowest number, so that log2(e) times
+      // it is one)
+      float top = -0.5f * FLT_MAX, total = 0.f, own = 0.f;
       auto score = [&](const Rows16<NL> &w, uint32_t there) {
-        float l[4], high = top;
+        float l[4];
         dots16<NL>(w, h, l);
         const float first = l[0];
-        there >>= group;
+        if (~there & 0xffffu) {  // (the same for the warp)
+          there >>= group;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          l[j] = there >> (4 * j) & 1 ? l[j] * kLog2e : -INFINITY;  // in units of log 2
-          high = fmaxf(high, l[j]);
+          for (int j = 0; j < 4; ++j)
+            if (!(there >> (4 * j) & 1)) l[j] = -INFINITY;
         }
-        // The reference point only moves if it has to by more than 2^10: the sums stay far from the type's limits, and their
-        // relative rounding does not depend on it.
-        if (high > top + 10.f) {
-          const float shrink = exp2f(top - high);
+        // The reference point only moves if it has to, by more than 2^10 in the exponentials: the sums stay far from the type's
+        // limits, and their relative rounding does not depend on it.
+        const float high = fmaxf(fmaxf(l[0], l[1]), fmaxf(l[2], l[3]));
+        if (high > top + 7.f) {
+          const float shrink = exp2f((top - high) * kLog2e);
           total *= shrink;
           if (GRAD) {
 #pragma unroll
@@ -263,8 +266,9 @@ __global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 8 : 4)
           }
           top = high;
         }
+        const float shift = -top * kLog2e;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) l[j] = exp2f(l[j] - top);
+        for (int j = 0; j < 4; ++j) l[j] = exp2f(fmaf(l[j], kLog2e, shift));
         total += (l[0] + l[1]) + (l[2] + l[3]);
         if (GRAD) weigh16<NL>(w, l, acc);
         return first;
@@ -284,6 +288,7 @@ __global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 8 : 4)
         }
         id = valid_negative(a, target, raw);
       }
+      top *= kLog2e;  // in units of log 2 from here on
       float high = top;
 #pragma unroll
       for (int o = 8; o < 32; o <<= 1) high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, o));
