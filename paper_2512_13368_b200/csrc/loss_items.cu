@@ -58,7 +58,7 @@ __global__ void __launch_bounds__(kSortThreads, 8) sort_count_kernel(Args a, Spl
       if (FIRST) {
         const uint32_t t = by(e);
         const int target = targets[t - t0];
-        if (target >= 0) key[r] = (uint32_t)candidate(a, (int)t, target, (int)(e - t * (uint32_t)(a.n + 1)));
+        if (target >= 0) key[r] = (uint32_t)candidate<true>(a, (int)t, target, (int)(e - t * (uint32_t)(a.n + 1)));
         key[r] = min(key[r], none);  // (-1: no candidate)
       } else {
         key[r] = keys[e];
@@ -165,8 +165,8 @@ __global__ void __launch_bounds__(kSortThreads, 4) sort_move_kernel(Args a, Spli
   uint32_t key[kSortPerThread], rank[kSortPerThread / 2];  // (two ranks a word)
 #pragma unroll
   for (int r = 0; r < kSortPerThread; ++r) {
-    const uint32_t e = e0 + 32 * r;
-    key[r] = e < entries ? keys[e] : 0;
+    const uint32_t e = e0 + 32 * r;  // (read for the last time, see load_id)
+    key[r] = e < entries ? __ldcs(keys + e) : 0;
   }
   uint16_t *mine = count + warp * digits;
 #pragma unroll
@@ -232,7 +232,7 @@ __global__ void __launch_bounds__(kSortThreads, 4) sort_move_kernel(Args a, Spli
     if (e0 + 32 * r < entries) {
       const uint32_t at = mine[key[r] >> shift & mask] + (r % 2 ? rank[r / 2] >> 16 : rank[r / 2] & 0xffffu);
       sk[at] = key[r];
-      sv[at] = FIRST ? e0 + 32 * r : vals[e0 + 32 * r];
+      sv[at] = FIRST ? e0 + 32 * r : __ldcs(vals + e0 + 32 * r);
     }
   __syncthreads();
   const uint32_t here = entries - tile0 < (uint32_t)kTile ? entries - tile0 : (uint32_t)kTile;
@@ -264,7 +264,7 @@ __global__ void __launch_bounds__(kSmallThreads) sort_small_kernel(Args a, Split
     if (e < entries) {
       const uint32_t t = by(e);
       const int target = row_target(a, (int)t);
-      if (target >= 0) key[r] = min((uint32_t)candidate(a, (int)t, target, (int)(e - t * (uint32_t)(a.n + 1))), none);
+      if (target >= 0) key[r] = min((uint32_t)candidate<true>(a, (int)t, target, (int)(e - t * (uint32_t)(a.n + 1))), none);
       val[r] = entry_val(a, by, e);
     }
   }
