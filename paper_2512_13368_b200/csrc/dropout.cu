@@ -1,7 +1,10 @@
 // Dropout from a counter-based generator: out = kept ? x * scale : 0, the mask a function of (seed, step, site, row,
 // column) that nobody stores.  The backward is the same kernel on the upstream gradient.
 //
-// Bound: memory, each element once in and once out.
+// Bound: memory, each element once in and once out.  131072 x 64 bf16 is 33.6 MB a call, 5.2 us at the rate of a copy; a
+// launch takes about 12 us alone and less in a row of them, most of it the chain load, generator, store.  Through autograd a
+// forward and a backward take 49 us, whatever the size up to there: that is the host's part of it.  Two rows a thread are under
+// way at a time; the groups of threads are as narrow as the row, so that a row of 64 keeps 8 threads and none idles.
 #include "rows.cuh"
 
 namespace blossom {

@@ -232,7 +232,8 @@ __device__ __forceinline__ void scatter16(const float2 (&acc)[NL][4], float2 (&o
 // the first of the two columns
 __device__ __forceinline__ int scattered_column(int c) { return 64 * c + 8 * ((int)threadIdx.x % 8) + 2 * (((int)threadIdx.x % 32) / 8); }
 // Lines of 64 columns where the matrix units take the rows (bf16, 16-byte aligned rows of up to 128 columns less than 4 GiB
-// apart), else 0.
+// apart), else 0.  Against groups of lanes, 131072 x 128 x 64: positions 286 us to 419, items 293 to 589; 32768 x 128 x 128:
+// 139 to 204, 220 to 283.
 inline int mma_lines(const Args &a, int dtype, int width) {
   if (dtype != BLOSSOM_DTYPE_BF16 || width != 8 || a.cols > 128 || a.sh > 0x7fffffffLL || a.st > 0x7fffffffLL) return 0;
   return a.cols <= 64 ? 1 : 2;

@@ -5,17 +5,22 @@
 // the same order every time), then groups of lanes walk equal chunks of the sorted list: the item's row of the table stays
 // in registers, each position's hidden row is read once for both the logit that is formed again and the sum.  An item
 // whose entries lie in one chunk is written there and then; the sums of others go to scratch, one a chunk, and are
-// added up in order.  No atomics: every sum has a fixed order whatever the popularity of the items.
+// added up in order.  No atomics on sums: every one has a fixed order whatever the popularity of the items.
 #include "loss.cuh"
 
 namespace blossom {
 namespace loss {
 namespace {
 
-// Up to so many tiles a block of the second kernel adds their counts up itself (64 loads a digit, against a launch).
-constexpr int kTilesWithoutScan = 64;
+// Up to so many tiles a block of the second kernel adds their counts up itself, instead of a kernel in between (whole step at 4
+// tiles 46 us against 51, at 16 58 against 56, at 64 120 against 76).
+constexpr int kTilesWithoutScan = 8;
 
 // ---- the sort ------------------------------------------------------------------------------------
+// Bound: each pass reads the keys twice and the list once and writes it once: 131072 x 128 entries of 50001 items, two passes,
+// 0.9 GB, 140 us at the rate of a copy.  It takes 310 us: counts 68 (with the keys made from 134 MB of ids) and 25, scans 12,
+// moves 96 each (issue slots half busy: eight ballots an entry find the lanes of the same digit, and 64 registers leave
+// half of an SM's warps; a warp's match instruction took longer than the ballots).  Tiles of 4096 entries in 256 threads.
 // Entry e of the unsorted list is candidate e % (n + 1) of position e / (n + 1); what is no candidate gets the item
 // number `items` and ends up behind all others.
 struct Split {  // e / (n + 1) for e < 2^31: a product and a shift
@@ -32,7 +37,7 @@ __device__ __forceinline__ uint32_t entry_val(const Args &a, const Split &by, ui
   return t | (e == t * (uint32_t)(a.n + 1) ? 0x80000000u : 0u);
 }
 
-// Counts of a tile's digits, to hist[digit][tile].  The first pass makes the keys.
+// Counts of a tile's digits, to hist[digit][tile].  The first pass makes the keys.  Bound: 61 % of the issue slots (first pass).
 template <bool FIRST>
 __global__ void __launch_bounds__(kSortThreads, 8) sort_count_kernel(Args a, Split by, uint32_t *__restrict__ keys, uint32_t entries,
                                                                   int shift, int bits, uint32_t *__restrict__ hist) {
@@ -242,7 +247,9 @@ __global__ void __launch_bounds__(kSortThreads, 4) sort_move_kernel(Args a, Spli
     vals_out[at] = FIRST ? entry_val(a, by, sv[i]) : sv[i];
   }
 }
-// Few entries: the whole sort in one block, in shared memory.
+
+// Few entries: the whole sort in one block, in shared memory, instead of in four launches and more (up to 8192: 25 us against
+// 45; 4096: 19 against 42; 256: 15 against 35).  Bound: the latency of its steps.
 constexpr int kSmallThreads = 1024, kSmallPerThread = 8, kSmallEntries = kSmallThreads * kSmallPerThread, kSmallBits = 8;
 constexpr size_t kSmallSmem = 2 * kSmallEntries * sizeof(uint32_t) + ((kSmallThreads / 32) << kSmallBits) * sizeof(uint16_t);
 __global__ void __launch_bounds__(kSmallThreads) sort_small_kernel(Args a, Split by, uint32_t entries, int passes,
@@ -340,12 +347,14 @@ constexpr size_t move_smem(int bits) {
 }
 
 // ---- sums over an item's entries ---------------------------------------------------------------
+// Bound: the hidden rows come from L2, one an entry.  131072 x 128 entries x 64 bf16: 2.1 GB in 290 us, 7.4 TB/s, with 70 % of the
+// issue slots busy; 32768 x 128 x 128 with 25 entries an item: 220 us; fp32, 12795 x 100 x 50: 68 us.
 // A block's groups of lanes (or warps) walk consecutive chunks, together a span of the list.  An item whose entries lie in one
 // chunk is written there and then.  The others' sums meet in shared memory: a group leaves that of its first item there if
 // the item began before its chunk, and the group in whose chunk an item began adds up those of the groups behind it.
 // What reaches over the span's ends goes to scratch, at most two sums a span: [0] of the span's first item if it began
 // before the span or at its start, [1] of its last item if that began inside.
-constexpr int kThreads = 256, kItemsPerGroup = 2, kDense = 8;
+constexpr int kThreads = 256, kItemsPerGroup = 2, kDense = 12;
 
 template <int NG>
 struct Ends {  // of every group's chunk
@@ -516,7 +525,9 @@ __global__ void __launch_bounds__(kThreads, P::V == 1 ? (sizeof(T) == 2 ? 4 : 3)
 }
 
 // The same on the matrix units: a warp walks a chunk 16 entries at a time, their hidden rows the first operand, the item's
-// row the second.  Sixteen entries of more than one item go through once an item.
+// row the second.  Sixteen entries of more than one item go through once an item, so it pays from kDense entries an item on
+// (16384 x 64 entries, against entry by entry: 8 an item 66 us to 57, with 128 columns 113 to 89; 16 an item 49 to 55, 78 to
+// 82; 32 an item 39 to 54, 60 to 80).  Blocks an SM: 7 and, with 128 columns, 4 (8 and 5: 291 us as with 7, 254 against 223).
 template <int NL, bool FULL>
 __global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 7 : 4)
     loss_items_mma_kernel(Args a, const __nv_bfloat16 *__restrict__ hidden, const __nv_bfloat16 *__restrict__ table,
@@ -682,7 +693,8 @@ __global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 7 : 4)
 }
 
 // The last kernel: blocks up to `join_ctas` finish the table's gradient, those behind them scale that of the hidden rows
-// (g / count * grad_hidden, rounded once).
+// (g / count * grad_hidden, rounded once).  Bound: memory and the latency of the ranges' checks; 131072 positions and 50001 items
+// of 64 columns (50 MB in, 23 MB out) 14 us, 32768 and 165001 of 128: 22 us.
 // Table: items without entries (zeros) and those whose entries reach over a span's end: their spans' sums, in order.  A
 // group of lanes takes two items one after another; items of many spans are left to the whole block.
 template <typename T, int W, typename P>
