@@ -18,8 +18,8 @@ constexpr int kTilesWithoutScan = 8;
 
 // ---- the sort ------------------------------------------------------------------------------------
 // Bound: each pass reads the keys twice and the list once and writes it once: 131072 x 128 entries of 50001 items, two passes,
-// 0.9 GB, 140 us at the rate of a copy.  It takes 310 us: counts 68 (with the keys made from 134 MB of ids) and 25, scans 12,
-// moves 96 each (issue slots half busy: eight ballots an entry find the lanes of the same digit, and 64 registers leave
+// 0.9 GB, 140 us at the rate of a copy.  It takes 310 us: counts 68 (with the keys made from 134 MB of ids) and 23, scans 10,
+// moves 97 each (issue slots 55 - 61 % busy: eight ballots an entry find the lanes of the same digit, and 64 registers leave
 // half of an SM's warps; a warp's match instruction took longer than the ballots).  Tiles of 4096 entries in 256 threads.
 // Entry e of the unsorted list is candidate e % (n + 1) of position e / (n + 1); what is no candidate gets the item
 // number `items` and ends up behind all others.
@@ -37,7 +37,7 @@ __device__ __forceinline__ uint32_t entry_val(const Args &a, const Split &by, ui
   return t | (e == t * (uint32_t)(a.n + 1) ? 0x80000000u : 0u);
 }
 
-// Counts of a tile's digits, to hist[digit][tile].  The first pass makes the keys.  Bound: 61 % of the issue slots (first pass).
+// Counts of a tile's digits, to hist[digit][tile].  The first pass makes the keys.  Issue slots 66 - 72 % busy.
 template <bool FIRST>
 __global__ void __launch_bounds__(kSortThreads, 8) sort_count_kernel(Args a, Split by, uint32_t *__restrict__ keys, uint32_t entries,
                                                                   int shift, int bits, uint32_t *__restrict__ hist) {
