@@ -4,8 +4,9 @@
 // dx = dz where the dropout kept, scaled; dweight = sum over rows of dout n, dbias = sum over rows of dout.
 // z and the mask are formed again: reading x and residual moves the bytes that a stored z would, and z is not rounded.
 //
-// Bound: memory, three tensors in and two out.  32768 x 1024 bf16 with dropout: 336 MB in 68 us, 77 % of the rate of a copy;
-// 131072 x 64: 84 MB in 22 us.  128 registers leave 16 warps an SM for it, each with one row under way and one worked on.
+// Bound: memory, three tensors in and two out.  32768 x 1024 bf16 with dropout: 336 MB in 66 us, 79 % of the rate of a copy;
+// 131072 x 64: 84 MB in 20 us.  128 registers leave 16 warps an SM for it (20 and 24 in fewer spill: 85 and 79 us), the rows to
+// come are in shared memory.
 // Each thread owns its columns for all rows of its CTA, so the column
 // sums stay in registers; a CTA leaves one partial sum a column, and a second kernel adds the CTAs up in a fixed order.
 #include "rows.cuh"
@@ -14,16 +15,31 @@ namespace blossom {
 namespace rows {
 namespace {
 
+// What a CTA has of its SM.
+template <typename P>
+constexpr int resident = 65536 / (P::V > 1 ? 128 : 96) / P::threads;
 template <typename T, int W, typename P>
-__global__ void __launch_bounds__(P::threads, 65536 / (P::V > 1 ? 128 : 96) / P::threads)
+struct Shape {
+  using Rows = Ring<3 * P::V, P::threads>;
+  static constexpr int fixed = (P::V > 1 ? P::TPR * P::V * 32 : 0) + (P::TPR <= 32 ? P::TPR * P::V * 64 : 0) + 128;  // bytes
+  static constexpr int stages = W == 8 ? Rows::stages(resident<P>, fixed) : 0;  // 0: rows in registers
+  static constexpr int smem = stages * Rows::kStage;
+};
+
+template <typename T, int W, typename P>
+__global__ void __launch_bounds__(P::threads, resident<P>)
     norm_bwd_kernel(Args a, const T *__restrict__ x, const T *__restrict__ res, const void *__restrict__ weight,
                     const int64_t *__restrict__ rng, const float2 *__restrict__ stats, const T *__restrict__ dout,
                     T *__restrict__ dx, T *__restrict__ dres, float *__restrict__ part) {
-  constexpr bool AHEAD = sizeof(T) == 2;  // the next row is under way while this one is worked on (see the forward)
+  constexpr int STAGES = Shape<T, W, P>::stages;
+  // The next rows are under way while this one is worked on (see the forward): by asynchronous copies 33.5 M elements in rows
+  // of 64, 256, 1024, 4096 take 65, 63, 69, 73 us, with the next row in registers 76, 79, 69, 85.
+  constexpr bool AHEAD = STAGES == 0 && sizeof(T) == 2;
   constexpr int TPR = P::TPR, V = P::V, kGroups = TPR * V;
   __shared__ float2 buf[TPR > 32 ? TPR / 16 : 1];
   __shared__ float2 sums[TPR <= 32 ? TPR * V * 8 : 1];
   __shared__ float4 ws[V > 1 ? 2 * kGroups : 1];  // the weights of wide rows, two quarters a group, the groups side by side
+  extern __shared__ float4 stages[];
   grid_chain_enter();
   Generator gen;
   if (a.drop == 1) gen.read(rng);
@@ -49,23 +65,40 @@ __global__ void __launch_bounds__(P::threads, 65536 / (P::V > 1 ? 128 : 96) / P:
   const T *px = x + row * a.sx + 8 * lane, *pr = res + row * a.sr + 8 * lane, *pd = dout + row * a.so + 8 * lane;
   T *pdx = dx + row * a.sdx + 8 * lane, *pdr = dres + row * a.sdr + 8 * lane;
   Raw<T, W> xs[V], rs[V], ds[V];
-  float2 next_stats;
-  auto load = [&](uint32_t row) {
-    const bool there = row < rows;
-    next_stats = there ? stats[row] : both(0.f);
+  const typename Shape<T, W, P>::Rows ring(stages);
+  int stage = 0;
+  auto stats_of = [&](uint32_t row) { return row < rows ? stats[row] : both(0.f); };
+  auto load = [&](uint32_t row) {  // from px, pr and pd, which go on to the next
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const int valid = there ? a.cols - 8 * (lane + v * TPR) : 0;
-      xs[v].load(px + 8 * v * TPR, a.drop < 2 ? valid : 0);
-      rs[v].load(pr + 8 * v * TPR, res ? valid : 0);
-      ds[v].load(pd + 8 * v * TPR, valid);
+      const int valid = row < rows ? a.cols - 8 * (lane + v * TPR) : 0;
+      const T *x1 = px + 8 * v * TPR, *r1 = pr + 8 * v * TPR, *d1 = pd + 8 * v * TPR;
+      if constexpr (STAGES > 0) {
+        ring.copy(stage, 3 * v, x1, a.drop < 2 && valid > 0);
+        ring.copy(stage, 3 * v + 1, r1, res && valid > 0);
+        ring.copy(stage, 3 * v + 2, d1, valid > 0);
+      } else {
+        xs[v].load(x1, a.drop < 2 ? valid : 0);
+        rs[v].load(r1, res ? valid : 0);
+        ds[v].load(d1, valid);
+      }
     }
+    if constexpr (STAGES > 0) {
+      copies_end();
+      stage = stage + 1 == STAGES ? 0 : stage + 1;
+    }
+    px += step * a.sx, pr += step * a.sr, pd += step * a.so;
   };
   if (AHEAD) load(row);
+#pragma unroll 1
+  for (int i = 0; i < STAGES; ++i) load(row + i * step);
+  float2 next_stats = stats_of(row);
   // (`left`, the CTA's first row, is the same for all of its threads: they meet in row_sum)
   for (; left < rows; left += step, row += step, pdx += step * a.sdx, pdr += step * a.sdr) {
-    if (!AHEAD) load(row);
+    if constexpr (STAGES > 0) copies_wait<STAGES - 1>();
+    else if (!AHEAD) load(row);
     const float2 st = next_stats;
+    next_stats = stats_of(row + step);
     Group z[V], d[V];
     uint4 bits[V];
     float2 s = both(0.f);
@@ -73,6 +106,11 @@ __global__ void __launch_bounds__(P::threads, 65536 / (P::V > 1 ? 128 : 96) / P:
     for (int v = 0; v < V; ++v) {
       bits[v] = make_uint4(0, 0, 0, 0);
       if (a.drop == 1) bits[v] = gen.bits(a, (int)row, lane + v * TPR);
+      if constexpr (STAGES > 0) {
+        ring.get(stage, 3 * v, xs[v]);
+        ring.get(stage, 3 * v + 1, rs[v]);
+        ring.get(stage, 3 * v + 2, ds[v]);
+      }
       z[v] = xs[v].get();
       d[v] = ds[v].get();
       if (a.drop == 1) drop(a, bits[v], z[v]);
@@ -80,8 +118,8 @@ __global__ void __launch_bounds__(P::threads, 65536 / (P::V > 1 ? 128 : 96) / P:
 #pragma unroll
       for (int i = 0; i < 4; ++i) z[v].p[i] = fma2(z[v].p[i], both(a.scale), r.p[i]);
     }
-    px += step * a.sx, pr += step * a.sr, pd += step * a.so;
-    if (AHEAD) load(row + step);
+    if (STAGES > 0) load(row + STAGES * step);  // (into the stage that has just been read)
+    else if (AHEAD) load(row + step);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const Group m = spread<W>(-st.x, a.cols - 8 * (lane + v * TPR));
@@ -206,7 +244,7 @@ int backward_ctas(const Args &a) {
   with_plan<2>(a.groups, [&](auto plan) {
     using P = decltype(plan);
     const int64_t ctas = ((int64_t)a.rows + P::slots - 1) / P::slots;
-    const int64_t most = kSMs * (65536 / (P::V > 1 ? 128 : 96) / P::threads);  // (as the kernel's bounds say)
+    const int64_t most = kSMs * resident<P>;  // (as the kernel's bounds say)
     n = ctas < most ? ctas : most;
   });
   return (int)n;
@@ -256,17 +294,23 @@ extern "C" int blossom_add_norm_bwd(const blossom_rows_params *params, const voi
   al.rows_at(dresidual, a.sdr, esz);
   const int ctas = rows::backward_ctas(a);
   float *part = dweight || dbias ? static_cast<float *>(workspace) : nullptr;
+  bool ok = true;
   rows::with_plan<2>(a.groups, [&](auto plan) {
     using P = decltype(plan);
     rows::with_type(params->dtype, al.elements(a.cols, esz), [&](auto t, auto w) {
       using T = decltype(t);
+      const auto kern = rows::norm_bwd_kernel<T, decltype(w)::value, P>;
+      using S = rows::Shape<T, decltype(w)::value, P>;
+      ok = rows::allow_stages(kern, S::smem, S::fixed);
+      if (!ok) return;
       LaunchScope ls(K_NORM_BWD, st);
-      launch_chained(rows::norm_bwd_kernel<T, decltype(w)::value, P>, dim3((unsigned)ctas), dim3(P::threads), 0, st, a,
+      launch_chained(kern, dim3((unsigned)ctas), dim3(P::threads), S::smem, st, a,
                      static_cast<const T *>(x), static_cast<const T *>(residual), weight, rng,
                      reinterpret_cast<const float2 *>(stats), static_cast<const T *>(dout), static_cast<T *>(dx),
                      static_cast<T *>(dresidual), part);
     });
   });
+  if (!ok) return BLOSSOM_ERR_CUDA;
   if (part) {
     LaunchScope ls(K_NORM_WEIGHTS, st);
     launch_chained(rows::norm_weights_kernel, dim3((unsigned)((2 * a.cols + rows::kSumCols - 1) / rows::kSumCols)),

@@ -1,6 +1,6 @@
 // Layer norm of residual + dropout(x), forward: out = (z - mean) * rstd * weight + bias per row, z never stored.
 //
-// Bound: memory, x and residual once in and out once out.  32768 x 1024 bf16 with dropout: 201 MB in 39 us, 80 % of the rate
+// Bound: memory, x and residual once in and out once out.  32768 x 1024 bf16 with dropout: 201 MB in 36 us, 86 % of the rate
 // of a copy; 131072 x 64: 50 MB in 16 us (what is left are the generator's and the norm's instructions: without the next
 // rows under way 47 us with a CTA a row, 39 with a warp a row of 1024).  12800 x 64: 5.4 us, one launch.
 // A row stays in registers between the three steps (mean, then
@@ -18,14 +18,27 @@ struct InFlight {
   static constexpr int rows = P::V == 1 ? 2 : 1;
 };
 
+// What a CTA has of its SM.
 template <typename T, int W, typename P>
-__global__ void __launch_bounds__(P::threads, 65536 / (P::V > 2 ? 128 : 80) / P::threads)
+struct Shape {
+  static constexpr int regs = P::V > 2 ? 128 : 80, resident = 65536 / regs / P::threads;
+  static constexpr int weights = P::V > 1 ? P::TPR * P::V * 4 * (int)sizeof(float4) : 0;  // bytes
+  static constexpr int fixed = 64;
+  using Rows = Ring<2 * InFlight<P>::rows * P::V, P::threads>;
+  // (not for narrow rows: 131072 x 64 18 us against 16, 12800 x 64 7.3 against 5.6; 32768 x 1024 38.5 against 41)
+  static constexpr int stages = W == 8 && P::V > 1 ? Rows::stages(resident, weights + fixed) : 0;  // 0: rows in registers
+  static constexpr int smem = weights + stages * Rows::kStage;
+};
+
+template <typename T, int W, typename P>
+__global__ void __launch_bounds__(P::threads, Shape<T, W, P>::resident)
     norm_fwd_kernel(Args a, const T *__restrict__ x, const T *__restrict__ res, const void *__restrict__ weight,
                     const void *__restrict__ bias, const int64_t *__restrict__ rng, T *__restrict__ out,
                     float2 *__restrict__ stats) {
-  // In bf16 the next rows are under way while these are worked on; in fp32, twice the bytes a column, they would take
-  // registers that the work needs.
-  constexpr bool AHEAD = sizeof(T) == 2;
+  // In bf16 the next rows are under way while these are worked on, wide ones by asynchronous copies; in fp32, twice the bytes a
+  // column, they would take registers that the work needs.
+  constexpr int STAGES = Shape<T, W, P>::stages;
+  constexpr bool AHEAD = STAGES == 0 && sizeof(T) == 2;
   constexpr int TPR = P::TPR, V = P::V, U = InFlight<P>::rows, kGroups = TPR * V;
   __shared__ float buf[TPR > 32 ? TPR / 16 : 1];
   // weight and bias of wide rows: per group of columns two quarters of each, the groups side by side (so that a warp reads
@@ -56,35 +69,55 @@ __global__ void __launch_bounds__(P::threads, 65536 / (P::V > 2 ? 128 : 80) / P:
   const T *px = x + row0 * a.sx + 8 * lane, *pr = res + row0 * a.sr + 8 * lane;
   T *po = out + row0 * a.so + 8 * lane;
   Raw<T, W> xs[U][V], rs[U][V];
-  auto load = [&](uint32_t row, const T *px, const T *pr) {
+  const typename Shape<T, W, P>::Rows ring(wb + Shape<T, W, P>::weights / sizeof(float4));
+  int stage = 0;
+  auto load = [&](uint32_t row) {  // from px and pr, which go on to the next
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         const int valid = row + u * P::slots < rows ? a.cols - 8 * (lane + v * TPR) : 0;
-        xs[u][v].load(px + u * P::slots * a.sx + 8 * v * TPR, a.drop < 2 ? valid : 0);
-        rs[u][v].load(pr + u * P::slots * a.sr + 8 * v * TPR, res ? valid : 0);
+        const T *x1 = px + u * P::slots * a.sx + 8 * v * TPR, *r1 = pr + u * P::slots * a.sr + 8 * v * TPR;
+        if constexpr (STAGES > 0) {
+          ring.copy(stage, 2 * (u * V + v), x1, a.drop < 2 && valid > 0);
+          ring.copy(stage, 2 * (u * V + v) + 1, r1, res && valid > 0);
+        } else {
+          xs[u][v].load(x1, a.drop < 2 ? valid : 0);
+          rs[u][v].load(r1, res ? valid : 0);
+        }
       }
+    if constexpr (STAGES > 0) {
+      copies_end();
+      stage = stage + 1 == STAGES ? 0 : stage + 1;
+    }
+    px += step * a.sx, pr += step * a.sr;
   };
-  if (AHEAD) load(row0, px, pr);
+  if (AHEAD) load(row0);
+#pragma unroll 1
+  for (int i = 0; i < STAGES; ++i) load(row0 + i * step);
   // (`left`, the CTA's first row, is the same for all of its threads: they meet in row_sum)
   for (; left < rows; left += step, row0 += step, po += step * a.so) {
     Group z[U][V];
-    if (!AHEAD) load(row0, px, pr);
+    if constexpr (STAGES > 0) copies_wait<STAGES - 1>();
+    else if (!AHEAD) load(row0);
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         uint4 bits = make_uint4(0, 0, 0, 0);
         if (a.drop == 1) bits = gen.bits(a, (int)(row0 + u * P::slots), lane + v * TPR);
+        if constexpr (STAGES > 0) {
+          ring.get(stage, 2 * (u * V + v), xs[u][v]);
+          ring.get(stage, 2 * (u * V + v) + 1, rs[u][v]);
+        }
         z[u][v] = xs[u][v].get();
         if (a.drop == 1) drop(a, bits, z[u][v]);
         const Group r = rs[u][v].get();
 #pragma unroll
         for (int i = 0; i < 4; ++i) z[u][v].p[i] = fma2(z[u][v].p[i], both(a.scale), r.p[i]);
       }
-    px += step * a.sx, pr += step * a.sr;
-    if (AHEAD) load(row0 + step, px, pr);
+    if (STAGES > 0) load(row0 + STAGES * step);  // (into the stage that has just been read)
+    else if (AHEAD) load(row0 + step);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       float s = 0.f;
@@ -157,12 +190,12 @@ extern "C" int blossom_add_norm_fwd(const blossom_rows_params *params, const voi
       if constexpr (P::V <= (sizeof(T) == 2 ? 4 : 2)) {
         const auto kern = rows::norm_fwd_kernel<T, decltype(w)::value, P>;
         const int64_t per = P::slots * rows::InFlight<P>::rows, ctas = (a.rows + per - 1) / per;
-        const int64_t most = rows::kSMs * (65536 / (P::V > 2 ? 128 : 80) / P::threads);  // (as many as run at once)
-        const size_t smem = P::V > 1 ? (size_t)P::TPR * P::V * 4 * sizeof(float4) : 0;
-        ok = allow_smem(kern, smem);
+        using S = rows::Shape<T, decltype(w)::value, P>;
+        const int64_t most = rows::kSMs * S::resident;  // (as many as run at once)
+        ok = rows::allow_stages(kern, S::smem, S::fixed);
         if (!ok) return;
         LaunchScope ls(K_NORM_FWD, (cudaStream_t)stream);
-        launch_chained(kern, dim3((unsigned)(ctas < most ? ctas : most)), dim3(P::threads), smem, (cudaStream_t)stream, a,
+        launch_chained(kern, dim3((unsigned)(ctas < most ? ctas : most)), dim3(P::threads), S::smem, (cudaStream_t)stream, a,
                        static_cast<const T *>(x), static_cast<const T *>(residual), weight, bias, rng,
                        static_cast<T *>(out), reinterpret_cast<float2 *>(stats));
       }

@@ -82,6 +82,45 @@ struct Raw {
     return v;
   }
 };
+// ---- bf16 rows under way in shared memory ----------------------------------------------------------
+// Asynchronous copies bring the rows to come without a register for them.  A thread copies and reads its own groups of 8 columns
+// alone, 16 bytes each, so that nobody meets at a barrier; the threads' groups lie side by side.  G: groups a thread and stage.
+// (In fp32 the two halves of a group would come by two copies that take the same sectors from L2 twice: 32768 x 1024 forward
+// 106 us instead of 70, backward 174 instead of 121.)
+template <int G, int THREADS>
+struct Ring {
+  static constexpr int kStage = G * 16 * THREADS;
+  char *mine;
+  __device__ __forceinline__ explicit Ring(void *smem) : mine(static_cast<char *>(smem) + 16 * threadIdx.x) {}
+  // 8 elements from p into group g; zeros if they are not there, which are not read
+  __device__ __forceinline__ void copy(int stage, int g, const void *p, bool there) const {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
+                     (uint32_t)__cvta_generic_to_shared(mine) + stage * kStage + g * 16 * THREADS),
+                 "l"(p), "r"(there ? 16 : 0)
+                 : "memory");
+  }
+  template <typename T, int W>
+  __device__ __forceinline__ void get(int stage, int g, Raw<T, W> &r) const {
+    const uint4 q = *reinterpret_cast<const uint4 *>(mine + stage * kStage + g * 16 * THREADS);
+    r.w[0] = q.x, r.w[1] = q.y, r.w[2] = q.z, r.w[3] = q.w;
+  }
+  // Stages for `resident` CTAs an SM that take `other` bytes besides: up to four.
+  static constexpr int stages(int resident, int other) {
+    const int n = (227 * 1024 / resident - 1024 - other) / kStage;
+    return n < 0 ? 0 : n < 4 ? n : 4;
+  }
+};
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }  // of a stage
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }  // all but N stages
+
+// More than 48 KB, `fixed` of them the kernel's own arrays, have to be asked for.
+template <typename K>
+inline bool allow_stages(K kern, int dynamic, int fixed) {
+  return dynamic + fixed <= 48 * 1024 ||
+         cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, dynamic) == cudaSuccess;
+}
+
 template <typename T, int W>
 __device__ __forceinline__ void store_piece(T *p, int j, Group &v) {
   if constexpr (sizeof(T) == 4 && W == 4) {

@@ -86,6 +86,21 @@ def test_add_norm_over_the_sizes(rows, cols, dtype):
         compare(dict(zip(names, grads), out=out), want, tol, {"all": dtype == "bf16"}, (p, residual))
 
 
+# more rows than the GPU takes at once, several times over: a CTA's rows follow each other through its stages
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(285001, 8), (60003, 50), (30011, 136), (9001, 520), (6007, 1024), (2003, 2056), (1501, 4096), (901, 8192)])
+def test_add_norm_over_many_rows_a_cta(rows, cols, dtype):
+    import torch
+    from paper_2512_13368_b200.autograd import blossom_add_norm
+    x, r, w, b, dout = tensors(rows, cols, dtype, rows + cols)
+    want, tol = reference(x, r, w, b, dout, 0.3, 7, 8, 9, 1e-5)
+    leaves = [t.requires_grad_(True) for t in (x, r, w, b)]
+    out = blossom_add_norm(x, r, w, b, p=0.3, rng=torch.tensor([7, 8], device="cuda"), site=9)
+    grads = torch.autograd.grad(out, leaves, dout)
+    compare(dict(zip(["dx", "dresidual", "dweight", "dbias"], grads), out=out), want, tol, {"all": dtype == "bf16"}, "many rows")
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("weights,wide", [(True, True), (True, False), (False, False)])
