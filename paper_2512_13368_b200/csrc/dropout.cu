@@ -1,10 +1,10 @@
 // Dropout from a counter-based generator: out = kept ? x * scale : 0, the mask a function of (seed, step, site, row,
 // column) that nobody stores.  The backward is the same kernel on the upstream gradient.
 //
-// Bound: memory, each element once in and once out.  131072 x 64 bf16 is 33.6 MB a call, 5.2 us at the rate of a copy; a
-// launch takes about 12 us alone and less in a row of them, most of it the chain load, generator, store.  Through autograd a
-// forward and a backward take 49 us, whatever the size up to there: that is the host's part of it.  Two rows a thread are under
-// way at a time; the groups of threads are as narrow as the row, so that a row of 64 keeps 8 threads and none idles.
+// Bound: memory, each element once in and once out, and the generator's instructions.  131072 x 64 bf16 is 33.6 MB a call, 5.2 us at
+// the rate of a copy, and takes 12 us alone; 32768 x 1024 134 MB, 21 us, takes 27; in fp32 53 of 42.  Through autograd a forward
+// and a backward of the former take 49 us: that is the host's part of it.  The groups of threads are as narrow as the row, so
+// that a row of 64 keeps 8 threads and none idles.
 #include "rows.cuh"
 
 namespace blossom {
@@ -41,11 +41,14 @@ int check(const blossom_rows_params *p, int max_cols, const int64_t *rng, Args *
 
 namespace {
 
-constexpr int kRowsInFlight = 2;  // rows a thread loads before it works on the first
+// Rows a thread loads before it works on the first (131072 x 64, 524288 x 64 in bf16 one 11.8, 30.5 us, two 13.7, 32.5; 32768 x
+// 1024 28.7, 27.0; in fp32 18.1, 57.1 and 16.1, 52.7).
+template <typename T, typename P>
+constexpr int kRowsInFlight = sizeof(T) == 2 && P::V == 1 ? 1 : 2;
 
 template <typename T, int W, typename P>
 __global__ void __launch_bounds__(P::threads) dropout_kernel(Args a, const T *x, const int64_t *rng, T *out) {
-  constexpr int U = kRowsInFlight, V = P::V;
+  constexpr int U = kRowsInFlight<T, P>, V = P::V;
   grid_chain_enter();
   Generator gen;
   if (a.drop == 1) gen.read(rng);
@@ -100,7 +103,7 @@ extern "C" int blossom_dropout(const blossom_rows_params *params, const void *x,
     using P = decltype(plan);
     rows::with_type(params->dtype, al.elements(a.cols, esz), [&](auto t, auto w) {
       using T = decltype(t);
-      const int64_t per = P::slots * rows::kRowsInFlight, ctas = (a.rows + per - 1) / per;
+      const int64_t per = P::slots * rows::kRowsInFlight<T, P>, ctas = (a.rows + per - 1) / per;
       const int64_t most = rows::kSMs * (2048 / P::threads);
       LaunchScope ls(K_DROPOUT, (cudaStream_t)stream);
       launch_chained(rows::dropout_kernel<T, decltype(w)::value, P>, dim3((unsigned)(ctas < most ? ctas : most)),
