@@ -124,10 +124,13 @@ inline int lanes_of(int groups) { return groups <= 4 ? 4 : groups <= 8 ? 8 : gro
 
 // ---- bf16 rows of up to 64 NL columns on the matrix units ---------------------------------------------
 // A warp scores 16 rows against one vector.  Lane 8 r + s loads 16 bytes at column 8 s of the rows r, 4 + r, 8 + r and 12 + r,
-// so that every load takes whole 128-byte lines.  As the order in which a product's columns are added up is free, two rows'
-// registers are the first operand of two m16n8k16 products as they come, without a detour through shared memory: its
-// row g = 2 r + s / 4 is the half s / 4 of a row.  The vector, laid out alike, is the second operand: its first half
-// in the even columns, its second in the odd ones, of which a lane keeps the one that belongs to its half.
+// so that every load takes whole 128-byte lines.  As the order in which a product's columns are added up is free, a load's four
+// registers are the first operand of an m16n8k16 product as they come, without a detour through shared memory or other
+// registers: its rows 2 r + s / 4 and 8 + 2 r + s / 4 are the first and third and the second and fourth words of the half s / 4 of a
+// row.  The vector's words are the second operand, by columns modulo four: the first half's first and third, its second and
+// fourth, the other half's.  Of a lane's four sums two belong to its half and words in every other lane.
+// (With the registers of two loads in one operand, which the compiler had to move together, positions of 131072 x 128 x 64 took
+// 285 us instead of 271, of 32768 x 128 x 128 140 instead of 128.)
 template <int NL>
 struct Rows16 {
   uint4 w[4][NL];
@@ -157,14 +160,17 @@ struct Lanes16 {
 #pragma unroll
     for (int j = 0; j < 4; ++j) load(__shfl_sync(0xffffffffu, rows, from + 4 * j + r), w.w[j]);
   }
-  // the vector, zero where there are no columns
-  __device__ __forceinline__ void vector(uint32_t row, int cols, uint4 (&w)[NL]) const {
-    load(row, w);
-    if (!FULL) {
-      const int s = (int)threadIdx.x % 8;
+  // the second operand: the lane's words of the vector, zero where there are no columns
+  __device__ __forceinline__ void vector(uint32_t row, int cols, uint2 (&w)[NL]) const {
+    const int lane = (int)threadIdx.x % 32, s = lane / 8 % 2 * 4 + lane % 4, own = FULL ? lane % 8 : 0;
+    const char *p = base + (uint64_t)row * stride - 16 * own;
 #pragma unroll
-      for (int c = 0; c < NL; ++c)
-        if (64 * c + 8 * s >= cols) w[c] = make_uint4(0, 0, 0, 0);
+    for (int c = 0; c < NL; ++c) {
+      w[c] = make_uint2(0, 0);
+      if (FULL || 64 * c + 8 * s < cols) {
+        const uint4 q = *reinterpret_cast<const uint4 *>(p + 128 * c + 16 * s);
+        w[c] = lane & 4 ? make_uint2(q.y, q.w) : make_uint2(q.x, q.z);
+      }
     }
   }
 };
@@ -182,23 +188,20 @@ __device__ __forceinline__ void mma16816_first(float (&d)[4], uint32_t a0, uint3
 }
 // l[j] = <row 4 j + r, v>
 template <int NL>
-__device__ __forceinline__ void dots16(const Rows16<NL> &r, const uint4 (&v)[NL], float (&l)[4]) {
-  const bool odd = threadIdx.x & 4;
+__device__ __forceinline__ void dots16(const Rows16<NL> &r, const uint2 (&v)[NL], float (&l)[4]) {
+  const int from = (int)threadIdx.x & 24;
 #pragma unroll
-  for (int j = 0; j < 4; j += 2) {
+  for (int j = 0; j < 4; ++j) {
     float d[4];
 #pragma unroll
     for (int c = 0; c < NL; ++c) {
-      const uint4 x = r.w[j][c], y = r.w[j + 1][c];
-      if (c == 0) mma16816_first(d, x.x, y.x, x.y, y.y, v[c].x, v[c].y);
-      else mma16816(d, x.x, y.x, x.y, y.y, v[c].x, v[c].y);
-      mma16816(d, x.z, y.z, x.w, y.w, v[c].z, v[c].w);
+      const uint4 x = r.w[j][c];
+      if (c == 0) mma16816_first(d, x.x, x.y, x.z, x.w, v[c].x, v[c].y);
+      else mma16816(d, x.x, x.y, x.z, x.w, v[c].x, v[c].y);
     }
-    l[j] = odd ? d[1] : d[0];
-    l[j + 1] = odd ? d[3] : d[2];
+    const float half = d[0] + d[3];
+    l[j] = __shfl_sync(0xffffffffu, half, from) + __shfl_sync(0xffffffffu, half, from + 5);
   }
-#pragma unroll
-  for (int j = 0; j < 4; ++j) l[j] += __shfl_xor_sync(0xffffffffu, l[j], 4);
 }
 // acc += sum_j p[j] * row 4 j + r, in single precision (the weights keep their 24 bits)
 template <int NL>

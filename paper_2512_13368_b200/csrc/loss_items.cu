@@ -556,7 +556,7 @@ __global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 7 : 4)
     if (i + lane < e) x.key = keys[i + lane], x.val = vals[i + lane];
     return x;
   };
-  uint4 w[NL];
+  uint2 w[NL];
   float2 acc[NL][4];
   uint32_t cur = s < entries ? keys[s] : none, before = s > 0 ? keys[s - 1] : 0xffffffffu;
   const bool open = cur < none && before == cur;  // the first item's entries began in a chunk before

@@ -3,7 +3,7 @@
 //
 // A warp takes a position.  Groups of LPC lanes hold one candidate's row each; a group keeps a running maximum, sum and
 // weighted sum of rows, and the groups are joined at the end.  Every candidate's row is read once.
-// Bound: 131072 positions of 128 candidates of 64 bf16 columns take 2.1 GB from L2 and 0.17 GB from HBM (26 us) in 282 us, 7.6
+// Bound: 131072 positions of 128 candidates of 64 bf16 columns take 2.1 GB from L2 and 0.17 GB from HBM (26 us) in 270 us, 8.0
 // TB/s; L2 is at a third of its rate, the issue slots are 67 % busy: unpacking, weighing (two FMAs an instruction) and the
 // ids.  32768 x 128 x 128: 135 us, 8 TB/s.  fp32, 12795 x 100 x 50: 45 us.  64 x 101, no gradient: 4 us of a block's latency.
 #include <float.h>
@@ -233,7 +233,7 @@ __global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 8 : 5)
 #pragma unroll
     for (int c = 0; c < NL; ++c) grad[c] = make_float2(0.f, 0.f);
     if (target >= 0) {
-      uint4 h[NL];
+      uint2 h[NL];
       from_hidden.vector((uint32_t)row, a.cols, h);
       float2 acc[NL][4];
 #pragma unroll
