@@ -123,53 +123,56 @@ inline void with_plan(int groups, F &&f) {
 inline int lanes_of(int groups) { return groups <= 4 ? 4 : groups <= 8 ? 8 : groups <= 16 ? 16 : 32; }
 
 // ---- bf16 rows of up to 64 NL columns on the matrix units ---------------------------------------------
-// A warp scores 16 rows against one vector.  Lane 8 r + s loads 16 bytes at column 8 s of the rows r, 4 + r, 8 + r and 12 + r,
-// so that every load takes whole 128-byte lines.  As the order in which a product's columns are added up is free, a load's four
-// registers are the first operand of an m16n8k16 product as they come, without a detour through shared memory or other
-// registers: its rows 2 r + s / 4 and 8 + 2 r + s / 4 are the first and third and the second and fourth words of the half s / 4 of a
-// row.  The vector's words are the second operand, by columns modulo four: the first half's first and third, its second and
-// fourth, the other half's.  Of a lane's four sums two belong to its half and words in every other lane.
-// (With the registers of two loads in one operand, which the compiler had to move together, positions of 131072 x 128 x 64 took
-// 285 us instead of 271, of 32768 x 128 x 128 140 instead of 128.)
-template <int NL>
+// A warp scores 16 rows against one vector.  L lanes hold a row, kParts times 16 bytes each (side by side: a load takes 64 or 128
+// bytes of a row), and of every kStep-th row of the 16.  As the order in which a product's columns are added up is free, a load's
+// four registers are the first operand of an m16n8k16 product as they come, without a detour through shared memory or other
+// registers: the first and third word are the columns of the product's row lane / 4, the second and fourth those of the row
+// 8 behind it.  The vector's words are the second operand, the first and third in even columns, the others in odd ones, so
+// that the two sums a lane wants are its first and its last.  With 8 lanes a row its two quads have different columns; the
+// vector's then alternate by twos, and what counts is fetched from a lane of either quad.
+// (With words of two loads in one operand, which the compiler had to move together, positions of 131072 x 128 x 64 took 285 us
+// instead of 271, of 32768 x 128 x 128 140 instead of 128.)
+template <int NL, int L>
 struct Rows16 {
-  uint4 w[4][NL];
+  static constexpr int kLanes = L, kStep = 32 / L, kRows = L / 2, kParts = 8 * NL / L;  // kRows: of a lane
+  uint4 w[kRows][kParts];
 };
 // Where a lane finds its columns of a row.  Columns that are not there are read as the row's first ones and meet a zero of the
 // vector (a row that is no number somewhere is none in its product anyway).
-template <int NL, bool FULL>
+template <int NL, int L, bool FULL>
 struct Lanes16 {
+  using R = Rows16<NL, L>;
   const char *base;
   uint32_t stride;  // bytes
-  uint32_t off[NL];
+  uint32_t off[R::kParts];
   __device__ __forceinline__ Lanes16(const __nv_bfloat16 *p, int64_t elements, int cols)
       : base(reinterpret_cast<const char *>(p)), stride((uint32_t)(elements * 2)) {
-    const int s = (int)threadIdx.x % 8;
-    if (FULL) base += 16 * s;
+    const int t = (int)threadIdx.x % L;
+    if (FULL) base += 16 * t;
 #pragma unroll
-    for (int c = 0; c < NL; ++c) off[c] = FULL ? 128 * c : 64 * c + 8 * s < cols ? 128 * c + 16 * s : 0;
+    for (int e = 0; e < R::kParts; ++e) off[e] = FULL ? 16 * L * e : 8 * (L * e + t) < cols ? 16 * (L * e + t) : 0;
   }
-  __device__ __forceinline__ void load(uint32_t row, uint4 (&w)[NL]) const {
+  __device__ __forceinline__ void load(uint32_t row, uint4 (&w)[R::kParts]) const {
     const char *p = base + (uint64_t)row * stride;
 #pragma unroll
-    for (int c = 0; c < NL; ++c) w[c] = *reinterpret_cast<const uint4 *>(p + off[c]);
+    for (int e = 0; e < R::kParts; ++e) w[e] = *reinterpret_cast<const uint4 *>(p + off[e]);
   }
   // rows named by one lane each, `from` on
-  __device__ __forceinline__ void load16(uint32_t rows, int from, Rows16<NL> &w) const {
-    const int r = ((int)threadIdx.x % 32) / 8;
+  __device__ __forceinline__ void load16(uint32_t rows, int from, R &w) const {
+    const int q = ((int)threadIdx.x % 32) / L;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) load(__shfl_sync(0xffffffffu, rows, from + 4 * j + r), w.w[j]);
+    for (int j = 0; j < R::kRows; ++j) load(__shfl_sync(0xffffffffu, rows, from + R::kStep * j + q), w.w[j]);
   }
   // the second operand: the lane's words of the vector, zero where there are no columns
-  __device__ __forceinline__ void vector(uint32_t row, int cols, uint2 (&w)[NL]) const {
-    const int lane = (int)threadIdx.x % 32, s = lane / 8 % 2 * 4 + lane % 4, own = FULL ? lane % 8 : 0;
+  __device__ __forceinline__ void vector(uint32_t row, int cols, uint2 (&w)[R::kParts]) const {
+    const int lane = (int)threadIdx.x % 32, t = L == 4 ? lane % 4 : lane / 8 % 2 * 4 + lane % 4, own = FULL ? lane % L : 0;
     const char *p = base + (uint64_t)row * stride - 16 * own;
 #pragma unroll
-    for (int c = 0; c < NL; ++c) {
-      w[c] = make_uint2(0, 0);
-      if (FULL || 64 * c + 8 * s < cols) {
-        const uint4 q = *reinterpret_cast<const uint4 *>(p + 128 * c + 16 * s);
-        w[c] = lane & 4 ? make_uint2(q.y, q.w) : make_uint2(q.x, q.z);
+    for (int e = 0; e < R::kParts; ++e) {
+      w[e] = make_uint2(0, 0);
+      if (FULL || 8 * (L * e + t) < cols) {
+        const uint4 q = *reinterpret_cast<const uint4 *>(p + 16 * (L * e + t));
+        w[e] = lane & 4 ? make_uint2(q.y, q.w) : make_uint2(q.x, q.z);
       }
     }
   }
@@ -186,57 +189,67 @@ __device__ __forceinline__ void mma16816_first(float (&d)[4], uint32_t a0, uint3
       : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
-// l[j] = <row 4 j + r, v>
-template <int NL>
-__device__ __forceinline__ void dots16(const Rows16<NL> &r, const uint2 (&v)[NL], float (&l)[4]) {
+// l[j] = <the lane's row j, v>
+template <int NL, int L>
+__device__ __forceinline__ void dots16(const Rows16<NL, L> &r, const uint2 (&v)[8 * NL / L], float (&l)[L / 2]) {
   const int from = (int)threadIdx.x & 24;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
+  for (int j = 0; j < r.kRows; ++j) {
     float d[4];
 #pragma unroll
-    for (int c = 0; c < NL; ++c) {
-      const uint4 x = r.w[j][c];
-      if (c == 0) mma16816_first(d, x.x, x.y, x.z, x.w, v[c].x, v[c].y);
-      else mma16816(d, x.x, x.y, x.z, x.w, v[c].x, v[c].y);
+    for (int e = 0; e < r.kParts; ++e) {
+      const uint4 x = r.w[j][e];
+      if (e == 0) mma16816_first(d, x.x, x.y, x.z, x.w, v[e].x, v[e].y);
+      else mma16816(d, x.x, x.y, x.z, x.w, v[e].x, v[e].y);
     }
-    const float half = d[0] + d[3];
-    l[j] = __shfl_sync(0xffffffffu, half, from) + __shfl_sync(0xffffffffu, half, from + 5);
+    l[j] = d[0] + d[3];
+    if (L == 8) l[j] = __shfl_sync(0xffffffffu, l[j], from) + __shfl_sync(0xffffffffu, l[j], from + 5);
   }
 }
-// acc += sum_j p[j] * row 4 j + r, in single precision (the weights keep their 24 bits)
-template <int NL>
-__device__ __forceinline__ void weigh16(const Rows16<NL> &r, const float (&p)[4], float2 (&acc)[NL][4]) {
+// acc += sum_j p[j] * the lane's row j, in single precision (the weights keep their 24 bits)
+template <int NL, int L>
+__device__ __forceinline__ void weigh16(const Rows16<NL, L> &r, const float (&p)[L / 2], float2 (&acc)[8 * NL / L][4]) {
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
+  for (int j = 0; j < r.kRows; ++j) {
     const float2 pp = make_float2(p[j], p[j]);
 #pragma unroll
-    for (int c = 0; c < NL; ++c) {
-      const uint32_t x[4] = {r.w[j][c].x, r.w[j][c].y, r.w[j][c].z, r.w[j][c].w};
+    for (int e = 0; e < r.kParts; ++e) {
+      const uint32_t x[4] = {r.w[j][e].x, r.w[j][e].y, r.w[j][e].z, r.w[j][e].w};
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        acc[c][i] = fma2(pp, make_float2(__uint_as_float(x[i] << 16), __uint_as_float(x[i] & 0xffff0000u)), acc[c][i]);
+        acc[e][i] = fma2(pp, make_float2(__uint_as_float(x[i] << 16), __uint_as_float(x[i] & 0xffff0000u)), acc[e][i]);
     }
   }
 }
-// The sum over the four groups of 8 lanes, scattered: lane 8 r + s is left with the columns 64 c + 8 s + 2 r and the next.
-template <int NL>
-__device__ __forceinline__ void scatter16(const float2 (&acc)[NL][4], float2 (&out)[NL]) {
-  const bool hi = threadIdx.x & 16, mid = threadIdx.x & 8;
-  auto exchange = [](float2 keep, float2 give, int o) {
+// The sum over the groups of lanes, scattered: two columns a lane and line are left (scattered_column).
+template <int NL, int L>
+__device__ __forceinline__ void scatter16(const float2 (&acc)[8 * NL / L][4], float2 (&out)[NL]) {
+  const bool b4 = threadIdx.x & 16, b3 = threadIdx.x & 8, b2 = threadIdx.x & 4;
+  auto exchange = [](bool second, float2 a, float2 b, int o) {  // of two sums one is kept
+    const float2 keep = second ? b : a, give = second ? a : b;
     return make_float2(keep.x + __shfl_xor_sync(0xffffffffu, give.x, o), keep.y + __shfl_xor_sync(0xffffffffu, give.y, o));
   };
+  if constexpr (L == 4) {
+    static_assert(NL == 1, "4 lanes hold a line");
+    float2 s[4];
 #pragma unroll
-  for (int c = 0; c < NL; ++c) {
-    const float2 a = exchange(hi ? acc[c][2] : acc[c][0], hi ? acc[c][0] : acc[c][2], 16);
-    const float2 b = exchange(hi ? acc[c][3] : acc[c][1], hi ? acc[c][1] : acc[c][3], 16);
-    out[c] = exchange(mid ? b : a, mid ? a : b, 8);
+    for (int i = 0; i < 4; ++i) s[i] = exchange(b4, acc[0][i], acc[1][i], 16);
+    out[0] = exchange(b2, exchange(b3, s[0], s[2], 8), exchange(b3, s[1], s[3], 8), 4);
+  } else {
+#pragma unroll
+    for (int c = 0; c < NL; ++c)
+      out[c] = exchange(b3, exchange(b4, acc[c][0], acc[c][2], 16), exchange(b4, acc[c][1], acc[c][3], 16), 8);
   }
 }
 // the first of the two columns
-__device__ __forceinline__ int scattered_column(int c) { return 64 * c + 8 * ((int)threadIdx.x % 8) + 2 * (((int)threadIdx.x % 32) / 8); }
+template <int L>
+__device__ __forceinline__ int scattered_column(int c) {
+  const int lane = (int)threadIdx.x % 32;
+  return L == 4 ? 32 * (lane / 16) + 8 * (lane % 4) + 2 * (lane / 4 % 4) : 64 * c + 8 * (lane % 8) + 2 * (lane / 8);
+}
 // Lines of 64 columns where the matrix units take the rows (bf16, 16-byte aligned rows of up to 128 columns less than 4 GiB
-// apart), else 0.  Against groups of lanes, 131072 x 128 x 64: positions 286 us to 419, items 293 to 589; 32768 x 128 x 128:
-// 139 to 204, 220 to 283.
+// apart), else 0.  Against groups of lanes, 131072 x 128 x 64: positions 252 us to 419, items 293 to 589; 32768 x 128 x 128:
+// 117 to 204, 211 to 283.
 inline int mma_lines(const Args &a, int dtype, int width) {
   if (dtype != BLOSSOM_DTYPE_BF16 || width != 8 || a.cols > 128 || a.sh > 0x7fffffffLL || a.st > 0x7fffffffLL) return 0;
   return a.cols <= 64 ? 1 : 2;

@@ -348,7 +348,7 @@ constexpr size_t move_smem(int bits) {
 
 // ---- sums over an item's entries ---------------------------------------------------------------
 // Bound: the hidden rows come from L2, one an entry.  131072 x 128 entries x 64 bf16: 2.1 GB in 290 us, 7.4 TB/s, with 70 % of the
-// issue slots busy; 32768 x 128 x 128 with 25 entries an item: 220 us; fp32, 12795 x 100 x 50: 68 us.
+// issue slots busy; 32768 x 128 x 128 with 25 entries an item: 211 us; fp32, 12795 x 100 x 50: 68 us.
 // A block's groups of lanes (or warps) walk consecutive chunks, together a span of the list.  An item whose entries lie in one
 // chunk is written there and then.  The others' sums meet in shared memory: a group leaves that of its first item there if
 // the item began before its chunk, and the group in whose chunk an item began adds up those of the groups behind it.
@@ -534,15 +534,17 @@ __global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 7 : 4)
                           const float *__restrict__ lse, const float *__restrict__ grad_loss, const uint32_t *__restrict__ keys,
                           const uint32_t *__restrict__ vals, uint32_t entries, int chunk, __nv_bfloat16 *__restrict__ dtable,
                           float *__restrict__ part, uint32_t *__restrict__ range) {
+  constexpr int L = 8;  // lanes a row (4 of 64 columns in 80 registers: 295 us as well)
+  using R = Rows16<NL, L>;
   constexpr int NG = kMmaThreads / 32;
   __shared__ float2 shared_sums[NG][NL][32];
   __shared__ Ends<NG> ends;
   grid_chain_enter();
-  const int lane = (int)threadIdx.x % 32, group = lane / 8, warp = (int)threadIdx.x / 32;
+  const int lane = (int)threadIdx.x % 32, group = lane / R::kLanes, warp = (int)threadIdx.x / 32;
   const uint32_t none = (uint32_t)a.items;
   const uint64_t start = ((uint64_t)blockIdx.x * NG + warp) * (uint32_t)chunk;
   const uint32_t s = start < entries ? (uint32_t)start : entries, e = entries - s < (uint32_t)chunk ? entries : s + (uint32_t)chunk;
-  const Lanes16<NL, FULL> from_hidden(hidden, a.sh, a.cols), from_table(table, a.st, a.cols);
+  const Lanes16<NL, L, FULL> from_hidden(hidden, a.sh, a.cols), from_table(table, a.st, a.cols);
   const float scale = grad_scale(a, lse, grad_loss);
   // 32 entries, one a lane; what lies behind the chunk is no candidate of the first position.  The positions' log-sum-exps are
   // asked for 32 entries after the positions (whoever asks at once waits for the positions to come).
@@ -556,8 +558,8 @@ __global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 7 : 4)
     if (i + lane < e) x.key = keys[i + lane], x.val = vals[i + lane];
     return x;
   };
-  uint2 w[NL];
-  float2 acc[NL][4];
+  uint2 w[R::kParts];
+  float2 acc[R::kParts][4];
   uint32_t cur = s < entries ? keys[s] : none, before = s > 0 ? keys[s - 1] : 0xffffffffu;
   const bool open = cur < none && before == cur;  // the first item's entries began in a chunk before
   bool first = true;
@@ -565,14 +567,14 @@ __global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 7 : 4)
     cur = item;
     from_table.vector(item, a.cols, w);
 #pragma unroll
-    for (int c = 0; c < NL; ++c)
+    for (int e = 0; e < R::kParts; ++e)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) acc[c][i] = make_float2(0.f, 0.f);
+      for (int i = 0; i < 4; ++i) acc[e][i] = make_float2(0.f, 0.f);
   };
   auto write = [&](const float2 (&sum)[NL]) {
 #pragma unroll
     for (int c = 0; c < NL; ++c) {
-      const int col = scattered_column(c);
+      const int col = scattered_column<L>(c);
       if (FULL || col < a.cols)
         *reinterpret_cast<uint32_t *>(dtable + cur * a.sdt + col) = rows::pack2(sum[c].x * scale, sum[c].y * scale);
     }
@@ -580,7 +582,7 @@ __global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 7 : 4)
   auto leave = [&](const float2 (&sum)[NL], int slot) {
 #pragma unroll
     for (int c = 0; c < NL; ++c) {
-      const int col = scattered_column(c);
+      const int col = scattered_column<L>(c);
       if (FULL || col < a.cols) *reinterpret_cast<float2 *>(part + ((int64_t)blockIdx.x * 2 + slot) * a.cols + col) = sum[c];
     }
   };
@@ -590,7 +592,7 @@ __global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 7 : 4)
   };
   auto finish = [&]() {
     float2 sum[NL];
-    scatter16<NL>(acc, sum);
+    scatter16<NL, L>(acc, sum);
     if (first && open) share(sum);
     else write(sum);
     first = false;
@@ -608,37 +610,37 @@ __global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 7 : 4)
     }
     before = __shfl_sync(0xffffffffu, x.key, 31);
   };
-  auto walk = [&](const Rows16<NL> &h, const Entries &x, int half) {
+  auto walk = [&](const R &h, const Entries &x, int half) {
     const float minus = -x.top * kLog2e;
-    float shift[4];
+    float shift[R::kRows];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) shift[j] = __shfl_sync(0xffffffffu, minus, half + 4 * j + group);
+    for (int j = 0; j < R::kRows; ++j) shift[j] = __shfl_sync(0xffffffffu, minus, half + R::kStep * j + group);
     const uint32_t targets = __ballot_sync(0xffffffffu, x.val >> 31) >> half & 0xffffu;
     for (;;) {
-      float p[4];
-      dots16<NL>(h, w, p);
+      float p[R::kRows];
+      dots16<NL, L>(h, w, p);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) p[j] = exp2f(fmaf(p[j], kLog2e, shift[j]));
+      for (int j = 0; j < R::kRows; ++j) p[j] = exp2f(fmaf(p[j], kLog2e, shift[j]));
       if (targets) {  // (the same for the warp)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) p[j] -= targets >> (4 * j + group) & 1 ? 1.f : 0.f;
+        for (int j = 0; j < R::kRows; ++j) p[j] -= targets >> (R::kStep * j + group) & 1 ? 1.f : 0.f;
       }
       uint32_t others = __ballot_sync(0xffffffffu, x.key != cur) >> half & 0xffffu;
       if (!others) {
-        weigh16<NL>(h, p, acc);
+        weigh16<NL, L>(h, p, acc);
         return;
       }
       // (a weight of zero would not do: another item's row may hold what is no number)
       others >>= group;
-      Rows16<NL> own = h;
+      R own = h;
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (others >> (4 * j) & 1) {
+      for (int j = 0; j < R::kRows; ++j)
+        if (others >> (R::kStep * j) & 1) {
           p[j] = 0.f;
 #pragma unroll
-          for (int c = 0; c < NL; ++c) own.w[j][c] = make_uint4(0, 0, 0, 0);
+          for (int e = 0; e < R::kParts; ++e) own.w[j][e] = make_uint4(0, 0, 0, 0);
         }
-      weigh16<NL>(own, p, acc);
+      weigh16<NL, L>(own, p, acc);
       // the next item among the 16, if there is one (they are sorted)
       const uint32_t later = __ballot_sync(0xffffffffu, (lane & 16) == half && x.key > cur && x.key < none);
       if (!later) return;
@@ -655,7 +657,7 @@ __global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 7 : 4)
   bool goes_on = false;
   if (some) {
     begin(cur);
-    Rows16<NL> h;
+    R h;
     for (uint32_t i = s; i < e; i += 32) {
       from_hidden.load16(x.val & 0x7fffffffu, 0, h);
       next.ask(lse);
@@ -670,7 +672,7 @@ __global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 7 : 4)
       next = after;
     }
     goes_on = e < entries && keys[e] == cur;
-    scatter16<NL>(acc, sum);
+    scatter16<NL, L>(acc, sum);
     if (first && open) share(sum);
     else if (!goes_on) write(sum);
   }

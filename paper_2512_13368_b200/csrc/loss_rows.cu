@@ -3,9 +3,9 @@
 //
 // A warp takes a position.  Groups of LPC lanes hold one candidate's row each; a group keeps a running maximum, sum and
 // weighted sum of rows, and the groups are joined at the end.  Every candidate's row is read once.
-// Bound: 131072 positions of 128 candidates of 64 bf16 columns take 2.1 GB from L2 and 0.17 GB from HBM (26 us) in 270 us, 8.0
+// Bound: 131072 positions of 128 candidates of 64 bf16 columns take 2.1 GB from L2 and 0.17 GB from HBM (26 us) in 250 us, 8.6
 // TB/s; L2 is at a third of its rate, the issue slots are 67 % busy: unpacking, weighing (two FMAs an instruction) and the
-// ids.  32768 x 128 x 128: 135 us, 8 TB/s.  fp32, 12795 x 100 x 50: 45 us.  64 x 101, no gradient: 4 us of a block's latency.
+// ids.  32768 x 128 x 128: 117 us, 9.2 TB/s.  fp32, 12795 x 100 x 50: 45 us.  64 x 101, no gradient: 4 us of a block's latency.
 #include <float.h>
 
 #include "loss.cuh"
@@ -206,21 +206,25 @@ __global__ void __launch_bounds__(kThreads, P::V == 1 ? 4 : P::V == 2 ? 2 : 1)
 }
 
 // The same on the matrix units: a warp scores 16 candidates at a time.  What is no candidate is read as the target's row and
-// weighs nothing.  Other warps work while a warp's 16 rows are under way: with 64 registers an SM holds 32 of them, and two
-// buffers of rows a warp in 80 registers were slower (324 us against 305, 131072 x 128 candidates x 64), and so are 28 warps
-// (305 against 281).  With 128 columns 20 warps in 96 registers: 134 us against 141 with 16 (32768 x 128 candidates).
+// weighs nothing.  Other warps work while a warp's 16 rows are under way: two buffers of rows a warp in 80 registers were slower
+// (324 us against 305, 131072 x 128 candidates x 64).  4 lanes a row of 64 columns need neither shuffles nor each exponential
+// eight times (252 us against 270 with 8; 51200 x 32 candidates 41 against 39); for 128 columns they take too many registers.
 // The weighted sum stays on the CUDA cores: as a second product, its operand transposed in registers, it took 377 us.
+// Blocks an SM: 8 and 5 (7 259 us, 9 283; with 128 columns 4 127 us, 6 125, 5 117); the grid is two rounds of them.
+constexpr int row_blocks(int lines) { return lines == 1 ? 8 : 5; }  // an SM
 template <int NL, bool FULL, bool GRAD>
-__global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 8 : 5)
+__global__ void __launch_bounds__(kMmaThreads, row_blocks(NL))
     loss_rows_mma_kernel(Args a, int split, const __nv_bfloat16 *__restrict__ hidden, const __nv_bfloat16 *__restrict__ table,
                          float *__restrict__ lse, float *__restrict__ dh, double2 *__restrict__ sums,
                          float *__restrict__ loss) {
+  constexpr int L = 4 * NL;  // lanes a row
+  using R = Rows16<NL, L>;
   constexpr int NW = kMmaThreads / 32;
   __shared__ Shares<NW> shares;
   __shared__ float2 shared_sums[NW][NL][32];
   grid_chain_enter();
-  const int lane = (int)threadIdx.x % 32, warp = (int)threadIdx.x / 32, group = lane / 8;
-  const Lanes16<NL, FULL> from_hidden(hidden, a.sh, a.cols), from_table(table, a.st, a.cols);
+  const int lane = (int)threadIdx.x % 32, warp = (int)threadIdx.x / 32, group = lane / R::kLanes;
+  const Lanes16<NL, L, FULL> from_hidden(hidden, a.sh, a.cols), from_table(table, a.st, a.cols);
   double2 mine = make_double2(0.0, 0.0);
   const int64_t step = split ? gridDim.x : (int64_t)gridDim.x * NW;
   const int c_first = split ? 32 * warp : 0, c_step = split ? 32 * NW : 32;
@@ -233,52 +237,55 @@ __global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 8 : 5)
 #pragma unroll
     for (int c = 0; c < NL; ++c) grad[c] = make_float2(0.f, 0.f);
     if (target >= 0) {
-      uint2 h[NL];
+      uint2 h[R::kParts];
       from_hidden.vector((uint32_t)row, a.cols, h);
-      float2 acc[NL][4];
+      float2 acc[R::kParts][4];
 #pragma unroll
-      for (int c = 0; c < NL; ++c)
+      for (int e = 0; e < R::kParts; ++e)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[c][i] = make_float2(0.f, 0.f);
+        for (int i = 0; i < 4; ++i) acc[e][i] = make_float2(0.f, 0.f);
       auto rows_of = [&](int id, uint32_t &there) {  // there: a bit for each candidate
         there = __ballot_sync(0xffffffffu, id >= 0);
         return (uint32_t)(id >= 0 ? id : target);
       };
-      // of a group of lanes: its four rows of every 16; logits as they come (top: half the lowest number, so that log2(e) times
+      // of a group of lanes: its rows of every 16; logits as they come (top: half the lowest number, so that log2(e) times
       // it is one)
       float top = -0.5f * FLT_MAX, total = 0.f, own = 0.f;
-      auto score = [&](const Rows16<NL> &w, uint32_t there) {
-        float l[4];
-        dots16<NL>(w, h, l);
+      auto score = [&](const R &w, uint32_t there) {
+        float l[R::kRows];
+        dots16<NL, L>(w, h, l);
         const float first = l[0];
         if (~there & 0xffffu) {  // (the same for the warp)
           there >>= group;
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (!(there >> (4 * j) & 1)) l[j] = -INFINITY;
+          for (int j = 0; j < R::kRows; ++j)
+            if (!(there >> (R::kStep * j) & 1)) l[j] = -INFINITY;
         }
         // The reference point only moves if it has to, by more than 2^10 in the exponentials: the sums stay far from the type's
         // limits, and their relative rounding does not depend on it.
-        const float high = fmaxf(fmaxf(l[0], l[1]), fmaxf(l[2], l[3]));
+        float high = l[0];
+#pragma unroll
+        for (int j = 1; j < R::kRows; ++j) high = fmaxf(high, l[j]);
         if (high > top + 7.f) {
           const float shrink = exp2f((top - high) * kLog2e);
           total *= shrink;
           if (GRAD) {
 #pragma unroll
-            for (int c = 0; c < NL; ++c)
+            for (int e = 0; e < R::kParts; ++e)
 #pragma unroll
-              for (int i = 0; i < 4; ++i) acc[c][i].x *= shrink, acc[c][i].y *= shrink;
+              for (int i = 0; i < 4; ++i) acc[e][i].x *= shrink, acc[e][i].y *= shrink;
           }
           top = high;
         }
         const float shift = -top * kLog2e;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) l[j] = exp2f(fmaf(l[j], kLog2e, shift));
-        total += (l[0] + l[1]) + (l[2] + l[3]);
-        if (GRAD) weigh16<NL>(w, l, acc);
+        for (int j = 0; j < R::kRows; ++j) l[j] = exp2f(fmaf(l[j], kLog2e, shift));
+#pragma unroll
+        for (int j = 0; j < R::kRows; ++j) total += l[j];
+        if (GRAD) weigh16<NL, L>(w, l, acc);
         return first;
       };
-      Rows16<NL> w;
+      R w;
       for (int c0 = c_first; c0 <= a.n; c0 += c_step) {
         uint32_t there;
         const uint32_t ids = rows_of(id, there);
@@ -296,17 +303,17 @@ __global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 8 : 5)
       top *= kLog2e;  // in units of log 2 from here on
       float high = top;
 #pragma unroll
-      for (int o = 8; o < 32; o <<= 1) high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, o));
+      for (int o = R::kLanes; o < 32; o <<= 1) high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, o));
       const float weight = exp2f(top - high);  // (0 for a group that met no candidate)
       total *= weight;
 #pragma unroll
-      for (int o = 8; o < 32; o <<= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+      for (int o = R::kLanes; o < 32; o <<= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
       if (GRAD) {
 #pragma unroll
-        for (int c = 0; c < NL; ++c)
+        for (int e = 0; e < R::kParts; ++e)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) acc[c][i] = mul2(acc[c][i], both(weight));
-        scatter16<NL>(acc, grad);
+          for (int i = 0; i < 4; ++i) acc[e][i] = mul2(acc[e][i], both(weight));
+        scatter16<NL, L>(acc, grad);
       }
       if (split) {
         if (lane == 0) shares.high[warp] = high, shares.total[warp] = total;
@@ -338,7 +345,7 @@ __global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 8 : 5)
         const float inv = 1.f / total;
 #pragma unroll
         for (int c = 0; c < NL; ++c) {
-          const int col = scattered_column(c);
+          const int col = scattered_column<L>(c);
           if (FULL || col < a.cols) {
             const float2 w = rows::halves(*reinterpret_cast<const uint32_t *>(table + target * a.st + col));
             grad[c] = fma2(grad[c], both(inv), make_float2(-w.x, -w.y));
@@ -351,7 +358,7 @@ __global__ void __launch_bounds__(kMmaThreads, NL == 1 ? 8 : 5)
     if (GRAD) {
 #pragma unroll
       for (int c = 0; c < NL; ++c) {
-        const int col = scattered_column(c);
+        const int col = scattered_column<L>(c);
         if (FULL || col < a.cols) *reinterpret_cast<float2 *>(dh + (int64_t)row * a.cols + col) = grad[c];
       }
     }
@@ -443,7 +450,7 @@ extern "C" int blossom_sampled_loss_fwd(const blossom_loss_params *params, const
   al.rows_at(table, a.st, esz);
   const int width = al.elements(a.cols, esz), lines = loss::mma_lines(a, params->dtype, width);
   const int warps = (lines ? loss::kMmaThreads : loss::kThreads) / 32;  // a row each
-  const int64_t want = ((int64_t)a.rows + warps - 1) / warps, most = loss::kSMs * 64 / warps;
+  const int64_t want = ((int64_t)a.rows + warps - 1) / warps, most = loss::kSMs * (lines ? 2 * loss::row_blocks(lines) : 64 / warps);
   // (a block a row while the rows alone do not give an SM 8 warps; measured at Shares)
   const int split = a.n >= 32 && a.rows <= loss::kSMs * 8;
   const int ctas = split ? a.rows : (int)(want < most ? want : most);
