@@ -294,7 +294,7 @@ extern "C" int blossom_add_norm_bwd(const blossom_rows_params *params, const voi
   al.rows_at(dresidual, a.sdr, esz);
   const int ctas = rows::backward_ctas(a);
   float *part = dweight || dbias ? static_cast<float *>(workspace) : nullptr;
-  bool ok = true;
+  bool ok = true, wide = false;
   rows::with_plan<2>(a.groups, [&](auto plan) {
     using P = decltype(plan);
     rows::with_type(params->dtype, al.elements(a.cols, esz), [&](auto t, auto w) {
@@ -302,6 +302,8 @@ extern "C" int blossom_add_norm_bwd(const blossom_rows_params *params, const voi
       const auto kern = rows::norm_bwd_kernel<T, decltype(w)::value, P>;
       using S = rows::Shape<T, decltype(w)::value, P>;
       ok = rows::allow_stages(kern, S::smem, S::fixed);
+      wide = S::stages > 0 && P::V > 1;
+      if (wide) rows::prefer_shared(kern);
       if (!ok) return;
       LaunchScope ls(K_NORM_BWD, st);
       launch_chained(kern, dim3((unsigned)ctas), dim3(P::threads), S::smem, st, a,
@@ -312,6 +314,7 @@ extern "C" int blossom_add_norm_bwd(const blossom_rows_params *params, const voi
   });
   if (!ok) return BLOSSOM_ERR_CUDA;
   if (part) {
+    if (wide) rows::prefer_shared(rows::norm_weights_kernel);
     LaunchScope ls(K_NORM_WEIGHTS, st);
     launch_chained(rows::norm_weights_kernel, dim3((unsigned)((2 * a.cols + rows::kSumCols - 1) / rows::kSumCols)),
                    dim3(rows::kSumCols * rows::kSumSlices), 0, st, a.cols, ctas,

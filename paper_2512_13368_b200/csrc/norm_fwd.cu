@@ -193,6 +193,7 @@ extern "C" int blossom_add_norm_fwd(const blossom_rows_params *params, const voi
         using S = rows::Shape<T, decltype(w)::value, P>;
         const int64_t most = rows::kSMs * S::resident;  // (as many as run at once)
         ok = rows::allow_stages(kern, S::smem, S::fixed);
+        if (S::stages) rows::prefer_shared(kern);
         if (!ok) return;
         LaunchScope ls(K_NORM_FWD, (cudaStream_t)stream);
         launch_chained(kern, dim3((unsigned)(ctas < most ? ctas : most)), dim3(P::threads), S::smem, (cudaStream_t)stream, a,

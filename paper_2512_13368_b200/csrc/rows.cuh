@@ -121,6 +121,14 @@ inline bool allow_stages(K kern, int dynamic, int fixed) {
          cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, dynamic) == cudaSuccess;
 }
 
+// All of an SM's shared memory for the kernels of wide rows: a CTA that starts before the kernel ahead of it has ended finds the
+// split between L1 and shared memory as that one left it, and while one runs it stays so, too small for the others (32768 x
+// 1024, forward and backward in turn: 141 us without, 110 with it; narrow rows, 131072 x 256: 106 without, 112 with).
+template <typename K>
+inline void prefer_shared(K kern) {
+  (void)cudaFuncSetAttribute(kern, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+}
+
 template <typename T, int W>
 __device__ __forceinline__ void store_piece(T *p, int j, Group &v) {
   if constexpr (sizeof(T) == 4 && W == 4) {
