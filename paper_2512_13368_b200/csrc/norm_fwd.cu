@@ -1,8 +1,8 @@
 // Layer norm of residual + dropout(x), forward: out = (z - mean) * rstd * weight + bias per row, z never stored.
 //
-// Bound: memory, x and residual once in and out once out.  32768 x 1024 bf16 with dropout: 201 MB in 36 us, 86 % of the rate
-// of a copy; 131072 x 64: 50 MB in 16 us (what is left are the generator's and the norm's instructions: without the next
-// rows under way 47 us with a CTA a row, 39 with a warp a row of 1024).  12800 x 64: 5.4 us, one launch.
+// Bound: memory, x and residual once in and out once out, and the generator's and the norm's instructions.  32768 x 1024 bf16 with
+// dropout: 201 MB in 36 us, 86 % of the rate of a copy, with a warp a row (with a CTA a row 46); 131072 x 64: 50 MB in 16 us.
+// 12800 x 64: 5.4 us, one launch.
 // A row stays in registers between the three steps (mean, then
 // the sum of squared distances from it, then the output), so its variance is that of the definition without a
 // second read and without the cancellation of E[z^2] - mean^2.
