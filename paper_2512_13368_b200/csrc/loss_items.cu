@@ -347,7 +347,7 @@ constexpr size_t move_smem(int bits) {
 }
 
 // ---- sums over an item's entries ---------------------------------------------------------------
-// Bound: the hidden rows come from L2, one an entry.  131072 x 128 entries x 64 bf16: 2.1 GB in 290 us, 7.4 TB/s, with 70 % of the
+// Bound: the hidden rows come from L2, one an entry.  131072 x 128 entries x 64 bf16: 2.1 GB in 290 us, 7.4 TB/s, with 65 % of the
 // issue slots busy; 32768 x 128 x 128 with 25 entries an item: 211 us; fp32, 12795 x 100 x 50: 68 us.
 // A block's groups of lanes (or warps) walk consecutive chunks, together a span of the list.  An item whose entries lie in one
 // chunk is written there and then.  The others' sums meet in shared memory: a group leaves that of its first item there if

@@ -4,7 +4,7 @@
 // A warp takes a position.  Groups of LPC lanes hold one candidate's row each; a group keeps a running maximum, sum and
 // weighted sum of rows, and the groups are joined at the end.  Every candidate's row is read once.
 // Bound: 131072 positions of 128 candidates of 64 bf16 columns take 2.1 GB from L2 and 0.17 GB from HBM (26 us) in 250 us, 8.6
-// TB/s; L2 is at a third of its rate, the issue slots are 67 % busy: unpacking, weighing (two FMAs an instruction) and the
+// TB/s; L2 is at 41 % of its rate, the issue slots are 64 % busy: unpacking, weighing (two FMAs an instruction) and the
 // ids.  32768 x 128 x 128: 117 us, 9.2 TB/s.  fp32, 12795 x 100 x 50: 45 us.  64 x 101, no gradient: 4 us of a block's latency.
 #include <float.h>
 
