@@ -357,6 +357,27 @@ blossom_stream_t stream_of(const Tensor &t) {
   return (blossom_stream_t)c10::cuda::getCurrentCUDAStream(t.device().index()).stream();
 }
 
+// What a node saved, as the saved-tensor hooks return it: the same numbers, in any layout (offloading to the host gives a slice
+// of a wider buffer back without the gaps), so that strides are those of what came back.
+void expect_saved(bool same, const char *what) {
+  if (!same) throw std::runtime_error(std::string(what) + ": a saved-tensor hook returned another tensor than it was given");
+}
+Tensor saved_rows(const SavedVariable &saved, int64_t rows, int64_t cols, at::ScalarType type, at::Device dev, const char *what,
+                  RowView *v) {
+  const Tensor t = saved.unpack();
+  expect_saved(t.defined() && t.device() == dev && t.scalar_type() == type && t.dim() > 0, what);
+  const Tensor r = as_rows(t, v);
+  expect_saved(v->rows == rows && v->cols == cols, what);
+  return r;
+}
+Tensor saved_plain(const SavedVariable &saved, int64_t numel, at::ScalarType type, at::Device dev, const char *what) {
+  const Tensor t = saved.unpack();
+  expect_saved(t.defined() && t.device() == dev && t.scalar_type() == type && t.numel() == numel, what);
+  Tensor r = t.contiguous();
+  make_plain(r);
+  return r;
+}
+
 // The gradients are not differentiable again: asked for a graph of them, whoever uses it is told so.
 void once_differentiable(variable_list &res, const char *what) {
   if (!at::GradMode::is_enabled()) return;
@@ -380,8 +401,8 @@ struct BlossomDropoutBackward : public Node {
     if (!grads[0].defined()) return res;
     {
       at::NoGradGuard no_grad;
-      const Tensor rng = rng_.unpack();
-      c10::cuda::CUDAGuard guard(rng.device());
+      c10::cuda::CUDAGuard guard(grads[0].device());
+      const Tensor rng = saved_plain(rng_, 2, at::kLong, grads[0].device(), "blossom_dropout");
       RowView v;
       const Tensor dout = as_rows(grads[0], &v);
       const Tensor dx = fresh(dout.sizes(), dout.scalar_type(), dout.device());
@@ -400,7 +421,7 @@ struct BlossomDropoutBackward : public Node {
 struct BlossomAddNormBackward : public Node {
   SavedVariable x_, res_, weight_, rng_, stats_;
   blossom_rows_params params_;
-  bool has_bias_;
+  bool has_res_, has_weight_, has_bias_;
 
   std::string name() const override { return "BlossomAddNormBackward"; }
   void release_variables() override {
@@ -411,19 +432,27 @@ struct BlossomAddNormBackward : public Node {
     if (!grads[0].defined()) return out;
     {
       at::NoGradGuard no_grad;
-      const Tensor x = x_.unpack(), res = res_.unpack(), weight = weight_.unpack(), rng = rng_.unpack(),
-                   stats = stats_.unpack();
-      c10::cuda::CUDAGuard guard(x.device());
-      RowView v;
-      Tensor dout = as_rows(grads[0], &v);
+      const char *const what = "blossom_add_norm";
       blossom_rows_params p = params_;
+      const at::Device dev = grads[0].device();
+      const auto type = p.dtype == BLOSSOM_DTYPE_FP32 ? at::kFloat : at::kBFloat16,
+                 wtype = p.weight_dtype == BLOSSOM_DTYPE_FP32 ? at::kFloat : at::kBFloat16;
+      c10::cuda::CUDAGuard guard(dev);
+      RowView xv, rv, v;
+      Tensor res, weight, rng;
+      const Tensor x = saved_rows(x_, p.rows, p.cols, type, dev, what, &xv);
+      if (has_res_) res = saved_rows(res_, p.rows, p.cols, type, dev, what, &rv);
+      if (has_weight_) weight = saved_plain(weight_, p.cols, wtype, dev, what);
+      if (p.dropout > 0.0) rng = saved_plain(rng_, 2, at::kLong, dev, what);
+      const Tensor stats = saved_plain(stats_, 2 * p.rows, at::kFloat, dev, what);
+      const Tensor dout = as_rows(grads[0], &v);
+      p.x_stride = xv.stride;
+      p.residual_stride = rv.stride;
       p.out_stride = v.stride;
-      const auto type = x.scalar_type(), wtype = p.weight_dtype == BLOSSOM_DTYPE_FP32 ? at::kFloat : at::kBFloat16;
-      const at::Device dev = x.device();
       const bool want_x = task_should_compute_output(0), want_res = res.defined() && task_should_compute_output(1);
       // without dropout the two gradients are one
-      if (want_x || (want_res && p.dropout == 0.0)) out[0] = fresh(x.sizes(), type, dev);
-      if (want_res && p.dropout > 0.0) out[1] = fresh(x.sizes(), type, dev);
+      if (want_x || (want_res && p.dropout == 0.0)) out[0] = fresh(dout.sizes(), type, dev);
+      if (want_res && p.dropout > 0.0) out[1] = fresh(dout.sizes(), type, dev);
       if (weight.defined() && task_should_compute_output(2)) out[2] = fresh({p.cols}, wtype, dev);
       if (has_bias_ && task_should_compute_output(3)) out[3] = fresh({p.cols}, wtype, dev);
       const size_t bytes = blossom_add_norm_workspace_bytes(&p);
@@ -574,6 +603,8 @@ PyObject *add_norm(PyObject *, PyObject *const *a, Py_ssize_t n) {
       node->rng_ = SavedVariable(state, false);
       node->stats_ = SavedVariable(stats, false);
       node->params_ = p;
+      node->has_res_ = res.defined();
+      node->has_weight_ = weight.defined();
       node->has_bias_ = bias.defined();
       torch::autograd::set_history(out, node);
     }
@@ -588,6 +619,7 @@ PyObject *add_norm(PyObject *, PyObject *const *a, Py_ssize_t n) {
 struct BlossomSampledLossBackward : public Node {
   SavedVariable hidden_, table_, targets_, negatives_, lse_, grad_;
   blossom_loss_params params_;
+  bool has_grad_;
 
   std::string name() const override { return "BlossomSampledLossBackward"; }
   void release_variables() override {
@@ -598,22 +630,39 @@ struct BlossomSampledLossBackward : public Node {
     if (!grads[0].defined()) return out;
     {
       at::NoGradGuard no_grad;
-      const Tensor hidden = hidden_.unpack(), table = table_.unpack(), targets = targets_.unpack(),
-                   negatives = negatives_.unpack(), lse = lse_.unpack(), grad = grad_.unpack();
-      c10::cuda::CUDAGuard guard(hidden.device());
+      const char *const what = "blossom_sampled_loss";
+      blossom_loss_params p = params_;
+      const at::Device dev = grads[0].device();
+      const auto type = p.dtype == BLOSSOM_DTYPE_FP32 ? at::kFloat : at::kBFloat16,
+                 ids = p.index_bytes == 8 ? at::kLong : at::kInt;
+      c10::cuda::CUDAGuard guard(dev);
+      RowView hv, tv, nv;
+      Tensor negatives, grad;
+      const Tensor hidden = saved_rows(hidden_, p.rows, p.cols, type, dev, what, &hv);
+      const Tensor table = saved_rows(table_, p.items, p.cols, type, dev, what, &tv);
+      const Tensor targets = saved_plain(targets_, p.rows, ids, dev, what);
+      if (p.negatives && p.negatives_stride) {
+        negatives = saved_rows(negatives_, p.rows, p.negatives, ids, dev, what, &nv);
+        p.negatives_stride = nv.stride;
+      } else if (p.negatives) {
+        negatives = saved_plain(negatives_, p.negatives, ids, dev, what);
+      }
+      const Tensor lse = saved_plain(lse_, p.rows + 1, at::kFloat, dev, what);
+      if (has_grad_) grad = saved_plain(grad_, p.rows * p.cols, at::kFloat, dev, what);
+      p.hidden_stride = hv.stride;
+      p.table_stride = tv.stride;
       Tensor g = grads[0];
       make_plain(g);
-      const at::Device dev = hidden.device();
       if (grad.defined() && task_should_compute_output(0)) out[0] = fresh(hidden.sizes(), hidden.scalar_type(), dev);
       Tensor ws;
       if (task_should_compute_output(1)) {
         out[1] = fresh(table.sizes(), table.scalar_type(), dev);
-        ws = fresh({(int64_t)blossom_sampled_loss_workspace_bytes(&params_)}, at::kByte, dev);
+        ws = fresh({(int64_t)blossom_sampled_loss_workspace_bytes(&p)}, at::kByte, dev);
       }
       auto at = [](const Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; };
       if (out[0].defined() || out[1].defined()) {
         const int rc = blossom_sampled_loss_bwd(
-            &params_, hidden.data_ptr(), table.data_ptr(), targets.data_ptr(), at(negatives), lse.data_ptr<float>(),
+            &p, hidden.data_ptr(), table.data_ptr(), targets.data_ptr(), at(negatives), lse.data_ptr<float>(),
             static_cast<const float *>(at(grad)), g.data_ptr<float>(), at(out[0]), at(out[1]), at(ws),
             ws.defined() ? (size_t)ws.nbytes() : 0, stream_of(hidden));
         if (rc) throw std::runtime_error(failure("blossom_sampled_loss_bwd", rc));
@@ -705,6 +754,7 @@ PyObject *sampled_loss(PyObject *, PyObject *const *a, Py_ssize_t n) {
       node->negatives_ = SavedVariable(n_neg ? negatives : Tensor(), false);
       node->lse_ = SavedVariable(lse, false);
       node->grad_ = SavedVariable(gh, false);
+      node->has_grad_ = gh.defined();
       node->params_ = p;
       torch::autograd::set_history(loss, node);
     }

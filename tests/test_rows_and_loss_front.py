@@ -1,0 +1,106 @@
+"""The autograd nodes of dropout, residual + layer norm and the sampled loss beyond the ordinary call: saved tensors that come
+back in another layout or as something else."""
+import pytest
+
+
+def operators(offset=3, pads=(16, 7, 16, 9), seed=0):
+    """(name, function of the leaves, leaves, ids of the loss): every tensor that is saved is a slice of a wider buffer."""
+    import torch
+    from paper_2512_13368_b200.autograd import blossom_add_norm, blossom_dropout, blossom_sampled_loss
+    g = torch.Generator(device="cuda").manual_seed(seed)
+
+    def sliced(rows, cols, pad, dtype):
+        return torch.randn(rows, cols + pad, generator=g, device="cuda").to(dtype)[:, offset:offset + cols].detach()
+
+    def ids(hi, *shape, pad=0):
+        t = torch.randint(0, hi, (*shape[:-1], shape[-1] + pad), generator=g, device="cuda")
+        return t[..., :shape[-1]]
+
+    rng = torch.tensor([[5, 0], [9, 0]], device="cuda")[:, 0]   # (its two numbers are not next to each other)
+    res = []
+    for dtype, cols in ((torch.bfloat16, 64), (torch.float32, 50)):
+        x, r, h, w = (sliced(n, cols, pad, dtype) for n, pad in zip((90, 90, 90, 40), pads))
+        weight, bias = (torch.randn(2 * cols, generator=g, device="cuda").to(dtype)[::2] for _ in range(2))
+        t, own, shared = ids(40, 180)[::2], ids(40, 90, 7, pad=5), ids(40, 14)[::2]
+        res += [("dropout", lambda a: blossom_dropout(a, 0.3, rng, site=4), [x], None),
+                ("norm", lambda a, b, c, d: blossom_add_norm(a, b, c, d, p=0.3, rng=rng, site=4), [x, r, weight, bias], None),
+                ("norm, no dropout", lambda a, b, c, d: blossom_add_norm(a, b, c, d), [x, r, weight, bias], None),
+                ("norm alone", lambda a: blossom_add_norm(a, None, None, None), [x], None),
+                ("loss", lambda a, b, t=t, n=own: blossom_sampled_loss(a, b, t, n), [h, w], (t, own)),
+                ("loss, shared", lambda a, b, t=t, n=shared: blossom_sampled_loss(a, b, t, n), [h, w], (t, shared)),
+                ("loss, no negatives", lambda a, b, t=t, n=own: blossom_sampled_loss(a, b, t, n[:, :0]), [h, w], (t, own[:, :0]))]
+    return res
+
+
+def step(f, leaves, make=None):
+    """Output and gradients; make: what calls f."""
+    import torch
+    a = [t.detach().requires_grad_(True) for t in leaves]
+    assert all(x.stride() == y.stride() for x, y in zip(a, leaves))
+    out = f(*a) if make is None else make(f, *a)
+    return [out.detach()] + list(torch.autograd.grad(out, a, torch.full_like(out, 0.75)))
+
+
+@pytest.mark.gpu
+def test_saved_tensors_may_come_back_in_another_layout():
+    """Offloaded to the host and brought back a slice has lost its gaps; computed again it may lie elsewhere.  The same bits, but for
+    the loss in layouts of another alignment, by which its kernels (the order of their sums) go: there within the
+    definition's bounds."""
+    import torch
+    from test_sampled_loss import compare, reference
+    from torch.utils.checkpoint import checkpoint
+
+    def offload(pin):
+        def make(f, *a):
+            with torch.autograd.graph.save_on_cpu(pin_memory=pin):
+                return f(*a)
+        return make
+
+    def gaps(t):    # the same numbers with gaps between rows, elements of a vector apart
+        if t.dim() == 0:
+            return t
+        big = torch.zeros(*t.shape[:-1], 2 * t.shape[-1] + 6, dtype=t.dtype, device=t.device)
+        view = big[..., 2:2 + t.shape[-1]] if t.dim() > 1 else big[2:2 + 2 * t.shape[-1]:2]
+        return view.copy_(t) if t.numel() else t
+
+    def widen(f, *a):
+        with torch.autograd.graph.saved_tensors_hooks(lambda t: t, gaps):
+            return f(*a)
+
+    for offset, pads in ((3, (16, 7, 16, 9)), (0, (16, 8, 16, 8))):
+        for name, f, leaves, ids in operators(offset, pads):
+            want = step(f, leaves)
+            if ids:
+                exact, tol = reference(*leaves, *ids)
+                exact, tol = ({k: d[k] * (1.0 if k == "loss" else 0.75) for k in ("loss", "dhidden", "dtable")} for d in (exact, tol))
+            for make in (offload(False), offload(True), widen, lambda f, *a: checkpoint(f, *a, use_reentrant=False)):
+                got = step(f, leaves, make)
+                if ids:
+                    compare(dict(zip(exact, got)), exact, tol, leaves[0].dtype == torch.bfloat16, name)
+                if not ids or (offset == 0 and make is not widen):
+                    assert all(torch.equal(a, b) for a, b in zip(got, want)), name
+
+
+@pytest.mark.gpu
+def test_saved_tensors_that_are_something_else_are_refused():
+    """Fewer rows, other types, another device: an error, whichever of the saved tensors it is."""
+    import torch
+    change = {"shorter": lambda t: t[:-1], "wider": lambda t: torch.cat([t, t], -1),
+              "type": lambda t: t.to(torch.float64 if t.is_floating_point() else torch.int16), "device": lambda t: t.cpu()}
+    for name, f, leaves, _ in operators():
+        for how, other in change.items():
+            which, count = 0, 1
+            while which < count:
+                packed = []
+
+                def pack(t):
+                    packed.append(t)  # noqa: B023
+                    return len(packed) - 1, t  # noqa: B023
+
+                a = [t.detach().requires_grad_(True) for t in leaves]
+                with torch.autograd.graph.saved_tensors_hooks(pack, lambda it: other(it[1]) if it[0] == which else it[1]):  # noqa: B023
+                    out = f(*a)
+                with pytest.raises(RuntimeError, match="hook"):
+                    torch.autograd.grad(out, a, torch.full_like(out, 0.75))
+                which, count = which + 1, len(packed)
+            assert count >= 1, (name, how)
