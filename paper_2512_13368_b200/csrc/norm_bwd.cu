@@ -62,7 +62,7 @@ __global__ void __launch_bounds__(P::threads, resident<P>)
     for (int i = 0; i < 4; ++i) gw[v].p[i] = gb[v].p[i] = both(0.f);
   const uint32_t rows = (uint32_t)a.rows, step = gridDim.x * (uint32_t)P::slots;
   uint32_t left = blockIdx.x * (uint32_t)P::slots, row = left + (uint32_t)slot;
-  const T *px = x + row * a.sx + 8 * lane, *pr = res + row * a.sr + 8 * lane, *pd = dout + row * a.so + 8 * lane;
+  const T *px = x + row * a.sx + 8 * lane, *pr = (res ? res : x) + row * a.sr + 8 * lane, *pd = dout + row * a.so + 8 * lane;
   T *pdx = dx + row * a.sdx + 8 * lane, *pdr = dres + row * a.sdr + 8 * lane;
   Raw<T, W> xs[V], rs[V], ds[V];
   const typename Shape<T, W, P>::Rows ring(stages);
@@ -288,6 +288,7 @@ extern "C" int blossom_add_norm_bwd(const blossom_rows_params *params, const voi
     return BLOSSOM_ERR_WORKSPACE;
   rows::Alignment al;
   al.rows_at(x, a.sx, esz);
+  if (!residual) a.sr = a.sx;  // (a copy of no bytes needs an aligned address as well: x's)
   al.rows_at(residual, a.sr, esz);
   al.rows_at(dout, a.so, esz);
   al.rows_at(dx, a.sdx, esz);

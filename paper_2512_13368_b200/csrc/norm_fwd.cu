@@ -66,7 +66,7 @@ __global__ void __launch_bounds__(P::threads, Shape<T, W, P>::resident)
   }
   const uint32_t rows = (uint32_t)a.rows, step = gridDim.x * (uint32_t)(P::slots * U);
   uint32_t row0 = blockIdx.x * (uint32_t)(P::slots * U) + (uint32_t)slot, left = blockIdx.x * (uint32_t)(P::slots * U);
-  const T *px = x + row0 * a.sx + 8 * lane, *pr = res + row0 * a.sr + 8 * lane;
+  const T *px = x + row0 * a.sx + 8 * lane, *pr = (res ? res : x) + row0 * a.sr + 8 * lane;
   T *po = out + row0 * a.so + 8 * lane;
   Raw<T, W> xs[U][V], rs[U][V];
   const typename Shape<T, W, P>::Rows ring(wb + Shape<T, W, P>::weights / sizeof(float4));
@@ -180,6 +180,7 @@ extern "C" int blossom_add_norm_fwd(const blossom_rows_params *params, const voi
   if (reinterpret_cast<uintptr_t>(stats) % 8) return BLOSSOM_ERR_INVALID_ARG;
   rows::Alignment al;
   al.rows_at(x, a.sx, esz);
+  if (!residual) a.sr = a.sx;  // (a copy of no bytes needs an aligned address as well: x's)
   al.rows_at(residual, a.sr, esz);
   al.rows_at(out, a.so, esz);
   bool ok = true;
