@@ -315,7 +315,7 @@ typedef struct {
   int64_t rows;             /* >= 0; rows * (negatives + 1) < 2^31                                        */
   int32_t cols;             /* 1 .. 1024                                                                 */
   int32_t items;            /* 1 <= items < 2^30                                                         */
-  int32_t negatives;        /* n >= 0 per row                                                            */
+  int32_t negatives;        /* 0 <= n < 2^24 per row                                                     */
   int32_t dtype;            /* of hidden, table, dhidden, dtable                                         */
   int32_t index_bytes;      /* 4 or 8: targets and negatives are int32 or int64                          */
   int32_t mask_hits;        /* 1: a negative equal to the row's target is no candidate                   */

@@ -223,7 +223,7 @@ def blossom_sampled_loss(hidden, table, targets, negatives, ignore_index=-100, m
     ``logsumexp(logits) - logits[target]`` with the logits ``<hidden, table[c]>`` of the target and the negatives.
 
     hidden [..., C] and table [items, C]: float32 or bfloat16 (CUDA), C up to 1024; targets [...]: int32 or int64, a position
-    whose target is ``ignore_index`` or no item takes no part; negatives [..., n], or [n] for all positions alike: ids
+    whose target is ``ignore_index`` or no item takes no part; negatives [..., n], or [n] for all positions alike (n < 2^24): ids
     that are no items are no candidates, and with ``mask_hits`` those equal to the position's target are none.
     Returns a float32 scalar (0 if no position takes part), differentiable in hidden and table."""
     res = _module().sampled_loss(hidden, table, targets, negatives, ignore_index, mask_hits)

@@ -10,6 +10,9 @@ using rows::both;
 using rows::Group;
 using rows::mul2;
 
+// A row's candidates: numbers of them, and where the strides behind the last one lead, stay far from 2^31, and a running sum of
+// exponentials in single precision still grows (it takes no more ones from 2^24 on).
+constexpr int kMaxNegatives = (1 << 24) - 1;
 constexpr int kMaxCols = 1024, kMaxRowCtas = kSMs * 16, kMmaThreads = 128;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 

@@ -397,7 +397,7 @@ int check(const blossom_loss_params *p, Args *a) {
   }
   if (p->negatives_stride < 0) return BLOSSOM_ERR_INVALID_ARG;
   const int64_t most = 0x7fffffffLL;
-  if (p->cols > kMaxCols || p->items >= 1 << 30 || p->negatives_stride > most || p->rows > most || p->negatives == most ||
+  if (p->cols > kMaxCols || p->items >= 1 << 30 || p->negatives_stride > most || p->rows > most || p->negatives > kMaxNegatives ||
       (p->rows > 0 && p->rows > most / ((int64_t)p->negatives + 1)))
     return BLOSSOM_ERR_UNSUPPORTED;
   a->rows = (int)p->rows, a->cols = p->cols, a->groups = (p->cols + 7) / 8, a->items = p->items, a->n = p->negatives;
