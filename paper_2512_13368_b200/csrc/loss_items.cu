@@ -721,11 +721,12 @@ __global__ void __launch_bounds__(kThreads) loss_join_kernel(Args a, const float
     const float scale = grad_scale(a, lse, grad_loss);
     const int64_t step = (int64_t)(gridDim.x - join_ctas) * NG;
     for (int64_t row = (int64_t)(blockIdx.x - join_ctas) * NG + grp; row < a.rows; row += step) {
+      const bool part = row_target(a, (int)row) >= 0;  // (else zeros whatever the upstream gradient is)
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         Group x = load_sums<W, P>(grad_hidden + row * a.cols, col, v, a.cols);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x.p[i] = mul2(x.p[i], both(scale));
+        for (int i = 0; i < 4; ++i) x.p[i] = part ? mul2(x.p[i], both(scale)) : both(0.f);
         S::store(dhidden + row * a.sdh, col, v, a.cols, x);
       }
     }
@@ -762,11 +763,11 @@ __global__ void __launch_bounds__(kThreads) loss_join_kernel(Args a, const float
       }
     }
   };
-  auto write = [&](int64_t to, Group (&acc)[V]) {
+  auto write = [&](int64_t to, Group (&acc)[V], bool some = true) {
 #pragma unroll
     for (int v = 0; v < V; ++v) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) acc[v].p[i] = mul2(acc[v].p[i], both(scale));
+      for (int i = 0; i < 4; ++i) acc[v].p[i] = some ? mul2(acc[v].p[i], both(scale)) : both(0.f);
       S::store(dtable + to * a.sdt, col, v, a.cols, acc[v]);
     }
   };
@@ -779,15 +780,8 @@ __global__ void __launch_bounds__(kThreads) loss_join_kernel(Args a, const float
     const uint32_t b0 = __shfl_sync(0xffffffffu, c0, from), b1 = __shfl_sync(0xffffffffu, c1, from);
     const bool in = __shfl_sync(0xffffffffu, (int)inside, from);
     if (item0 + from >= a.items || many == 1 || many > kAlone) continue;  // (one span: written by the kernel before)
-    if (many) {
-      add_up(b0, b1, in, 0, 1, acc);
-    } else {
-#pragma unroll
-      for (int v = 0; v < V; ++v)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc[v].p[i] = both(0.f);
-    }
-    write(item0 + from, acc);
+    if (many) add_up(b0, b1, in, 0, 1, acc);
+    write(item0 + from, acc, many > 0);  // (nobody's candidate: zeros whatever the upstream gradient is)
   }
   if (n > kAlone) {  // (in which order they are noted does not matter: each is summed by itself)
     const int at = atomicAdd(&populars, 1);
