@@ -202,7 +202,10 @@ __global__ void __launch_bounds__(P::threads, resident<P>)
 
 // dweight and dbias from the CTAs' partial sums: 16 columns and 32 slices of the CTAs a block, 8 loads in flight a thread.
 // Bound: latency of a few dependent loads (1184 x 2048 sums, 9.7 MB: 6 us behind the backward).
+// SHARED: behind a backward that asked for all of an SM's shared memory (prefer_shared).  A function keeps that request from call
+// to call; with a kernel of their own the narrow rows' launches do not depend on whether a wide call came before.
 constexpr int kSumCols = 16, kSumSlices = 32;
+template <bool SHARED>
 __global__ void __launch_bounds__(kSumCols *kSumSlices) norm_weights_kernel(int cols, int ctas, const float *__restrict__ part,
                                                                             int wide, void *__restrict__ dweight,
                                                                             void *__restrict__ dbias) {
@@ -315,9 +318,10 @@ extern "C" int blossom_add_norm_bwd(const blossom_rows_params *params, const voi
   });
   if (!ok) return BLOSSOM_ERR_CUDA;
   if (part) {
-    if (wide) rows::prefer_shared(rows::norm_weights_kernel);
+    const auto kern = wide ? rows::norm_weights_kernel<true> : rows::norm_weights_kernel<false>;
+    if (wide) rows::prefer_shared(kern);
     LaunchScope ls(K_NORM_WEIGHTS, st);
-    launch_chained(rows::norm_weights_kernel, dim3((unsigned)((2 * a.cols + rows::kSumCols - 1) / rows::kSumCols)),
+    launch_chained(kern, dim3((unsigned)((2 * a.cols + rows::kSumCols - 1) / rows::kSumCols)),
                    dim3(rows::kSumCols * rows::kSumSlices), 0, st, a.cols, ctas,
                    (const float *)part, a.wide_weights, dweight, dbias);
   }
