@@ -166,6 +166,10 @@ bool read_int(PyObject *o, int32_t *out) {
     Py_DECREF(n);
   }
   if (x == -1 && PyErr_Occurred()) return false;
+  if (x != static_cast<int32_t>(x)) {
+    PyErr_Format(PyExc_OverflowError, "%ld does not fit 32 bits", x);
+    return false;
+  }
   *out = static_cast<int32_t>(x);
   return true;
 }

@@ -1,6 +1,8 @@
 """The autograd nodes of dropout, residual + layer norm and the sampled loss beyond the ordinary call: saved tensors that come
-back in another layout or as something else."""
+back in another layout or as something else, integers that do not fit."""
 import pytest
+
+from paper_2512_13368_b200 import build
 
 
 def operators(offset=3, pads=(16, 7, 16, 9), seed=0):
@@ -104,3 +106,22 @@ def test_saved_tensors_that_are_something_else_are_refused():
                     torch.autograd.grad(out, a, torch.full_like(out, 0.75))
                 which, count = which + 1, len(packed)
             assert count >= 1, (name, how)
+
+
+def test_integers_of_more_than_32_bits_are_refused():
+    """Their low half must not pass for the number, in the attention's arguments neither."""
+    import torch
+    build.build()
+    from paper_2512_13368_b200 import autograd
+    front = autograd._module()
+    x, rng, ids = torch.zeros(4, 8), torch.zeros(2, dtype=torch.int64), torch.zeros(4, dtype=torch.int64)
+    q, gate = torch.zeros(1, 1, 8, 32), torch.zeros(1, 2)
+    tail = (8, 2, 8, 0.0, 0, 8, 0, 0, 0, 0, 1, 0.0)
+    assert front.dropout(x, 0.5, rng, 5) is None      # (a host tensor: the caller says what is wrong)
+    assert front.attention(q, q, q, gate, None, None, *tail) is None
+    for wide in ((1 << 32) + 5, 1 << 31, -(1 << 31) - 1, 1 << 62, 1 << 70, torch.tensor((1 << 32) + 5)):
+        for call in (lambda: front.dropout(x, 0.5, rng, wide), lambda: front.add_norm(x, None, None, None, 0.5, rng, wide, 1e-5),  # noqa: B023
+                     lambda: front.sampled_loss(x, x, ids, ids, -100, wide),  # noqa: B023
+                     lambda: front.attention(q, q, q, gate, None, None, wide, *tail[1:])):  # noqa: B023
+            with pytest.raises(OverflowError):
+                call()
