@@ -291,8 +291,8 @@ int blossom_add_norm_fwd(const blossom_rows_params *params /* host */, const voi
  *   x, residual, weight, rng   in   as given to the forward (z and what is kept are formed again)
  *   dx, dresidual              out  either may be NULL (not wanted); without dropout they are equal, so one suffices
  *   dweight, dbias             out  [cols], either may be NULL (not wanted)
- *   workspace                  blossom_add_norm_workspace_bytes, 256-byte aligned: partial sums of dweight and dbias,
- *                              added up in a fixed order; carries nothing from call to call */
+ *   workspace                  needed for dweight and dbias only: blossom_add_norm_workspace_bytes, 256-byte aligned, for
+ *                              their partial sums, added up in a fixed order; carries nothing from call to call */
 int blossom_add_norm_bwd(const blossom_rows_params *params /* host */, const void *x, const void *residual,
                          const void *weight, const int64_t *rng, const float *stats, const void *dout, void *dx,
                          void *dresidual, void *dweight, void *dbias, void *workspace, size_t workspace_bytes,

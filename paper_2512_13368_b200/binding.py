@@ -152,6 +152,8 @@ def _ptr(x):
 
 
 def _nbytes(x):
+    if x is None:
+        return 0
     if isinstance(x, int):
         return x
     return x.numel() * x.element_size()

@@ -459,12 +459,13 @@ struct BlossomAddNormBackward : public Node {
       if (want_res && p.dropout > 0.0) out[1] = fresh(dout.sizes(), type, dev);
       if (weight.defined() && task_should_compute_output(2)) out[2] = fresh({p.cols}, wtype, dev);
       if (has_bias_ && task_should_compute_output(3)) out[3] = fresh({p.cols}, wtype, dev);
-      const size_t bytes = blossom_add_norm_workspace_bytes(&p);
-      const Tensor ws = fresh({(int64_t)bytes}, at::kByte, dev);
+      const size_t bytes = out[2].defined() || out[3].defined() ? blossom_add_norm_workspace_bytes(&p) : 0;
+      Tensor ws;
+      if (bytes) ws = fresh({(int64_t)bytes}, at::kByte, dev);
       auto at = [](const Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; };
       const int rc = blossom_add_norm_bwd(&p, x.data_ptr(), at(res), at(weight), static_cast<const int64_t *>(at(rng)),
                                           stats.data_ptr<float>(), dout.data_ptr(), at(out[0]), at(out[1]), at(out[2]),
-                                          at(out[3]), ws.data_ptr(), bytes, stream_of(x));
+                                          at(out[3]), at(ws), bytes, stream_of(x));
       if (rc) throw std::runtime_error(failure("blossom_add_norm_bwd", rc));
       if (want_res && p.dropout == 0.0) {
         out[1] = out[0];

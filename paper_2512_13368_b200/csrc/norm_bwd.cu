@@ -286,8 +286,8 @@ extern "C" int blossom_add_norm_bwd(const blossom_rows_params *params, const voi
   for (const void *p : {x, residual, dout, (const void *)dx, (const void *)dresidual})
     if (reinterpret_cast<uintptr_t>(p) % esz) return BLOSSOM_ERR_INVALID_ARG;
   if (reinterpret_cast<uintptr_t>(stats) % 8) return BLOSSOM_ERR_INVALID_ARG;
-  if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256 ||
-      workspace_bytes < blossom_add_norm_workspace_bytes(params))
+  if ((dweight || dbias) && (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256 ||
+                             workspace_bytes < blossom_add_norm_workspace_bytes(params)))
     return BLOSSOM_ERR_WORKSPACE;
   rows::Alignment al;
   al.rows_at(x, a.sx, esz);
