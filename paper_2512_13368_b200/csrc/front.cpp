@@ -513,6 +513,7 @@ PyObject *dropout(PyObject *, PyObject *const *a, Py_ssize_t n) {
       at::NoGradGuard no_grad;
       x = as_rows(x0, &v);
       state = rng.contiguous();
+      make_plain(state);
     }
     p.rows = v.rows;
     p.cols = (int32_t)std::min<int64_t>(v.cols, INT32_MAX);
@@ -578,7 +579,10 @@ PyObject *add_norm(PyObject *, PyObject *const *a, Py_ssize_t n) {
           *t = t->contiguous();
           make_plain(*t);
         }
-      if (p.dropout != 0.0) state = rng.contiguous();
+      if (p.dropout != 0.0) {
+        state = rng.contiguous();
+        make_plain(state);
+      }
     }
     p.rows = v.rows;
     p.cols = (int32_t)std::min<int64_t>(v.cols, INT32_MAX);

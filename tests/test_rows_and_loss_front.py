@@ -1,5 +1,5 @@
 """The autograd nodes of dropout, residual + layer norm and the sampled loss beyond the ordinary call: saved tensors that come
-back in another layout or as something else, integers that do not fit."""
+back in another layout or as something else, integers that do not fit, tensors that are not plain memory."""
 import pytest
 
 from paper_2512_13368_b200 import build
@@ -125,3 +125,41 @@ def test_integers_of_more_than_32_bits_are_refused():
                      lambda: front.attention(q, q, q, gate, None, None, wide, *tail[1:])):  # noqa: B023
             with pytest.raises(OverflowError):
                 call()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,cols", [("bf16", 64), ("fp32", 50)])
+def test_negated_views_and_zero_tensors_that_need_no_copy_for_their_layout(dtype, cols):
+    """Every input, the generator's state among them, and the upstream gradient: what plain copies give."""
+    import torch
+    from paper_2512_13368_b200.autograd import blossom_add_norm, blossom_dropout, blossom_sampled_loss
+    dt = torch.float32 if dtype == "fp32" else torch.bfloat16
+    g = torch.Generator(device="cuda").manual_seed(cols)
+    mk = lambda *s: torch.randn(s, generator=g, device="cuda").to(dt)  # noqa: E731
+    ids = lambda *s: torch.randint(0, 40, s, generator=g, device="cuda")  # noqa: E731
+    rng = torch.tensor([7, 3], device="cuda")
+    cases = [(lambda x, rng: blossom_dropout(x, 0.4, rng, site=2), dict(x=mk(30, cols), rng=rng), mk(30, cols)),
+             (lambda x, r, w, b, rng: blossom_add_norm(x, r, w, b, p=0.4, rng=rng, site=2),
+              dict(x=mk(30, cols), r=mk(30, cols), w=mk(cols), b=mk(cols), rng=rng), mk(30, cols)),
+             (blossom_sampled_loss, dict(hidden=mk(30, cols), table=mk(40, cols), targets=ids(30), negatives=ids(30, 5)),
+              torch.tensor(0.75, device="cuda")),
+             (blossom_sampled_loss, dict(hidden=mk(30, cols), table=mk(40, cols), targets=ids(30), negatives=ids(5)),
+              torch.tensor(0.75, device="cuda"))]
+
+    def step(f, args, dout):
+        a = {k: (t.detach().requires_grad_(True) if t.is_floating_point() else t) for k, t in args.items()}
+        out = f(**a)
+        return [out.detach()] + list(torch.autograd.grad(out, [t for t in a.values() if t.requires_grad], dout))
+
+    for f, args, dout in cases:
+        want = step(f, args, dout)
+        for k, t in dict(args, dout=dout).items():
+            neg = torch._neg_view(-t)
+            assert neg.is_neg() and torch.equal(neg, t) and neg.stride() == t.stride()
+            zero = torch._efficientzerotensor(t.shape, dtype=t.dtype, device="cuda")
+            assert zero._is_zerotensor()
+            plain = torch.zeros_like(t)
+            ref = step(f, args, plain) if k == "dout" else step(f, dict(args, **{k: plain}), dout)
+            for other, res in ((neg, want), (zero, ref)):
+                got = step(f, args, other) if k == "dout" else step(f, dict(args, **{k: other}), dout)
+                assert all(torch.equal(x, y) for x, y in zip(got, res)), k
