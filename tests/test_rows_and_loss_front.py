@@ -1,5 +1,8 @@
 """The autograd nodes of dropout, residual + layer norm and the sampled loss beyond the ordinary call: saved tensors that come
-back in another layout or as something else, integers that do not fit, tensors that are not plain memory."""
+back in another layout or as something else, integers that do not fit, tensors that are not plain memory, transforms without a
+rule, host threads."""
+import threading
+
 import pytest
 
 from paper_2512_13368_b200 import build
@@ -163,3 +166,98 @@ def test_negated_views_and_zero_tensors_that_need_no_copy_for_their_layout(dtype
             for other, res in ((neg, want), (zero, ref)):
                 got = step(f, args, other) if k == "dout" else step(f, dict(args, **{k: other}), dout)
                 assert all(torch.equal(x, y) for x, y in zip(got, res)), k
+
+
+def calls():
+    """(function of its tensors, tensors): every operator, with what is differentiable in front."""
+    import torch
+    from paper_2512_13368_b200.autograd import blossom_add_norm, blossom_dropout, blossom_sampled_loss
+    g = torch.Generator(device="cuda").manual_seed(3)
+    mk = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
+    ids = lambda *s: torch.randint(0, 40, s, generator=g, device="cuda")  # noqa: E731
+    rng = torch.tensor([7, 3], device="cuda")
+    return [(lambda x, rng: blossom_dropout(x, 0.4, rng), [mk(30, 48), rng], 1),
+            (lambda x, r, w, b, rng: blossom_add_norm(x, r, w, b, p=0.4, rng=rng), [mk(30, 48), mk(30, 48), mk(48), mk(48), rng], 4),
+            (lambda x, r, w, b: blossom_add_norm(x, r, w, b), [mk(30, 48), mk(30, 48), mk(48), mk(48)], 4),
+            (blossom_sampled_loss, [mk(30, 48), mk(40, 48), ids(30), ids(30, 5)], 2),
+            (blossom_sampled_loss, [mk(30, 48), mk(40, 48), ids(30), ids(5)], 2)]
+
+
+@pytest.mark.gpu
+def test_transforms_without_a_rule_are_refused():
+    """Batched tensors (vmap) and those of functional gradients have no memory that the library could read."""
+    import torch
+    for f, args, n in calls():
+        for i, x in enumerate(args):
+            one = lambda t: f(*args[:i], t, *args[i + 1:])  # noqa: E731,B023
+            with pytest.raises(RuntimeError):
+                torch.func.vmap(one)(torch.stack([x, x]))
+            if i < n:
+                with pytest.raises(RuntimeError):
+                    torch.func.grad(lambda t: one(t).sum())(x)  # noqa: B023
+        # several upstream gradients at once
+        a = [t.detach().requires_grad_(t.is_floating_point()) for t in args]
+        out = f(*a)
+        with pytest.raises(RuntimeError):
+            torch.autograd.grad(out, a[0], torch.ones((2, *out.shape), device="cuda"), is_grads_batched=True)
+        assert f(*args).shape == out.shape     # (and the interpreter is in order)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("train", [False, True])
+def test_forward_mode_is_refused(train):
+    """There is no forward-mode rule: a tangent is an error, never dropped."""
+    import torch
+    import torch.autograd.forward_ad as fwd
+    for f, args, n in calls():
+        args = [t.detach().requires_grad_(train and t.is_floating_point()) for t in args]
+        with fwd.dual_level():
+            for i in range(n):
+                a = list(args)
+                a[i] = fwd.make_dual(a[i], torch.ones_like(a[i]))
+                with pytest.raises(NotImplementedError):
+                    f(*a)
+        assert torch.isfinite(f(*args)).all()
+
+
+@pytest.mark.gpu
+def test_threads_do_not_disturb_each_other():
+    """Host threads that train at once, each on a stream of its own, with sizes whose kernels want different amounts of shared
+    memory: the bits of the same steps one after another."""
+    import torch
+    from paper_2512_13368_b200.autograd import blossom_add_norm, blossom_dropout, blossom_sampled_loss
+    g = torch.Generator(device="cuda").manual_seed(4)
+    mk = lambda *s: torch.randn(s, generator=g, device="cuda").bfloat16()  # noqa: E731
+    problems = []
+    for rows, cols, items, n in ((400, 64, 700, 9), (900, 512, 300, 3), (300, 1024, 90, 20), (5000, 128, 4000, 15)):
+        problems.append([mk(rows, cols), mk(rows, cols), mk(cols), mk(cols), mk(items, cols),
+                         torch.randint(0, items, (rows,), generator=g, device="cuda"),
+                         torch.randint(0, items, (rows, n), generator=g, device="cuda"), torch.tensor([rows, 1], device="cuda")])
+
+    def step(x, r, w, b, table, targets, negatives, rng):
+        leaves = [t.detach().requires_grad_(True) for t in (x, r, w, b, table)]
+        y = blossom_add_norm(blossom_dropout(leaves[0], 0.2, rng), *leaves[1:4], p=0.1, rng=rng, site=1)
+        loss = blossom_sampled_loss(y, leaves[4], targets, negatives)
+        return [loss.detach()] + list(torch.autograd.grad(loss, leaves))
+
+    want = [step(*p) for p in problems]
+    torch.cuda.synchronize()
+    failures, start = [], threading.Barrier(len(problems))
+
+    def work(p, ref):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                start.wait()
+                for _ in range(60):
+                    got = step(*p)
+                torch.cuda.current_stream().synchronize()
+                assert all(torch.equal(a, b) for a, b in zip(got, ref))
+        except BaseException as e:  # noqa: BLE001
+            failures.append(e)
+
+    threads = [threading.Thread(target=work, args=a) for a in zip(problems, want)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failures, failures
