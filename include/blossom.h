@@ -256,7 +256,8 @@ int blossom_copy_rows(int32_t batch, int32_t heads, int32_t seq_len, int32_t row
  * Tensors are rows of cols elements, row r at r * stride (elements; 0 = cols, else at least cols); any
  * alignment of the element type (16-byte aligned rows of a multiple of 8 columns take the widest accesses).  Sums,
  * mean, variance and gradients are formed in single precision from the unrounded residual + dropout(x) and
- * rounded once to the tensor's type.  The same call gives the same bits.
+ * rounded once to the tensor's type.  The same call gives the same bits.  Layer norm's arithmetic (like the
+ * sampled loss's below) takes subnormal numbers, those below 2^-126, for zeros; blossom_dropout scales them.
  */
 typedef struct {
   int64_t rows;         /* 0 <= rows < 2^31; 0: nothing but dweight, dbias (zeros) is written           */

@@ -22,8 +22,9 @@ NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
     "--use_fast_math", "-Xcompiler", "-fPIC", "-Xptxas", "-v",
 ]
-# --use_fast_math only affects the fp32 attention kernels' exp2f/logf/division; the fp64 block
-# scoring is untouched by it.
+# --use_fast_math shapes all single-precision arithmetic: the attention's and the sampled loss's exp2f, log2f, logf
+# and divisions, the layer norm's rsqrtf, and subnormal numbers, which it takes for zeros (the packed
+# instructions written by hand do as well, but for dropout's scaling).  The fp64 block scoring is untouched by it.
 
 
 def sources():
