@@ -6,6 +6,8 @@
 // in registers, each position's hidden row is read once for both the logit that is formed again and the sum.  An item
 // whose entries lie in one chunk is written there and then; the sums of others go to scratch, one a chunk, and are
 // added up in order.  No atomics on sums: every one has a fixed order whatever the popularity of the items.
+#include <float.h>
+
 #include "loss.cuh"
 
 namespace blossom {
@@ -719,9 +721,11 @@ __global__ void __launch_bounds__(kThreads) loss_join_kernel(Args a, const float
   const int lane = (int)threadIdx.x % 32, col = lane % LPC, sub = lane / LPC, grp = (int)threadIdx.x / LPC;
   if (blockIdx.x >= join_ctas) {
     const float scale = grad_scale(a, lse, grad_loss);
+    const bool number = fabsf(scale) <= FLT_MAX;
     const int64_t step = (int64_t)(gridDim.x - join_ctas) * NG;
     for (int64_t row = (int64_t)(blockIdx.x - join_ctas) * NG + grp; row < a.rows; row += step) {
-      const bool part = row_target(a, (int)row) >= 0;  // (else zeros whatever the upstream gradient is)
+      // (padding has zeros there, which stay zeros in a product with any number: the targets are read only if it is none)
+      const bool part = number || row_target(a, (int)row) >= 0;
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         Group x = load_sums<W, P>(grad_hidden + row * a.cols, col, v, a.cols);
