@@ -257,7 +257,7 @@ int blossom_copy_rows(int32_t batch, int32_t heads, int32_t seq_len, int32_t row
  * alignment of the element type (16-byte aligned rows of a multiple of 8 columns take the widest accesses).  Sums,
  * mean, variance and gradients are formed in single precision from the unrounded residual + dropout(x) and
  * rounded once to the tensor's type.  The same call gives the same bits.  Layer norm's arithmetic (like the
- * sampled loss's below) takes subnormal numbers, those below 2^-126, for zeros; blossom_dropout scales them.
+ * sampled loss's below) may take subnormal numbers, those below 2^-126, for zeros; blossom_dropout scales them.
  */
 typedef struct {
   int64_t rows;         /* 0 <= rows < 2^31; 0: nothing but dweight, dbias (zeros) is written           */

@@ -102,7 +102,8 @@ class BlossomEncoder(nn.Module):
         return x
 
     def loss(self, ids, targets, negatives):
-        """Sampled softmax: the positive against `negatives` [B, L, N] uniform item ids."""
+        """Sampled softmax: the positive against `negatives` [B, L, N] uniform item ids (none of them 0, the
+        padding).  With ``native`` positions whose target is 0 take no part."""
         h = self.forward(ids)                                        # [B, L, C]
         if self.native:
             return blossom_sampled_loss(h, self.emb.weight, targets, negatives, ignore_index=0)
