@@ -437,8 +437,7 @@ int blossom_linear_fwd(const blossom_linear_params *params /* host */, const voi
                        const void *residual, void *out, void *workspace, size_t workspace_bytes, blossom_stream_t stream);
 
 /* With G = dout o act'(x W^T + bias): dx = G W, dweight = G^T x, dbias = sum over the rows of G (dresidual is dout).  For bf16
- * tensors and an activation G is the sum of two bf16 between the products (16 bits); one bf16 where outs >= 512 and
- * rows * cols * outs >= 2^35.
+ * tensors and an activation G is the sum of two bf16 between the products (16 bits).
  *   x         in   as given to the forward; with params.packed its codes; read for dweight and with an activation only, else it
  *                  may be NULL
  *   x_scales  in   with params.packed its scales; otherwise not read

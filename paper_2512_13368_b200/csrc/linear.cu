@@ -46,12 +46,9 @@ struct Scratch {
   size_t bytes;
 };
 // Between the products G is bf16.  Rounded to one its error is as large as the results' own rounding (together 1.4 times that), so
-// what the rounding leaves goes through the products as a second part of G, which makes that of dx and dweight twice the work.
-// Not for the largest layers, where that is the most of the time: 32768 x 1024 -> 4096 1145 us without, 1721 with it
-// (8192 x 1024 -> 1024 128 and 165).
-bool keeps_low(const Args &a) {
-  return a.act && a.esz == 2 && (a.outs < 512 || (double)a.rows * a.cols * a.outs < (double)(1ull << 35));
-}
+// what the rounding leaves goes through the products as a second part of G, which makes that of dx and dweight twice the work:
+// 32768 x 1024 -> 4096 1145 us without, 1721 with it (8192 x 1024 -> 1024 128 and 165).
+bool in_parts(const Args &a) { return a.act && a.esz == 2; }
 // Few rows go to kernels of their own rather than to tiles of 128 rows that are mostly empty.  Forward, us against tiles: single
 // precision 1, 16 rows of 1024 -> 4096 4.8, 19.4 against 23; bf16 1, 4, 8, 16 rows 4.1, 4.9, 8.8, 14.5 against 8.  Forward and
 // backward with GELU, 16 rows: 1024 -> 4096 single 62 against 98, bf16 53 against 61; 64 -> 256 single 23 against 31, but bf16 24
@@ -93,7 +90,7 @@ Scratch carve(const Args &a, void *base) {
     return s;
   }
   s.g = take(a.act ? (size_t)a.rows * s.ld_g * a.esz : 0);
-  s.g_low = keeps_low(a) ? take((size_t)a.rows * s.ld_g * a.esz) : nullptr;
+  s.g_low = in_parts(a) ? take((size_t)a.rows * s.ld_g * a.esz) : nullptr;
   s.x = take(a.packed ? (size_t)a.rows * s.ld_x * a.esz : 0);
   if (a.esz == 2) {
     s.splits = tc_splits(a.outs, a.cols, a.rows ? a.rows : 1);
