@@ -284,8 +284,8 @@ def blossom_linear(x, weight, bias=None, residual=None, activation="none", packe
     """``act(x W^T + bias) + residual`` in one pass for x [..., K] and weight [N, K] as ``nn.Linear`` has it (float32 or
     bfloat16, CUDA, all of one type; K and N up to 65536): [..., N], differentiable in x, weight, bias and residual.
 
-    bias: [N] or None.  residual: [..., N] or None.  activation: "none", "relu", "gelu" (with the error function) or "silu";
-    its argument is not kept, the backward forms it again from x.
+    bias: [N] or None.  residual: [..., N] or None.  activation: "none", "relu", "gelu" (x Phi(x), the one with the error
+    function, to single precision, of bf16 results to 2^-10) or "silu"; its argument is not kept, the backward forms it again from x.
     packed: keep x for the backward in 8 bits, a power of two per 32 columns (33/32 bytes an element; K up to 8192): the
     weight's gradient and the activation's argument in the backward are those of the rounded x.  The output is not
     affected, nor is the gradient of x without an activation.

@@ -26,12 +26,14 @@ __device__ __forceinline__ float2 at_least(float2 x, float least) { return make_
 __device__ __forceinline__ float2 at_most(float2 x, float most) { return make_float2(at_most(x.x, most), at_most(x.y, most)); }
 // Two arguments at a time.
 // Phi(x) = sigmoid(x P(x^2)), P a polynomial fitted to the logit of Phi (weighted least squares, the weights moved towards the
-// largest errors): with five terms x Phi(x) is off by 4e-6 at most; with four, whose derivative serves for that of the whole,
-// the derivative is off by 4.4e-5, where a rounding to bf16 is off by 2e-3 of the value; with seven, for results in single
-// precision, by 8e-8 and 4e-7.  An exponential an element and a
-// reciprocal for two: the unit for those, 16 a clock and SM, bounds the value (131072 x 256 elements 11 us), the FMA pipes
-// the derivative; with the error function it is these pipes, four times as long.  From |x| = 6 on the
-// derivative is 0 or 1 to 1e-7, from x = -6 down the value is 0 to 1e-8: arguments are cut there, so that
+// largest errors).  For bf16 results P has nine terms: x Phi(x) is off by 9e-4 of itself at most, from x = -6 on, a quarter of
+// their half step; else seven, off by 7e-8, for whom a relative error would be asking for more than their argument is known to.
+// The derivative is Phi(x) + x phi(x), Phi off by 5e-8.  (Five terms of the value are off by 4e-6, 2.6 % of it at x = -4, and four
+// of a logit that serves for the derivative's polynomial as well by 4.4e-5: 131072 x 64 -> 256, forward and backward, 91 us, with
+// these terms 96; 99 with seven terms and the derivative of their polynomial.)
+// An exponential and half a reciprocal an element (and an exponential for phi), which the unit for those gives 16 a clock
+// and SM: 131072 x 256 elements 11 us, and 18; with the error function it is the FMA pipes, four times as long.  From |x| = 6 on the
+// derivative is 0 or 1 to 4e-8, from x = -6 down the value is 0 to 6e-9: arguments are cut there, so that
 // no product of two exponentials overflows.
 constexpr float kLog2e = 1.4426950408889634f;
 __device__ __forceinline__ float2 mul2f(float2 a, float2 b) {
@@ -57,28 +59,37 @@ template <int ACT, bool SLOPE, bool WIDE = false>
 struct Curve {
   static constexpr bool kGelu = ACT == BLOSSOM_ACT_GELU, kSilu = ACT == BLOSSOM_ACT_SILU;
   static constexpr float kCut = kGelu ? 6.f : 40.f;  // (silu: from x = -40 down 0 to 2e-16)
-  static constexpr int kTerms = kGelu ? (WIDE ? 7 : SLOPE ? 4 : 5) : 1;
-  float2 p[kTerms], d[kTerms], one, minus;
-  __device__ __forceinline__ Curve() {
+  static constexpr bool kFar = kGelu && !SLOPE && !WIDE;  // nine terms
+  // (the lowest terms are held; the others, which would not fit the registers, are one-element instructions' own)
+  static constexpr int kTerms = kFar ? 9 : 7, kHeld = kGelu ? 5 : 1;
+  float2 p[kHeld], half, top, one, minus;
+  // Of P: the terms of a short fit and what those of the long one have besides.
+  static __device__ constexpr float term(int i) {
     constexpr float value[5] = {1.5957043f, 0.072862640f, -0.00021803212f, -6.5811037e-05f, 2.4471922e-06f};
+    constexpr float value_rest[9] = {6.89029694e-05f, -0.00020750612f, 0.000163902325f, -4.95181739e-05f, 6.45735508e-06f,
+                                     -3.66156229e-07f, 8.67401528e-09f, -1.09854764e-10f, 5.69511343e-13f};
     constexpr float both[4] = {1.5954539f, 0.073342353f, -0.00046575911f, -2.1383154e-05f};
-    constexpr float wide[7] = {1.59576964f, 0.0726662353f, -6.48020578e-05f, -0.000110872024f, 7.98777546e-06f, -2.69765849e-07f, 3.67201225e-09f};
+    constexpr float both_rest[7] = {0.000315785408f, -0.000676117837f, 0.00040095704f, -8.94888726e-05f, 7.98777546e-06f,
+                                    -2.69765849e-07f, 3.67201225e-09f};
+    return kFar ? (i < 5 ? value[i % 5] : 0.f) + value_rest[i] : (i < 4 ? both[i % 4] : 0.f) + both_rest[i % 7];
+  }
+  __device__ __forceinline__ Curve() {
     if constexpr (kGelu) {
 #pragma unroll
-      for (int i = 0; i < kTerms; ++i) p[i] = held(-kLog2e * (WIDE ? wide[i] : SLOPE ? both[i % 4] : value[i % 5]));
+      for (int i = 0; i < kHeld; ++i) p[i] = held(-kLog2e * term(i));
     }
-    if constexpr (kGelu && SLOPE) {
-#pragma unroll
-      for (int i = 0; i < kTerms; ++i) d[i] = held((2.f * i + 1.f) * (WIDE ? wide[i] : both[i % 4]));
-    }
+    if constexpr (kGelu && SLOPE) half = held(-0.5f * kLog2e), top = held(0.3989422804014327f);
     if constexpr (kSilu) p[0] = held(-kLog2e);
     if constexpr (kGelu || kSilu) one = held(1.f);
-    if constexpr ((kGelu || kSilu) && SLOPE) minus = held(-1.f);
+    if constexpr (kSilu && SLOPE) minus = held(-1.f);
   }
-  static __device__ __forceinline__ float2 horner(const float2 (&c)[kTerms], float2 t) {
-    float2 s = c[kTerms - 1];
+  // -log2(e) P(t)
+  __device__ __forceinline__ float2 scaled_p(float2 t) const {
+    float2 s = make_float2(-kLog2e * term(kTerms - 1), -kLog2e * term(kTerms - 1));
 #pragma unroll
-    for (int i = kTerms - 2; i >= 0; --i) s = fma2(s, t, c[i]);
+    for (int i = kTerms - 2; i >= kHeld; --i) s = make_float2(fmaf(s.x, t.x, -kLog2e * term(i)), fmaf(s.y, t.y, -kLog2e * term(i)));
+#pragma unroll
+    for (int i = kHeld - 1; i >= 0; --i) s = fma2(s, t, p[i]);
     return s;
   }
   // 1 / (1 + 2^v) of two exponents of at most 60
@@ -99,13 +110,15 @@ struct Curve {
       float2 t = x, u = p[0];
       if constexpr (kGelu) {
         t = mul2f(x, x);
-        u = horner(p, t);
+        u = scaled_p(t);
       }
       const float2 s = sigmoid2(mul2f(x, u));
       if constexpr (!SLOPE) return mul2f(x, s);
-      float2 w = mul2f(x, fma2(s, minus, one));
-      if constexpr (kGelu && SLOPE) w = mul2f(w, horner(d, t));
-      return mul2f(s, add2(w, one));
+      if constexpr (kGelu) {  // Phi + x phi
+        const float2 v = mul2f(t, half);
+        return fma2(mul2f(x, top), make_float2(exp2f(v.x), exp2f(v.y)), s);
+      }
+      return mul2f(s, add2(mul2f(x, fma2(s, minus, one)), one));
     }
     return x;
   }

@@ -108,7 +108,7 @@ __global__ void __launch_bounds__(kThreads) few_rows_kernel(int rows, int cols, 
     if (bias) y += load1(bias + c);
     const float e = extra ? load1(extra + (int64_t)r * ld_extra + c) : 0.f;
     with_curve(act, SLOPE, extra != nullptr, [&](auto a, auto slope, auto) {
-      const Curve<decltype(a)::value, decltype(slope)::value, true> curve;
+      const Curve<decltype(a)::value, decltype(slope)::value, sizeof(T) == 4> curve;
       y = curve(make_float2(y, 0.f)).x;
     });
     if (SLOPE) static_cast<float *>(out)[(int64_t)r * ld_out + c] = y * e;
