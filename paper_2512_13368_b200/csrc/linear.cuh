@@ -31,10 +31,12 @@ __device__ __forceinline__ float2 at_most(float2 x, float most) { return make_fl
 // The derivative is Phi(x) + x phi(x), Phi off by 5e-8.  (Five terms of the value are off by 4e-6, 2.6 % of it at x = -4, and four
 // of a logit that serves for the derivative's polynomial as well by 4.4e-5: 131072 x 64 -> 256, forward and backward, 91 us, with
 // these terms 96; 99 with seven terms and the derivative of their polynomial.)
-// An exponential and half a reciprocal an element (and an exponential for phi), which the unit for those gives 16 a clock
-// and SM: 131072 x 256 elements 11 us, and 18; with the error function it is the FMA pipes, four times as long.  From |x| = 6 on the
+// An exponential and a reciprocal an element (and an exponential for phi), which the unit for those gives 16 a clock and SM:
+// 131072 x 256 elements 15 us, and 22; with the error function it is the FMA pipes, three times as long.  (One reciprocal for two
+// elements makes both of them no number if one is, and keeps an element's bits from depending on itself alone; without that, by
+// a minimum that takes what is no number for 60, 131072 x 64 -> 256 takes 98 us instead of 95.)  From |x| = 6 on the
 // derivative is 0 or 1 to 4e-8, from x = -6 down the value is 0 to 6e-9: arguments are cut there, so that
-// no product of two exponentials overflows.
+// infinite ones have their limits.
 constexpr float kLog2e = 1.4426950408889634f;
 __device__ __forceinline__ float2 mul2f(float2 a, float2 b) {
   uint64_t d;
@@ -92,11 +94,10 @@ struct Curve {
     for (int i = kHeld - 1; i >= 0; --i) s = fma2(s, t, p[i]);
     return s;
   }
-  // 1 / (1 + 2^v) of two exponents of at most 60
+  // 1 / (1 + 2^v)
   __device__ __forceinline__ float2 sigmoid2(float2 v) const {
     const float2 y = add2(make_float2(exp2f(v.x), exp2f(v.y)), one);
-    const float r = reciprocal(y.x * y.y);
-    return make_float2(r * y.y, r * y.x);
+    return make_float2(reciprocal(y.x), reciprocal(y.y));
   }
   __device__ __forceinline__ float2 operator()(float2 x) const {
     if constexpr (ACT == BLOSSOM_ACT_NONE) return x;
