@@ -44,11 +44,20 @@ __device__ __forceinline__ uint32_t top_of_four(const Raw<T, W> &v, uint32_t fou
   top = larger(top, __shfl_xor_sync(four, top, 2));
   return sizeof(T) == 4 ? top : max(top & 0xffff0000u, top << 16);
 }
+// x * f + c of subnormal x too, which this build's arithmetic would take for zeros: beside a largest magnitude below 2^-119 they
+// have codes of 1
+__device__ __forceinline__ float2 fma2_of_all(float2 x, float2 f, float2 c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;"
+      : "=l"(d)
+      : "l"(*reinterpret_cast<uint64_t *>(&x)), "l"(*reinterpret_cast<uint64_t *>(&f)), "l"(*reinterpret_cast<uint64_t *>(&c)));
+  return *reinterpret_cast<float2 *>(&d);
+}
 // 8 values' codes, f a value.  1.5 * 2^23 rounds a sum to whole numbers and leaves them in the lowest bits; the product is exact.
 __device__ __forceinline__ void codes_of(Group z, float f, uint32_t top, uint32_t (&c)[2]) {
   constexpr float magic = 12582912.f;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) z.p[i] = fma2(z.p[i], both(f), both(magic));
+  for (int i = 0; i < 4; ++i) z.p[i] = fma2_of_all(z.p[i], both(f), both(magic));
   if ((top & 0x7fffffu) >= 0x7f0000u) {  // of 127.5 and more there are 128s
 #pragma unroll
     for (int j = 0; j < 8; ++j) z.at(j) = fminf(fmaxf(z.at(j), magic - 127.f), magic + 127.f);
