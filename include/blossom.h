@@ -390,9 +390,9 @@ size_t blossom_embedding_workspace_bytes(const blossom_embedding_params *params 
  * backward, at 33 / 32 bytes an element.  Of every 32 columns of a row, from column 0 on (the last ones may be fewer), E is the
  * biased exponent of the largest magnitude (bits 23 .. 30 of it in single precision), kept as one byte;
  * an element x is kept as the integer round(x * 2^(133 - E)), to nearest and halves to even, but no further from 0 than 127, and
- * stands for that integer times 2^(E - 133): off by 2^-8 of the largest magnitude at most (next to
- * the limit of 127: by 2^-7).  E <= 6 (all below 2^-120): all stand for zeros.  E = 255 (an infinity or what is no
- * number among them): all stand for what is no number.  The values are exact in either type.
+ * stands for that integer times 2^(E - 133): off by 2^(E - 134) at most, next to the limit of 127 by twice that, and so by
+ * 2^-7 of the largest magnitude at most.  E <= 6 (all below 2^-120): all stand for zeros.  E = 255 (an infinity or what is
+ * no number among them): all stand for what is no number.  The values are exact in either type.
  *   codes    int8 [rows][cols], any alignment
  *   scales   uint8 [rows][ceil(cols / 32)]
  * params: rows, cols, dtype and x_stride (pack) or out_stride (unpack); the rest is checked, but not used.

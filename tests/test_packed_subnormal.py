@@ -1,4 +1,4 @@
-"""Rows in 8 bits whose elements are subnormal beside a largest one that is not: codes of 1, not zeros."""
+"""Rows in 8 bits at their limits: elements that are subnormal beside a largest one that is not, and how far values may be off."""
 import numpy as np
 import pytest
 
@@ -30,3 +30,17 @@ def test_subnormal_elements(cols, dtype):
     out = torch.empty_like(x)
     binding.blossom_unpack_rows(p, codes, scales, out)
     assert np.array_equal(out.double().cpu().numpy(), lo.unpack(want_codes, want_scales))
+
+
+def test_how_far_a_value_may_be_off():
+    """2^-7 of a group's largest magnitude and no less: half a unit where that begins with 1, a unit at the limit of 127."""
+    x = np.full((2, 32), 0.0, dtype=np.float32)
+    x[0, :2] = 1.0, 0.9999 * 2.0 ** -7     # (half a unit is 2^-7: zero)
+    x[1, :2] = 1.9999, 1.0                 # 127.99 units
+    off = np.abs(lo.unpack(*lo.pack(x)) - x)
+    assert off[0, 1] > 0.99 * 2.0 ** -7 and off[1, 0] > 0.99 * 2.0 ** -7 * x[1, 0]
+    g = np.random.default_rng(0)
+    x = (g.standard_normal((2000, 64)) * np.exp2(g.integers(-100, 100, (2000, 1)))).astype(np.float32)
+    off, top = np.abs(lo.unpack(*lo.pack(x)) - x), np.abs(x)
+    for c in (0, 32):
+        assert (off[:, c:c + 32] <= 2.0 ** -7 * top[:, c:c + 32].max(axis=1, keepdims=True)).all()
