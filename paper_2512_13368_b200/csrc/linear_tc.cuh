@@ -165,6 +165,12 @@ __device__ __forceinline__ uint4 finish8(const C &curve, const float *y, const f
                     finish2<READ>(curve, make_float2(y[4], y[5]), make_float2(b1.x, b1.y), e.z),
                     finish2<READ>(curve, make_float2(y[6], y[7]), make_float2(b1.z, b1.w), e.w));
 }
+// No further from 0 than 2^120, which no remainder is; what is no number (an infinity's remainder) counts as that as well.
+__device__ __forceinline__ uint32_t remainders(uint32_t two) {
+  uint32_t r;
+  asm("{\n\t.reg .b32 t;\n\tmin.bf16x2 t, %1, %2;\n\tmax.bf16x2 %0, t, %3;\n\t}" : "=r"(r) : "r"(two), "r"(0x7b807b80u), "r"(0xfb80fb80u));
+  return r;
+}
 // 8 columns of dout o act'(v + bias) as a sum of two bf16: the first is returned, `low` is what it leaves
 template <typename C>
 __device__ __forceinline__ uint4 finish8_parts(const C &curve, const float *y, const float *bias, uint4 read, uint4 &low) {
@@ -176,7 +182,7 @@ __device__ __forceinline__ uint4 finish8_parts(const C &curve, const float *y, c
     const float2 g = mul2f(curve(add2(make_float2(y[2 * i], y[2 * i + 1]), b)), rows::halves(d[i]));
     h[i] = tc::pack_bf16(g.x, g.y);
     const float2 f = rows::halves(h[i]);
-    l[i] = tc::pack_bf16(g.x - f.x, g.y - f.y);
+    l[i] = remainders(tc::pack_bf16(g.x - f.x, g.y - f.y));
   }
   low = make_uint4(l[0], l[1], l[2], l[3]);
   return make_uint4(h[0], h[1], h[2], h[3]);

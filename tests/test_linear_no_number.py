@@ -72,3 +72,33 @@ def test_an_infinite_row_has_the_limits(rows, cols, outs, act):
     want = (dout[1].double() * up) @ w.double()
     size = dout[1].double().abs() @ w.double().abs()
     assert bool(((got["dx"][1].double() - want).abs() <= 2.0 ** -8 * want.abs() + (outs + 64) * 2.0 ** -23 * size + 1e-6 * size).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("act", ["none", "gelu", "silu"])
+@pytest.mark.parametrize("rows,cols,outs", SHAPES)
+def test_an_infinite_upstream_gradient(rows, cols, outs, act):
+    """bf16: one infinite element makes its row of dx, its row of dweight and its dbias infinite, of the signs of the terms, and
+    nothing else."""
+    import torch
+    x, w, b, dout = tensors(rows, cols, outs, "bf16")
+    x, w = (torch.where(t == 0, torch.ones_like(t), t) for t in (x, w))
+    clean = step(x, w, b, dout, act)
+    for n, big in ((0, float("inf")), (outs // 2 + 1, float("-inf")), (outs - 1, 3.3895e38)):
+        d = dout.clone()
+        d[1, n] = big
+        got = step(x, w, b, d, act)
+        p = x[1].double() @ w[n].double() + b[n].double()
+        s = torch.sigmoid(p)
+        slope = {"none": 1.0, "silu": float(s * (1 + p * (1 - s))),
+                 "gelu": float(0.5 * torch.special.erfc(-p / 2 ** 0.5) + p * torch.exp(-p * p / 2) * 0.3989422804)}[act]
+        assert abs(slope) > 1e-3
+        others, rest = torch.arange(outs, device="cuda") != n, torch.arange(rows, device="cuda") != 1
+        assert torch.equal(got["dw"][others], clean["dw"][others]) and torch.equal(got["db"][others], clean["db"][others])
+        assert torch.equal(got["dx"][rest], clean["dx"][rest])
+        if big == big + 1 and abs(big) > 3.4e38:
+            sign = slope * big
+            assert torch.equal(got["db"][n].float(), torch.tensor(sign, device="cuda"))
+            assert torch.equal(got["dw"][n].float(), sign * x[1].float()) and torch.equal(got["dx"][1].float(), sign * w[n].float())
+        else:   # the largest bf16: products with it may pass the largest number, but none is no number
+            assert not bool(got["db"][n].isnan()) and not bool(got["dw"][n].isnan().any()) and not bool(got["dx"][1].isnan().any())
