@@ -48,18 +48,19 @@ struct Scratch {
 // Between the products G is bf16.  Rounded to one its error is as large as the results' own rounding (together 1.4 times that), so
 // what the rounding leaves goes through the products as a second part of G, which makes that of dx and dweight twice the work:
 // 32768 x 1024 -> 4096 1145 us without, 1721 with it (8192 x 1024 -> 1024 128 and 165).
-bool in_parts(const Args &a) { return a.act && a.esz == 2; }
+int parts(const Args &a) { return a.act && a.esz == 2 ? 2 : 1; }
 // Few rows go to kernels of their own rather than to tiles of 128 rows that are mostly empty.  Forward, us against tiles: single
 // precision 1, 16 rows of 1024 -> 4096 4.8, 19.4 against 23; bf16 1, 4, 8, 16 rows 4.1, 4.9, 8.8, 14.5 against 8.  Forward and
 // backward with GELU, 16 rows: 1024 -> 4096 single 62 against 98, bf16 53 against 61; 64 -> 256 single 23 against 31, but bf16 24
 // against 21 (4 rows 15), where the narrow layers' kernel is.
 bool few_forward(const Args &a) { return a.rows <= (a.esz == 4 ? kFewRows : 4); }
 bool few_backward(const Args &a) { return a.rows <= 4 || (a.rows <= kFewRows && (a.esz == 4 || a.cols > 256 || a.outs > 256)); }
-// Rows that the kernel for narrow layers takes at a time, as many as its accumulators may add up.
-constexpr int64_t kNarrowRows = (int64_t)kSMs * kMostSlabs * 64;
-NarrowBackward from_row(const NarrowBackward &n, int64_t row) {
+// Rows that the kernel for narrow layers takes at a time, as many as its accumulators may add up; those from `row` on.
+int64_t narrow_rows(const Args &a) { return (int64_t)kSMs * kMostSlabs * 64 / parts(a); }
+int narrow_rows(const Args &a, int64_t row) { return (int)(a.rows - row < narrow_rows(a) ? a.rows - row : narrow_rows(a)); }
+NarrowBackward from_row(const Args &a, const NarrowBackward &n, int64_t row) {
   NarrowBackward m = n;
-  m.rows = (int)(n.rows - row < kNarrowRows ? n.rows - row : kNarrowRows);
+  m.rows = narrow_rows(a, row);
   auto on = [&](const void *p, int64_t bytes) { return p ? static_cast<const char *>(p) + row * bytes : nullptr; };
   m.x = on(n.x, n.ld_x * 2), m.dout = on(n.dout, n.ld_dout * 2);
   m.dx = const_cast<char *>(on(n.dx, n.ld_dx * 2));
@@ -90,27 +91,29 @@ Scratch carve(const Args &a, void *base) {
     return s;
   }
   s.g = take(a.act ? (size_t)a.rows * s.ld_g * a.esz : 0);
-  s.g_low = in_parts(a) ? take((size_t)a.rows * s.ld_g * a.esz) : nullptr;
+  s.g_low = parts(a) == 2 ? take((size_t)a.rows * s.ld_g * a.esz) : nullptr;
   s.x = take(a.packed ? (size_t)a.rows * s.ld_x * a.esz : 0);
   if (a.esz == 2) {
-    s.splits = tc_splits(a.outs, a.cols, a.rows ? a.rows : 1);
-    s.bias_parts = tc_bias_parts(a.outs, a.cols, a.rows ? a.rows : 1);
+    s.splits = tc_splits(a.outs, a.cols, a.rows ? a.rows : 1, parts(a));
+    s.bias_parts = tc_bias_parts(a.outs, a.cols, a.rows ? a.rows : 1, parts(a));
   } else {
     s.splits = s.bias_parts = f32_splits(a.outs, a.cols, a.rows ? a.rows : 1);
   }
   s.narrow = 0;
   if (a.esz == 2 && a.outs <= 256 && a.cols <= 256)
-    for (int64_t r = 0; r < a.rows; r += kNarrowRows) s.narrow += narrow_splits((int)(a.rows - r < kNarrowRows ? a.rows - r : kNarrowRows));
+    for (int64_t r = 0; r < a.rows; r += narrow_rows(a)) s.narrow += narrow_splits(narrow_rows(a, r));
   // dx of few tiles (all of a row's columns in one) over many outs leaves SMs idle: its sums are split as well (forward and backward in
   // single precision, us with splits and with a cluster a tile: 64 x 64 -> 1000 17.8, 23.0, 600 x 64 -> 1000 24.6, 31.5, but
-  // 200 x 1000 -> 1000 37.8, 33.9)
+  // 200 x 1000 -> 1000 37.8, 33.9).  So is dx over more outs than an accumulator adds up.
   s.dx_splits = 1;
-  if ((int64_t)parts_of(a.rows, 128) * parts_of(a.cols, 128) < kSMs && a.outs >= 256 && a.rows)
-    s.dx_splits = a.esz == 2 ? tc_splits(a.rows, a.cols, a.outs) : f32_splits(a.rows, a.cols, a.outs);
+  const bool few_tiles = (int64_t)parts_of(a.rows, 128) * parts_of(a.cols, 128) < kSMs && a.outs >= 256,
+             long_sums = a.esz == 2 && (int64_t)a.outs * parts(a) > kMostSlabs * 64;
+  if ((few_tiles || long_sums) && a.rows)
+    s.dx_splits = a.esz == 2 ? tc_splits(a.rows, a.cols, a.outs, parts(a)) : f32_splits(a.rows, a.cols, a.outs);
   // (one split's sums go where they belong; the narrow layers' kernel leaves its own in any case)
-  const size_t parts = s.narrow || s.splits > 1 ? s.splits > s.narrow ? s.splits : s.narrow : 0;
+  const size_t sets = s.narrow || s.splits > 1 ? s.splits > s.narrow ? s.splits : s.narrow : 0;
   const size_t sums = s.bias_parts > s.narrow ? s.bias_parts : s.narrow;
-  const size_t weight = parts * a.outs * (size_t)a.cols, dx = s.dx_splits > 1 ? (size_t)s.dx_splits * a.rows * a.cols : 0;
+  const size_t weight = sets * a.outs * (size_t)a.cols, dx = s.dx_splits > 1 ? (size_t)s.dx_splits * a.rows * a.cols : 0;
   s.part = reinterpret_cast<float *>(take((weight > dx ? weight : dx) * sizeof(float)));
   s.part_bias = reinterpret_cast<float *>(take(sums * a.outs * sizeof(float)));
   s.bytes = off;
@@ -206,8 +209,8 @@ extern "C" int blossom_linear_bwd(const blossom_linear_params *params, const voi
                                        a.act ? nullptr : s.status, st);
   }
   if (in_place || (s.narrow && linear::narrow_takes(n))) {
-    for (int64_t r = 0; r < a.rows; r += linear::kNarrowRows) {
-      linear::NarrowBackward m = linear::from_row(n, r);
+    for (int64_t r = 0; r < a.rows; r += linear::narrow_rows(a)) {
+      linear::NarrowBackward m = linear::from_row(a, n, r);
       if (int rc = linear::launch_narrow(m, st)) return rc;
       const int64_t splits = linear::narrow_splits(m.rows);
       if (n.part) n.part += splits * a.outs * a.cols;

@@ -181,9 +181,9 @@ int launch_tc(int kernel_id, Mode mode, const Operand &a, const Operand &b, int 
 int launch_f32(int kernel_id, Mode mode, const Operand &a, const Operand &b, int m, int n, int k, const Epilogue &e, int32_t *status,
                cudaStream_t st);
 int f32_splits(int m, int n, int k);
-// Into how many parts the contraction over the rows is split.
-int tc_splits(int m, int n, int k);
-int tc_bias_parts(int m, int n, int k);  // and the sums over k alone
+// Into how many splits k goes; parts: of A.
+int tc_splits(int m, int n, int k, int parts);
+int tc_bias_parts(int m, int n, int k, int parts);  // and the sums over k alone
 // Few rows.
 constexpr int kFewRows = 16;
 struct FewRows {

@@ -413,12 +413,13 @@ int tile_columns(int m, int n, int splits, bool ends) {
   return best;
 }
 
-int tc_splits(int m, int n, int k) {
+int tc_splits(int m, int n, int k, int parts) {
   // In clocks: a slab of a tile 1.6 a column and 100, an item's hand-offs and epilogue 4000, a partial sum's way to memory and
   // back 8 bytes at 3500 a clock.  Forward and backward, us with 1, 4, 9, 16, 37 splits: 5000 x 512 -> 512 45, 32, 31, 31, 45 (the rule:
   // 32); 2000 x 1024 -> 1024 with GELU 60, 81, 100, 155, 214 (60).
-  // No accumulator adds up more than kMostSlabs: it cuts its sums, which loses 2e-6 of sums of one sign over 1024 steps of k.
-  const int64_t slabs = parts_of(k, kK), mt = parts_of(m, kM), fewest = parts_of((int)slabs, kMostSlabs);
+  // No accumulator adds up more than kMostSlabs, those of both parts of A: it cuts its sums, which loses 2e-6 of sums of one sign
+  // over 1024 steps of k.
+  const int64_t slabs = parts_of(k, kK), mt = parts_of(m, kM), fewest = parts_of((int)slabs, kMostSlabs / parts);
   int best = 1;
   double least = 1e30;
   for (int bn : {64, 128, 192, 256}) {
@@ -436,8 +437,8 @@ int tc_splits(int m, int n, int k) {
   return best;
 }
 
-int tc_bias_parts(int m, int n, int k) {
-  const int splits = tc_splits(m, n, k), bn = tile_columns(m, n, splits, false);
+int tc_bias_parts(int m, int n, int k, int parts) {
+  const int splits = tc_splits(m, n, k, parts), bn = tile_columns(m, n, splits, false);
   return splits * ((n + bn - 1) / bn);
 }
 

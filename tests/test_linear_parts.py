@@ -106,3 +106,71 @@ def test_gradients_of_large_layers(rows, cols, outs, act):
     for got, want, size, slack in ((dw[some], G.t() @ x, (G.abs() + off).t() @ x.abs(), off.t() @ x.abs()),
                                    (db[some], G.sum(0), (G.abs() + off).sum(0), off.sum(0))):
         good(got, want, BF16 * want.abs() + slack + (rows + 4) * 2 * F32 * size, "dweight or dbias")
+
+
+def size(*a):
+    return binding.blossom_linear_workspace_bytes(binding.make_linear_params(*a))
+
+
+def test_how_many_steps_an_accumulator_adds_up():
+    """65536 steps of k, those of both parts of the upstream gradient behind an activation: seen by the partial sums that the
+    workspace has room for, beside the upstream gradient's parts."""
+    binding.load()
+    tiles = 4096 * 4096 * 4
+    assert size(65536, 4096, 4096, "bf16", "none") < tiles
+    assert size(32768, 4096, 4096, "bf16", "gelu") < 2 * 32768 * 4096 * 2 + tiles
+    for rows, act, parts, splits in ((140000, "none", 0, 3), (70000, "gelu", 2, 3), (300000, "silu", 2, 10)):
+        assert size(rows, 4096, 4096, "bf16", act) >= parts * rows * 4096 * 2 + splits * tiles, (rows, act)
+    # the narrow layers' kernel: 148 blocks at a time
+    block = 256 * 256 * 4
+    for rows, act, splits in ((148 * 65536, "none", 148), (148 * 32768, "gelu", 148), (148 * 65536, "gelu", 2 * 148)):
+        assert size(rows, 256, 256, "bf16", act) >= splits * block, (rows, act)
+    # dx over very many outs
+    rows = 40000
+    assert size(rows, 64, 60000, "bf16", "gelu") >= 2 * rows * 60000 * 2 + 2 * rows * 64 * 4
+    assert size(rows, 64, 30000, "bf16", "gelu") < 2 * rows * 30000 * 2 + 2 * rows * 64 * 4
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,cols,outs", [(4849664 * 2 + 777, 16, 8), (4849664 + 129, 32, 24), (140000, 520, 264), (20000, 48, 40000)])
+def test_long_sums_behind_an_activation(rows, cols, outs):
+    """Of one sign.  An accumulator's 65536 steps by 16 at a time are off by 2^-23 each, and so are the terms; two parts of the
+    upstream gradient leave 2^-16 of it, its slope is off by 2^-20."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(0)
+
+    def t(*s):
+        return (torch.rand(*s, generator=g, device="cuda") + 0.5).bfloat16()
+
+    x, w, dout = t(rows, cols), t(outs, cols), t(rows, outs)
+    b = torch.full((outs,), -0.9 * cols, device="cuda").bfloat16()
+    dx, dw, db = backward(x, w, b, dout, "silu")
+
+    def behind(rows_):
+        p = x[rows_].double() @ w.double().t() + b.double()
+        s = torch.sigmoid(p)
+        return dout[rows_].double() * (s * (1 + p * (1 - s))), p
+
+    want_w = torch.zeros(outs, cols, dtype=torch.float64, device="cuda")
+    want_b = torch.zeros(outs, dtype=torch.float64, device="cuda")
+    size_w, size_b = want_w.clone(), want_b.clone()
+    for r0 in range(0, rows, 1 << (27 - max(outs, 64).bit_length())):
+        part = slice(r0, r0 + (1 << (27 - max(outs, 64).bit_length())))
+        G, _ = behind(part)
+        want_w += G.t() @ x[part].double()
+        want_b += G.sum(0)
+        size_w += G.abs().t() @ x[part].double()
+        size_b += G.abs().sum(0)
+    steps = (65536 / 16 + 64) * 2.0 ** -23 + 2.0 ** -16 + 2.0 ** -20
+    # (the argument, a sum over cols of numbers of up to 2.25, is off by 2^-23 a step of its magnitudes, its slope by as much)
+    argument = 0.5 * (cols + 4) * 2.0 ** -23 * 3.2 * cols
+    for got, want, mag in ((dw, want_w, size_w), (db, want_b, size_b)):
+        off = (got.double() - want).abs()
+        tol = half_step(want) + steps * mag + argument * mag.max() * 2
+        assert bool((off <= 1.01 * tol).all()), float((off / tol).max())
+    at = torch.tensor([0, 1, rows // 2, rows - 1], device="cuda")
+    G, _ = behind(at)
+    want, mag = G @ w.double(), G.abs() @ w.double()
+    off = (dx[at].double() - want).abs()
+    tol = half_step(want) + steps * mag + argument * (dout[at].double() @ w.double())
+    assert bool((off <= 1.01 * tol).all()), float((off / tol).max())
