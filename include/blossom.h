@@ -427,11 +427,15 @@ typedef struct {
   int64_t dx_stride, dweight_stride; /* 0 = cols                                                          */
 } blossom_linear_params;
 
-/* One size serves both calls, of which the forward uses the first BLOSSOM_LINEAR_FORWARD_BYTES and asks for no more; 0 for
+/* blossom_linear_workspace_bytes serves both calls, of which the forward uses the first BLOSSOM_LINEAR_FORWARD_BYTES and asks for
+ * no more.  A backward whose tensors are at hand may need much less: _bwd_workspace_bytes says how much for tensors that lie where x,
+ * weight and dout do (of which only the alignment counts; x: its codes with params.packed, or NULL if it is not read).  Both are 0 for
  * invalid or unsupported params.  256-byte aligned; carries nothing from call to call but the status words that
  * blossom_device_status reads, which each call clears. */
 #define BLOSSOM_LINEAR_FORWARD_BYTES 256
 size_t blossom_linear_workspace_bytes(const blossom_linear_params *params /* host */);
+size_t blossom_linear_bwd_workspace_bytes(const blossom_linear_params *params /* host */, const void *x, const void *weight,
+                                          const void *dout);
 
 /*   bias      in   [outs] or NULL
  *   residual  in   [rows][outs] or NULL; out may be residual itself (with the same stride) */

@@ -34,7 +34,7 @@ EXPORTS = (
     "blossom_sampled_loss_fwd", "blossom_sampled_loss_bwd", "blossom_sampled_loss_workspace_bytes",
     "blossom_embedding_fwd", "blossom_embedding_bwd", "blossom_embedding_workspace_bytes",
     "blossom_pack_rows", "blossom_unpack_rows",
-    "blossom_linear_fwd", "blossom_linear_bwd", "blossom_linear_workspace_bytes",
+    "blossom_linear_fwd", "blossom_linear_bwd", "blossom_linear_workspace_bytes", "blossom_linear_bwd_workspace_bytes",
 )
 LOSS_FORWARD_BYTES = 65536  # what blossom_sampled_loss_fwd uses of its workspace
 LINEAR_FORWARD_BYTES = 256  # the same of blossom_linear_fwd
@@ -176,6 +176,8 @@ def load():
     np_ = ctypes.POINTER(blossom_linear_params)
     lib.blossom_linear_workspace_bytes.restype = sz
     lib.blossom_linear_workspace_bytes.argtypes = [np_]
+    lib.blossom_linear_bwd_workspace_bytes.restype = sz
+    lib.blossom_linear_bwd_workspace_bytes.argtypes = [np_] + [vp] * 3
     lib.blossom_linear_fwd.restype = ctypes.c_int
     lib.blossom_linear_fwd.argtypes = [np_] + [vp] * 6 + [sz, vp]
     lib.blossom_linear_bwd.restype = ctypes.c_int
@@ -438,6 +440,11 @@ def make_linear_params(rows, cols, outs, dtype, activation="none", packed=False,
 
 def blossom_linear_workspace_bytes(params) -> int:
     return int(load().blossom_linear_workspace_bytes(ctypes.byref(params)))
+
+
+def blossom_linear_bwd_workspace_bytes(params, x, weight, dout) -> int:
+    """What the backward needs for tensors that lie where these do."""
+    return int(load().blossom_linear_bwd_workspace_bytes(ctypes.byref(params), _ptr(x), _ptr(weight), _ptr(dout)))
 
 
 def blossom_linear_fwd(params, x, weight, bias, residual, out, workspace, workspace_bytes=None, stream=None,

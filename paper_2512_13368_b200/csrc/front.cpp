@@ -906,8 +906,10 @@ struct BlossomLinearBackward : public Node {
         if (want_x) out[0] = fresh(sizes, type, dev);
         if (want_w) out[1] = fresh({p.outs, p.cols}, type, dev);
         if (want_b) out[2] = fresh({p.outs}, type, dev);
-        const Tensor ws = fresh({(int64_t)blossom_linear_workspace_bytes(&p)}, at::kByte, dev);
         auto at = [](const Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; };
+        const bool reads_x = want_w || p.activation;
+        const size_t need = blossom_linear_bwd_workspace_bytes(&p, reads_x ? at(x) : nullptr, weight.data_ptr(), dout.data_ptr());
+        const Tensor ws = fresh({(int64_t)need}, at::kByte, dev);
         const int rc = blossom_linear_bwd(&p, at(x), static_cast<const uint8_t *>(at(scales)), weight.data_ptr(), at(bias),
                                           dout.data_ptr(), at(out[0]), at(out[1]), at(out[2]), ws.data_ptr(),
                                           (size_t)ws.nbytes(), stream_of(dout));

@@ -70,7 +70,28 @@ NarrowBackward from_row(const Args &a, const NarrowBackward &n, int64_t row) {
 }
 int64_t align8(int64_t n) { return (n + 7) / 8 * 8; }
 
-Scratch carve(const Args &a, void *base) {
+// What becomes of a backward whose tensors lie where these do: one kernel, for narrow layers, and from x as it is or its codes.
+struct Way {
+  bool one_kernel, x_as_it_is;
+};
+NarrowBackward narrow_of(const Args &a, const void *x, const uint8_t *scales, const void *weight, const void *dout) {
+  NarrowBackward n = {};
+  n.rows = a.rows, n.cols = a.cols, n.outs = a.outs, n.act = a.act;
+  n.weight = weight, n.ld_weight = a.sw, n.dout = dout, n.ld_dout = a.so, n.ld_dx = a.sdx;
+  if (a.packed) n.codes = static_cast<const int8_t *>(x), n.scales = scales;
+  else n.x = x, n.ld_x = a.sx;
+  return n;
+}
+Way way_of(const Args &a, const void *x, const void *weight, const void *dout) {
+  Way w = {};
+  if (few_backward(a) || a.esz != 2 || a.rows == 0) return w;
+  w.x_as_it_is = narrow_takes(narrow_of(a, x, nullptr, weight, dout));
+  // (codes can be turned into rows first)
+  w.one_kernel = w.x_as_it_is || (a.packed && narrow_takes(narrow_of(a, nullptr, nullptr, weight, dout)));
+  return w;
+}
+
+Scratch carve(const Args &a, const Way &way, void *base) {
   Scratch s;
   size_t off = 0;
   auto take = [&](size_t bytes) {
@@ -90,32 +111,34 @@ Scratch carve(const Args &a, void *base) {
     s.bytes = off;
     return s;
   }
+  s.x = take(a.packed && !way.x_as_it_is ? (size_t)a.rows * s.ld_x * a.esz : 0);
+  s.g = s.g_low = nullptr, s.splits = s.bias_parts = s.narrow = 0, s.dx_splits = 1;
+  if (way.one_kernel) {
+    for (int64_t r = 0; r < a.rows; r += narrow_rows(a)) s.narrow += narrow_splits(narrow_rows(a, r));
+    s.part = reinterpret_cast<float *>(take((size_t)s.narrow * a.outs * a.cols * sizeof(float)));
+    s.part_bias = reinterpret_cast<float *>(take((size_t)s.narrow * a.outs * sizeof(float)));
+    s.bytes = off;
+    return s;
+  }
   s.g = take(a.act ? (size_t)a.rows * s.ld_g * a.esz : 0);
   s.g_low = parts(a) == 2 ? take((size_t)a.rows * s.ld_g * a.esz) : nullptr;
-  s.x = take(a.packed ? (size_t)a.rows * s.ld_x * a.esz : 0);
   if (a.esz == 2) {
     s.splits = tc_splits(a.outs, a.cols, a.rows ? a.rows : 1, parts(a));
     s.bias_parts = tc_bias_parts(a.outs, a.cols, a.rows ? a.rows : 1, parts(a));
   } else {
     s.splits = s.bias_parts = f32_splits(a.outs, a.cols, a.rows ? a.rows : 1);
   }
-  s.narrow = 0;
-  if (a.esz == 2 && a.outs <= 256 && a.cols <= 256)
-    for (int64_t r = 0; r < a.rows; r += narrow_rows(a)) s.narrow += narrow_splits(narrow_rows(a, r));
   // dx of few tiles (all of a row's columns in one) over many outs leaves SMs idle: its sums are split as well (forward and backward in
   // single precision, us with splits and with a cluster a tile: 64 x 64 -> 1000 17.8, 23.0, 600 x 64 -> 1000 24.6, 31.5, but
   // 200 x 1000 -> 1000 37.8, 33.9).  So is dx over more outs than an accumulator adds up.
-  s.dx_splits = 1;
   const bool few_tiles = (int64_t)parts_of(a.rows, 128) * parts_of(a.cols, 128) < kSMs && a.outs >= 256,
              long_sums = a.esz == 2 && (int64_t)a.outs * parts(a) > kMostSlabs * 64;
   if ((few_tiles || long_sums) && a.rows)
     s.dx_splits = a.esz == 2 ? tc_splits(a.rows, a.cols, a.outs, parts(a)) : f32_splits(a.rows, a.cols, a.outs);
-  // (one split's sums go where they belong; the narrow layers' kernel leaves its own in any case)
-  const size_t sets = s.narrow || s.splits > 1 ? s.splits > s.narrow ? s.splits : s.narrow : 0;
-  const size_t sums = s.bias_parts > s.narrow ? s.bias_parts : s.narrow;
-  const size_t weight = sets * a.outs * (size_t)a.cols, dx = s.dx_splits > 1 ? (size_t)s.dx_splits * a.rows * a.cols : 0;
+  // (one split's sums go where they belong)
+  const size_t weight = s.splits > 1 ? (size_t)s.splits * a.outs * a.cols : 0, dx = s.dx_splits > 1 ? (size_t)s.dx_splits * a.rows * a.cols : 0;
   s.part = reinterpret_cast<float *>(take((weight > dx ? weight : dx) * sizeof(float)));
-  s.part_bias = reinterpret_cast<float *>(take(sums * a.outs * sizeof(float)));
+  s.part_bias = reinterpret_cast<float *>(take((size_t)s.bias_parts * a.outs * sizeof(float)));
   s.bytes = off;
   return s;
 }
@@ -138,7 +161,18 @@ int check_workspace(const void *p, size_t bytes, size_t need) {
 extern "C" size_t blossom_linear_workspace_bytes(const blossom_linear_params *params) {
   using namespace blossom;
   linear::Args a;
-  return linear::check(params, &a) ? 0 : linear::carve(a, nullptr).bytes;
+  if (linear::check(params, &a)) return 0;
+  // one kernel's partial sums may be more than what products after one another need
+  const linear::Way one = linear::way_of(a, nullptr, nullptr, nullptr);
+  const size_t any = linear::carve(a, {}, nullptr).bytes, single = one.one_kernel ? linear::carve(a, {true, false}, nullptr).bytes : 0;
+  return any > single ? any : single;
+}
+
+extern "C" size_t blossom_linear_bwd_workspace_bytes(const blossom_linear_params *params, const void *x, const void *weight,
+                                                     const void *dout) {
+  using namespace blossom;
+  linear::Args a;
+  return linear::check(params, &a) ? 0 : linear::carve(a, linear::way_of(a, x, weight, dout), nullptr).bytes;
 }
 
 extern "C" int blossom_linear_fwd(const blossom_linear_params *params, const void *x, const void *weight, const void *bias,
@@ -178,27 +212,20 @@ extern "C" int blossom_linear_bwd(const blossom_linear_params *params, const voi
   for (const void *p : {weight, bias, dout, (const void *)dx, (const void *)dweight, (const void *)dbias})
     if (linear::misaligned(p, a.esz)) return BLOSSOM_ERR_INVALID_ARG;
   if (!a.packed && linear::misaligned(x, a.esz)) return BLOSSOM_ERR_INVALID_ARG;
-  const linear::Scratch s = linear::carve(a, workspace);
+  const linear::Way way = linear::way_of(a, reads_x ? x : nullptr, weight, dout);
+  const linear::Scratch s = linear::carve(a, way, workspace);
   if (int rc = linear::check_workspace(workspace, workspace_bytes, s.bytes)) return rc;
   const cudaStream_t st = (cudaStream_t)stream;
   if (a.rows == 0) {  // sums over no rows
     if (cudaMemsetAsync(workspace, 0, 32, st) != cudaSuccess) return BLOSSOM_ERR_CUDA;
     return dweight || dbias ? linear::launch_join(a.dtype, s.part, s.part_bias, 0, 0, a.outs, a.cols, dweight, a.sdw, dbias, st) : BLOSSOM_OK;
   }
-  linear::NarrowBackward n = {};
-  n.rows = a.rows, n.cols = a.cols, n.outs = a.outs, n.act = a.act;
-  n.x = x, n.ld_x = a.sx, n.weight = weight, n.ld_weight = a.sw, n.bias = bias, n.dout = dout, n.ld_dout = a.so;
-  n.dx = dx, n.ld_dx = a.sdx, n.part = dweight ? s.part : nullptr, n.part_bias = dbias ? s.part_bias : nullptr, n.status = s.status;
-  if (a.packed) n.codes = static_cast<const int8_t *>(x), n.scales = x_scales;
-  if (!reads_x) n.codes = nullptr, n.x = nullptr;
-  const bool in_place = s.narrow && linear::narrow_takes(n);  // x as it is
   linear::Operand xo = {x, a.sx, true}, g = {dout, a.so, true};
-  if (a.packed && reads_x && !in_place) {
+  if (a.packed && reads_x && !way.x_as_it_is) {
     blossom_rows_params p = {};
     p.rows = a.rows, p.cols = a.cols, p.dtype = p.weight_dtype = a.dtype, p.out_stride = s.ld_x;
     if (int rc = blossom_unpack_rows(&p, static_cast<const int8_t *>(x), x_scales, s.x, stream)) return rc;
     xo = {s.x, s.ld_x, true};
-    n.codes = nullptr, n.x = s.x, n.ld_x = s.ld_x;
   }
   // (the first kernel clears the status words: a call for that alone would stand between two kernels that follow closely)
   if (linear::few_backward(a)) {
@@ -208,7 +235,10 @@ extern "C" int blossom_linear_bwd(const blossom_linear_params *params, const voi
     return linear::launch_few_backward(f, a.act ? s.g : dout, a.act ? s.ld_g : a.so, a.act != 0, s.part, dx, a.sdx, dweight, a.sdw, dbias,
                                        a.act ? nullptr : s.status, st);
   }
-  if (in_place || (s.narrow && linear::narrow_takes(n))) {
+  if (way.one_kernel) {
+    linear::NarrowBackward n = linear::narrow_of(a, reads_x ? x : nullptr, x_scales, weight, dout);
+    if (!way.x_as_it_is) n.codes = nullptr, n.scales = nullptr, n.x = xo.p, n.ld_x = xo.ld;
+    n.bias = bias, n.dx = dx, n.part = dweight ? s.part : nullptr, n.part_bias = dbias ? s.part_bias : nullptr, n.status = s.status;
     for (int64_t r = 0; r < a.rows; r += linear::narrow_rows(a)) {
       linear::NarrowBackward m = linear::from_row(a, n, r);
       if (int rc = linear::launch_narrow(m, st)) return rc;

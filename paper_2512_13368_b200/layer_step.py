@@ -132,7 +132,8 @@ def attention_share(batch=128, seq_len=1024, n_items=50000, negatives=127, steps
 
     Returns a dict: ms per step, ms of the library's attention kernels per step (summed device times from
     the per-launch event profile), their share, the same sum for its other kernels (0 without ``native`` and
-    ``products``), the memory that a forward keeps for its backward, and the loss of the last step.
+    ``products``), the memory that a forward keeps for its backward, the most that is in use during that beside the model (its gradients
+    included), and the loss of the last step.
     """
     torch.manual_seed(seed)
     dev = torch.device(device)
@@ -156,6 +157,9 @@ def attention_share(batch=128, seq_len=1024, n_items=50000, negatives=127, steps
     before = torch.cuda.memory_allocated(dev)
     loss = model.loss(ids, targets, neg)
     kept = torch.cuda.memory_allocated(dev) - before
+    torch.cuda.reset_peak_memory_stats(dev)
+    loss.backward()
+    peak = torch.cuda.max_memory_allocated(dev) - before
     del loss
     torch.cuda.synchronize(dev)
     e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
@@ -172,7 +176,7 @@ def attention_share(batch=128, seq_len=1024, n_items=50000, negatives=127, steps
     others = sum(ms for name, ms in launches if name.startswith(around)) / steps
     return {"ms_per_step": total, "attention_ms_per_step": ours, "attention_share": ours / total,
             "rows_and_loss_ms_per_step": others, "library_launches_per_step": len(launches) / steps,
-            "kept_mb": kept / 1e6, "loss": float(loss.detach())}
+            "kept_mb": kept / 1e6, "peak_mb": peak / 1e6, "loss": float(loss.detach())}
 
 
 if __name__ == "__main__":
