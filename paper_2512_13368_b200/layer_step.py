@@ -92,6 +92,8 @@ class BlossomEncoder(nn.Module):
     def __init__(self, n_items=50000, hidden=64, heads=2, ffn=256, layers=2, block=32, topk=8, window=64, native=False,
                  dropout=0.0, seed=0, products=False, packed=False):
         super().__init__()
+        if packed and not products:
+            raise ValueError("packed: only the library's linear layers (products) keep their inputs in 8 bits")
         self.native, self.dropout, self.products = native, dropout, products
         self.emb = nn.Embedding(n_items + 1, hidden, padding_idx=0)
         nn.init.normal_(self.emb.weight, std=0.02)
@@ -132,8 +134,8 @@ def attention_share(batch=128, seq_len=1024, n_items=50000, negatives=127, steps
 
     Returns a dict: ms per step, ms of the library's attention kernels per step (summed device times from
     the per-launch event profile), their share, the same sum for its other kernels (0 without ``native`` and
-    ``products``), the memory that a forward keeps for its backward, the most that is in use during that beside the model (its gradients
-    included), and the loss of the last step.
+    ``products``), the memory that a forward keeps for its backward, the most that is in use during that beside
+    the model (its gradients included), and the loss of the last step.
     """
     torch.manual_seed(seed)
     dev = torch.device(device)
@@ -188,5 +190,7 @@ if __name__ == "__main__":
     args.add_argument("--products", action="store_true", help="embedding and linear layers in the library")
     args.add_argument("--packed", action="store_true", help="with --products: the feed-forward block's inputs kept in 8 bits")
     opts = args.parse_args()
+    if opts.packed and not opts.products:
+        args.error("--packed goes with --products")
     binding.load()
     print(json.dumps(attention_share(native=opts.native, dropout=opts.dropout, products=opts.products, packed=opts.packed)))

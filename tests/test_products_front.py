@@ -113,3 +113,16 @@ def test_a_backward_captured_while_an_eager_graph_of_other_leaves_lives(packed):
         want = step(own)
         assert torch.equal(got[0], want[0]) and all(torch.equal(x, y) for x, y in zip(got[1], want[1]))
     assert alive[0].requires_grad
+
+
+def test_inputs_in_8_bits_are_for_the_librarys_layers():
+    """A layer case that would ignore `packed` says so."""
+    import subprocess
+    import sys
+
+    from paper_2512_13368_b200.layer_step import BlossomEncoder
+    with pytest.raises(ValueError, match="products"):
+        BlossomEncoder(n_items=10, hidden=32, packed=True)
+    BlossomEncoder(n_items=10, hidden=32, products=True, packed=True)
+    run = subprocess.run([sys.executable, "-m", "paper_2512_13368_b200.layer_step", "--native", "--packed"], capture_output=True, text=True)
+    assert run.returncode == 2 and "--products" in run.stderr
