@@ -2,7 +2,7 @@
 #pragma once
 #include <math.h>
 
-#include "common.cuh"
+#include "rows.cuh"
 
 namespace blossom {
 namespace linear {
@@ -38,13 +38,7 @@ __device__ __forceinline__ float2 at_most(float2 x, float most) { return make_fl
 // derivative is 0 or 1 to 4e-8, from x = -6 down the value is 0 to 6e-9: arguments are cut there, so that
 // infinite ones have their limits.
 constexpr float kLog2e = 1.4426950408889634f;
-__device__ __forceinline__ float2 mul2f(float2 a, float2 b) {
-  uint64_t d;
-  asm("mul.rn.ftz.f32x2 %0, %1, %2;"
-      : "=l"(d)
-      : "l"(*reinterpret_cast<uint64_t *>(&a)), "l"(*reinterpret_cast<uint64_t *>(&b)));
-  return *reinterpret_cast<float2 *>(&d);
-}
+using rows::mul2;
 // a constant in a pair of registers (which the compiler would otherwise fill anew for every use)
 __device__ __forceinline__ float2 held(float v) {
   float2 p = make_float2(v, v);
@@ -110,16 +104,16 @@ struct Curve {
       if constexpr (SLOPE) x = at_most(x, kCut);
       float2 t = x, u = p[0];
       if constexpr (kGelu) {
-        t = mul2f(x, x);
+        t = mul2(x, x);
         u = scaled_p(t);
       }
-      const float2 s = sigmoid2(mul2f(x, u));
-      if constexpr (!SLOPE) return mul2f(x, s);
+      const float2 s = sigmoid2(mul2(x, u));
+      if constexpr (!SLOPE) return mul2(x, s);
       if constexpr (kGelu) {  // Phi + x phi
-        const float2 v = mul2f(t, half);
-        return fma2(mul2f(x, top), make_float2(exp2f(v.x), exp2f(v.y)), s);
+        const float2 v = mul2(t, half);
+        return fma2(mul2(x, top), make_float2(exp2f(v.x), exp2f(v.y)), s);
       }
-      return mul2f(s, add2(mul2f(x, fma2(s, minus, one)), one));
+      return mul2(s, add2(mul2(x, fma2(s, minus, one)), one));
     }
     return x;
   }

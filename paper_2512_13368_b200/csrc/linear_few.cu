@@ -7,7 +7,6 @@
 //   dx       a thread has 4 columns and all rows, a block a share of the outs; the shares' sums are added up behind it
 //   dweight  a thread has 4 columns of all rows of x in registers and goes down the outs
 #include "linear.cuh"
-#include "rows.cuh"
 
 namespace blossom {
 namespace linear {

@@ -1,7 +1,6 @@
 // Products on the tensor cores: what the kernel for matrices of any size and the one for narrow layers share.
 #pragma once
 #include "linear.cuh"
-#include "rows.cuh"
 #include "tc_common.cuh"
 
 namespace blossom {
@@ -179,7 +178,7 @@ __device__ __forceinline__ uint4 finish8_parts(const C &curve, const float *y, c
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const float2 b = *reinterpret_cast<const float2 *>(bias + 2 * i);
-    const float2 g = mul2f(curve(add2(make_float2(y[2 * i], y[2 * i + 1]), b)), rows::halves(d[i]));
+    const float2 g = mul2(curve(add2(make_float2(y[2 * i], y[2 * i + 1]), b)), rows::halves(d[i]));
     h[i] = tc::pack_bf16(g.x, g.y);
     const float2 f = rows::halves(h[i]);
     l[i] = remainders(tc::pack_bf16(g.x - f.x, g.y - f.y));

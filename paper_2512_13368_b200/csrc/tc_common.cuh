@@ -558,7 +558,11 @@ __device__ __forceinline__ void store_row_chunk(uint8_t *tile, int r, int ch, ui
   else *reinterpret_cast<uint4 *>(tile + r * 64 + ((ch ^ ((r >> 1) & 3)) << 4)) = v;
 }
 
-// ---- host: TMA descriptor of a q-shaped bf16 tensor, box = (D, rows, 1, 1) -----------------
+// ---- host: TMA descriptors ---------------------------------------------------------------
+// Of a bf16 tensor of 2 to 4 dimensions, the innermost first, and the strides of the others in bytes; false if the driver refuses.
+bool encode_map(CUtensorMap *map, const void *base, int rank, const cuuint64_t *dims, const cuuint64_t *strides, const cuuint32_t *box,
+                CUtensorMapSwizzle swizzle);
+// Of a q-shaped bf16 tensor, box = (D, rows, 1, 1); 0 if that went well
 int make_tensor_map(CUtensorMap *map, const void *base, const Shape &s, int box_rows, bool kv = false,
                     int box_heads = 1);
 

@@ -21,29 +21,32 @@ static EncodeTiledFn encode_fn() {
   return fn;
 }
 
+bool encode_map(CUtensorMap *map, const void *base, int rank, const cuuint64_t *dims, const cuuint64_t *strides, const cuuint32_t *box,
+                CUtensorMapSwizzle swizzle) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  const cuuint32_t one[4] = {1, 1, 1, 1};
+  for (int attempt = 0; attempt < 2; ++attempt) {
+    if (fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void *>(base), dims, strides, box, one,
+           CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS)
+      return true;
+    // the driver call wants a current context, which a thread that has made no runtime call yet (autograd's)
+    // lacks: make the device's own current and try once more
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaSetDevice(dev) != cudaSuccess) return false;
+  }
+  return false;
+}
+
 // q-shaped bf16 tensor [B][H][L][D] with the caller's strides, box = (D, box_rows, box_heads, 1)
 // (the box's heads follow one another in shared memory, box_rows rows each); rows past L read as zeros.  The swizzle matches the shared-memory descriptors of the kernels.
 int make_tensor_map(CUtensorMap *map, const void *base, const Shape &s, int box_rows, bool kv, int box_heads) {
-  EncodeTiledFn fn = encode_fn();
-  if (!fn) return 1;
   // kv: a key/value-shaped tensor [B][Hkv][L][D] with its own strides
   const cuuint64_t dims[4] = {(cuuint64_t)s.D, (cuuint64_t)s.L, (cuuint64_t)(kv ? s.Hkv : s.H), (cuuint64_t)s.B};
   const cuuint64_t strides[3] = {(cuuint64_t)(kv ? s.ksl : s.sl) * 2, (cuuint64_t)(kv ? s.ksh : s.sh) * 2,
                                  (cuuint64_t)(kv ? s.ksb : s.sb) * 2};
   const cuuint32_t box[4] = {(cuuint32_t)s.D, (cuuint32_t)box_rows, (cuuint32_t)box_heads, 1};
-  const cuuint32_t estr[4] = {1, 1, 1, 1};
-  const CUtensorMapSwizzle sw = s.D == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B;
-  for (int attempt = 0; attempt < 2; ++attempt) {
-    if (fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(base), dims, strides, box, estr,
-           CU_TENSOR_MAP_INTERLEAVE_NONE, sw, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
-           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS)
-      return 0;
-    // the driver call wants a current context, which a thread that has made no runtime call yet (autograd's)
-    // lacks: make the device's own current and try once more
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaSetDevice(dev) != cudaSuccess) return 1;
-  }
-  return 1;
+  return encode_map(map, base, 4, dims, strides, box, s.D == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B) ? 0 : 1;
 }
 
 // Diagnostic kernel: the bounded-wait machinery of the attention kernels on a wait that cannot
