@@ -130,9 +130,10 @@ Scratch carve(const Args &a, const Way &way, void *base) {
   }
   // dx of few tiles (all of a row's columns in one) over many outs leaves SMs idle: its sums are split as well (forward and backward in
   // single precision, us with splits and with a cluster a tile: 64 x 64 -> 1000 17.8, 23.0, 600 x 64 -> 1000 24.6, 31.5, but
-  // 200 x 1000 -> 1000 37.8, 33.9).  So is dx over more outs than an accumulator adds up.
+  // 200 x 1000 -> 1000 37.8, 33.9).  So is dx over more than the forward's most
+  // steps in one accumulator.
   const bool few_tiles = (int64_t)parts_of(a.rows, 128) * parts_of(a.cols, 128) < kSMs && a.outs >= 256,
-             long_sums = a.esz == 2 && (int64_t)a.outs * parts(a) > kMostSlabs * 64;
+             long_sums = a.esz == 2 && a.outs * parts(a) > kMaxWidth;
   if ((few_tiles || long_sums) && a.rows)
     s.dx_splits = a.esz == 2 ? tc_splits(a.rows, a.cols, a.outs, parts(a)) : f32_splits(a.rows, a.cols, a.outs);
   // (one split's sums go where they belong)

@@ -167,7 +167,7 @@ struct Epilogue {
 // n / by, rounded up (n may be the largest int)
 inline int parts_of(int n, int by) { return (int)(((int64_t)n + by - 1) / by); }
 
-constexpr int kMostSlabs = 1024;  // of 64 steps of k in one accumulator of a bf16 product
+constexpr int kMostSlabs = 256;  // of 64 rows in one accumulator of a bf16 product over the rows
 // Tensor cores, bf16, any alignment.  No split of k may be empty.
 int launch_tc(int kernel_id, Mode mode, const Operand &a, const Operand &b, int m, int n, int k, const Epilogue &e, int32_t *status,
               cudaStream_t st);

@@ -399,7 +399,8 @@ int tc_splits(int m, int n, int k, int parts) {
   // back 8 bytes at 3500 a clock.  Forward and backward, us with 1, 4, 9, 16, 37 splits: 5000 x 512 -> 512 45, 32, 31, 31, 45 (the rule:
   // 32); 2000 x 1024 -> 1024 with GELU 60, 81, 100, 155, 214 (60).
   // No accumulator adds up more than kMostSlabs, those of both parts of A: it cuts its sums, which loses 2e-6 of sums of one sign
-  // over 1024 steps of k.
+  // over 1024 steps of k.  (32768 x 1024 -> 4096 with GELU: dweight is 3e-5 too small with 256 slabs, 5e-5 with 512 and 1e-4 with
+  // 1024, where plain single precision loses 5e-6 and the rounding to bf16 is off by 1.7e-3; the step takes 1767, 1744, 1746 us.)
   const int64_t slabs = parts_of(k, kK), mt = parts_of(m, kM), fewest = parts_of((int)slabs, kMostSlabs / parts);
   int best = 1;
   double least = 1e30;

@@ -25,8 +25,8 @@ def test_sizes():
     _, here = sizes(131072, 64, 256, "bf16", "gelu", True)
     assert 131072 * 64 * 2 <= here <= 131072 * 64 * 2 + 11 * MB
     # as many rows at a time as an accumulator may add up
-    for rows, cols, outs, act, splits in ((148 * 65536, 256, 64, "none", 148), (148 * 65536 + 1, 256, 64, "none", 149),
-                                          (148 * 32768, 64, 256, "gelu", 148), (148 * 65536, 64, 256, "gelu", 296)):
+    for rows, cols, outs, act, splits in ((148 * 16384, 256, 64, "none", 148), (148 * 16384 + 1, 256, 64, "none", 149),
+                                          (148 * 8192, 64, 256, "gelu", 148), (148 * 16384, 64, 256, "gelu", 296)):
         _, here = sizes(rows, cols, outs, "bf16", act)
         sums = splits * outs * (cols + 1) * 4
         assert sums <= here <= sums + 4096, (rows, act)
