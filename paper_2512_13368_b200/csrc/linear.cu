@@ -47,7 +47,7 @@ struct Scratch {
 };
 // Between the products G is bf16.  Rounded to one its error is as large as the results' own rounding (together 1.4 times that), so
 // what the rounding leaves goes through the products as a second part of G, which makes that of dx and dweight twice the work:
-// 32768 x 1024 -> 4096 1145 us without, 1721 with it (8192 x 1024 -> 1024 128 and 165).
+// forward and backward of 32768 x 1024 -> 4096 1145 us without, 1721 with it, of 8192 x 1024 -> 1024 128 and 165.
 int parts(const Args &a) { return a.act && a.esz == 2 ? 2 : 1; }
 // Few rows go to kernels of their own rather than to tiles of 128 rows that are mostly empty.  Forward, us against tiles: single
 // precision 1, 16 rows of 1024 -> 4096 4.8, 19.4 against 23; bf16 1, 4, 8, 16 rows 4.1, 4.9, 8.8, 14.5 against 8.  Forward and
@@ -276,7 +276,7 @@ extern "C" int blossom_linear_bwd(const blossom_linear_params *params, const voi
     linear::Epilogue e;
     e.first = !a.act && !dx;
     e.part = dweight ? s.part : nullptr, e.part_bias = dbias ? s.part_bias : nullptr, e.splits = s.splits;
-    // one split's sums are the results (32768 x 1024 -> 4096 with GELU: 1106 us; by way of single precision 1132)
+    // one split's sums are the results (32768 x 1024 -> 4096 with GELU as one: 1106 us; by way of single precision 1132)
     const bool direct = s.splits == 1 && dweight;
     if (direct) e.out = dweight, e.ld_out = a.sdw;
     const bool direct_bias = s.bias_parts == 1 && dbias && a.esz == 4;

@@ -2,8 +2,10 @@
 //
 // Bound: memory.  dout and x are read once and dx is written once, where three products after one another would write and
 // read the upstream gradient behind the activation (G) as well, and x and dout twice.  131072 x 64 -> 192 21 us, 84 MB at 4.0 TB/s;
-// 131072 x 64 -> 256 with GELU 62 us, 101 MB: there it is the issue slots, forming G takes 4500 of a step's 6000 clocks beside
-// 3400 of products.  (Forward and backward 41 and 93 us; with three products 49 and 152.)
+// 131072 x 64 -> 256 with GELU 67 us, 101 MB: there it is forming G, an exponential, a reciprocal and an exponential an element (22 us
+// of the special function units) and what is around them, by warps that empty the dx of the tile before as well (schedulers issue in
+// 49 % of the cycles, the first stall is the wait for loads).  (Forward and backward 41 and 97 us; with three products, and a
+// shorter polynomial for GELU, 49 and 152 where this took 93.)
 //
 // A CTA an SM walks tiles of 128 rows.  x and dout of a tile come by TMA (or x from its 8 bits, see below), the weight once.  Per tile
 //   pre = x W^T           (with an activation)   128 x outs   rows of x and of the weight along k

@@ -10,10 +10,11 @@
 // Epilogue: a warp has 32 rows and 32 columns at a time.  A row is a thread's (its lane of tensor memory); memory is touched by
 // whole rows of the 32 columns, four lanes a row, and shared memory turns one into the other.
 //
-// Bound: 131072 x 64 -> 256 with GELU 24 us, the epilogue's instructions (84 MB, 3.5 TB/s; two accumulators 26, one and half the
-// warps 31);
-// 32768 x 1024 -> 4096 209 us forward, 223 dx, 262 dW, the power (1.3 PFLOP/s, 94 % of what a library product sustains; dW's 128
-// tiles leave 20 SMs idle).
+// Bound: 131072 x 64 -> 256 with GELU 27 us, the epilogue's instructions (84 MB, 3.1 TB/s; with a shorter polynomial 24, then two
+// accumulators 26, one and half the warps 31);
+// 32768 x 1024 -> 4096 209 us forward, 223 dx, 272 dW and 29 the join of its two splits, the power (1.3 PFLOP/s, 94 % of what a
+// library product sustains).  Rows that TMA does not take cost more the narrower the access: 32768 x 1023 -> 4096 2011 us forward,
+// 2351 dx, 3266 dW, 96 loads of two bytes a thread and slab; 60000 x 490 -> 470 127, 121, 111 where 496 -> 472 takes 43, 45, 41.
 #include "linear_tc.cuh"
 
 namespace blossom {
@@ -381,8 +382,8 @@ bool make_map(CUtensorMap *map, const void *base, int64_t rows, int64_t cols, in
 
 // Columns of a tile.  What a tile costs beside its columns (its rows' operand, hand-offs) weighs as 64 of them, as 24 where the
 // epilogue bounds (ends: few slabs, by TMA) and four accumulators hide the hand-offs: the width with the least work of the busiest SM.
-// Forward, us with 64, 128, 192, 256 columns: 131072 x 64 -> 192 15.3, 18.4, 14.3, 15.4; 131072 x 64 -> 256 with GELU 26.5, 24.2, 36.8,
-// 26.2; x 256 -> 64 10.4, 15.3, 20.1, 26.9; 32768 x 1024 -> 4096 with GELU 398, 264, 243, 232.
+// Forward, us with 64, 128, 192, 256 columns: 131072 x 64 -> 192 15.3, 18.4, 14.3, 15.4; 131072 x 64 -> 256 with GELU 29.9, 27.4, 36.8,
+// 29.7; x 256 -> 64 10.4, 15.3, 20.1, 26.9; 32768 x 1024 -> 4096 with GELU 398, 264, 243, 232.
 int tile_columns(int m, int n, int splits, bool ends) {
   const int64_t mt = ((int64_t)m + kM - 1) / kM * splits;
   int best = 64;
