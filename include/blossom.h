@@ -408,9 +408,9 @@ int blossom_unpack_rows(const blossom_rows_params *params /* host */, const int8
  *
  * Products are summed in single precision on the tensor cores, float32 numbers as the sum of three bf16; the tensor cores cut their
  * sums instead of rounding them, bf16 products over 16384 rows or over all columns or outs at a time, by 2^-23 of the sum for 16
- * steps at most.  What follows is done in single precision, and the result is rounded once.  The argument of the activation is not kept: the backward forms it again
- * from x.  The same call gives the same bits.  Subnormal numbers may be taken for zeros, and of float32 numbers below 2^-109 the
- * parts that are subnormal; a float32 infinity may come out as what is no number.  Phi is the sigmoid of a polynomial: GELU is
+ * steps at most.  What follows is done in single precision, and the result is rounded once.  The argument of the activation is
+ * not kept: the backward forms it again from x.  The same call gives the same bits.  Subnormal numbers may be taken for zeros, and
+ * of float32 numbers below 2^-109 the parts that are subnormal; a float32 infinity may come out as what is no number.  Phi is the sigmoid of a polynomial: GELU is
  * off, beside its roundings, by 2^-10 of itself for bf16 and by 2^-23 for float32 results, its derivative by 2^-22;
  * arguments below -6 have the value of -6, -6e-9 (of SiLU below -40: -2e-16).
  */
